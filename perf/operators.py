@@ -192,7 +192,7 @@ def prepare(c, seed):
                                  prefix_pages_dev=st["prefix_pages"] if prefix else None)
         if c["op"] == "append":
             q, k, v = st["qkv"].split([c["heads"], c["kv_heads"], c["kv_heads"]], dim=1)
-            st["new"] = dc.KVRows(kind[c["x_type"]], c["heads"], k, v, q, st["out"], row_stride=q.stride(0), rot_dim=c["rot"],
+            st["new"] = dc.KVRows(kind[c["x_type"]], c["heads"], k, v, q, st["out"], rot_dim=c["rot"],
                                   pairing={"halves": dc.ROPE_HALVES, "neighbours": dc.ROPE_NEIGHBOURS}[c["pairing"]], cos_dev=st["cos"],
                                   sin_dev=st["sin"], n_positions=c["len"])
         else:
