@@ -495,6 +495,112 @@ int dc_gemv_i8(const int8_t *q_dev, const float *row_scale_dev, uint32_t rows, u
                const uint16_t *x_bf16_dev, float *y_f32_dev, uint16_t *y_bf16_dev, void *hip_stream);
 
 /*
+ * What a decoder layer does between its products: keys and values in pages, and the attention that reads them
+ * ------------------------------------------------------------------------------------------------------------
+ * A layer whose weights stay compressed is run as query/key/value products (dc_decompress_gemv_layer), dc_kv_append,
+ * dc_attention_paged, output product, and the feed-forward products.  The two calls here work for one new token a
+ * sequence (generation) as for many (prompts and pieces of prompts), for any number of sequences of different lengths.
+ *
+ * Cache.  k_dev and v_dev are pools of n_pages pages; a page holds page_tokens tokens of every key/value head:
+ * element [page][head][token][i], i < head_dim, type bf16 or f16.  16-byte aligned; offsets are 64-bit.
+ *
+ * Batch.  Sequence b has len_dev[b] tokens, the new ones included; its new tokens are its last ones and their rows
+ * (queries, keys, values, results) stand one after the other: rows row_start_dev[b] .. row_start_dev[b+1]-1.
+ * So row r of sequence b has position p = len_dev[b] - row_start_dev[b+1] + r.  The token at position j is token
+ * j mod page_tokens of page pages_dev[b * pages_stride + j / page_tokens].  An entry outside [0, n_pages) (say -1) is a page
+ * that is not there: its tokens are seen by no row, and not written.  A program with a sliding window gives such pages back.
+ * With prefix_len > 0 all sequences begin with the same prefix_len tokens, which are held once: position j < prefix_len is token
+ * j mod page_tokens of page prefix_pages_dev[j / page_tokens], and pages_dev covers the positions from prefix_len on (counted from
+ * there).  prefix_len need not be a multiple of page_tokens.
+ * The device arrays are not read by the host.  Whatever they hold, the kernels read and write only inside the pools, the rows
+ * [0, n_rows) and the arrays' stated sizes: positions beyond pages_stride * page_tokens are not there, rows that belong to
+ * no sequence are left alone.
+ */
+#define DC_TYPE_BF16 0
+#define DC_TYPE_F16 1
+#define DC_TYPE_F32 2 /* rows given to dc_kv_append only */
+
+/* which values of a head turn as a pair, i < rot_dim / 2 */
+#define DC_ROPE_HALVES 0     /* i and i + rot_dim / 2 */
+#define DC_ROPE_NEIGHBOURS 1 /* 2 i and 2 i + 1 */
+
+typedef struct {
+    uint32_t type;        /* DC_TYPE_BF16 or DC_TYPE_F16 */
+    uint32_t n_kv_heads;  /* 1 .. 65535 */
+    uint32_t head_dim;    /* 64, 128 or 256 */
+    uint32_t page_tokens; /* 16, 32, 64, 128 or 256 */
+    uint32_t n_pages;     /* 1 .. 2^31 - 1 */
+    void *k_dev;
+    void *v_dev;
+} dc_kv_cache;
+
+typedef struct {
+    uint32_t n_seqs;       /* 1 .. 65535 */
+    uint32_t n_rows;       /* rows in the row buffers; below 2^31 */
+    uint32_t max_new;      /* no sequence has more rows than this (more are left alone), 1 .. n_rows */
+    uint32_t max_len;      /* about the largest length: work is split by it; results do not depend on it beyond rounding */
+    uint32_t pages_stride; /* entries of a sequence's row of pages_dev; prefix_len + pages_stride * page_tokens < 2^31 */
+    uint32_t prefix_len;   /* 0: no common prefix */
+    const int32_t *len_dev;          /* n_seqs */
+    const int32_t *pages_dev;        /* n_seqs * pages_stride */
+    const int32_t *row_start_dev;    /* n_seqs + 1, or NULL: row b is the one new token of sequence b (n_rows == n_seqs, max_new == 1) */
+    const int32_t *prefix_pages_dev; /* ceil(prefix_len / page_tokens); NULL when prefix_len is 0 */
+} dc_kv_batch;
+
+/* New tokens for the cache.  A row of queries is element [row * q_row_stride + head * q_head_stride + i], likewise the others;
+ * strides count elements and are multiples of 8, so that rows may be parts of one fused query/key/value row.  All pointers
+ * 16-byte aligned. */
+typedef struct {
+    uint32_t type;        /* DC_TYPE_* of q, k, v */
+    uint32_t n_heads;     /* query heads; 0: no queries (q_dev and q_out_dev are not read) */
+    uint32_t rot_dim;     /* values of a head that turn, its first ones: 0 or a multiple of 16, at most head_dim */
+    uint32_t pairing;     /* DC_ROPE_* */
+    uint32_t n_positions; /* rows of cos_dev and sin_dev */
+    const void *k_dev, *v_dev, *q_dev;
+    void *q_out_dev;      /* turned queries, type of the cache; may be q_dev itself (same type and strides) */
+    uint64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride, q_row_stride, q_head_stride, q_out_row_stride, q_out_head_stride;
+    const float *cos_dev, *sin_dev;  /* fp32 [n_positions][rot_dim / 2]; NULL when rot_dim is 0 */
+    const int32_t *position_dev;     /* n_rows: the row of cos_dev and sin_dev for each row; NULL: the token's position */
+} dc_kv_rows;
+
+/*
+ * Rotary positions and cache append.  For every row of the batch, with c and s the row's cosines and sines, a pair (a, b) of every
+ * query and key head becomes (a c_i - b s_i, b c_i + a s_i), evaluated in fp32 and rounded once to the cache's type; values are only
+ * rounded.  Queries go to q_out_dev, keys and values into the pages.  A row whose cosines lie outside the table (rot_dim > 0) is
+ * left out as a whole, one whose page is not there is not put into the cache.  Positions below prefix_len belong to the prefix
+ * and are written there.  Two rows of one call must not share a place in the cache.  One launch.
+ * Errors: DC_E_ARG, DC_E_HIP.
+ */
+int dc_kv_append(const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_kv_rows *rows, void *hip_stream);
+
+typedef struct {
+    uint32_t n_heads; /* query heads, a multiple of n_kv_heads: query head h reads key/value head h / (n_heads / n_kv_heads) */
+    uint32_t window;  /* 0: a row sees all positions j <= p; else p - window < j <= p */
+    uint32_t sinks;   /* the first positions j < sinks (j <= p) are seen whatever the window */
+    float scale;      /* finite */
+    const void *q_dev; /* type of the cache; 16-byte aligned, strides as in dc_kv_rows */
+    void *out_dev;     /* type of the cache, likewise; not q_dev */
+    float *lse_dev;    /* fp32 [n_rows][n_heads], may be NULL */
+    uint64_t q_row_stride, q_head_stride, out_row_stride, out_head_stride;
+} dc_attention;
+
+/*
+ * Attention of the batch's rows over the cache.  With s_j = scale * (q . k_j) over the positions j that a row sees:
+ *   out = sum_j exp(s_j - lse) v_j,   lse = log sum_j exp(s_j)   (natural logarithm).
+ * A row that sees nothing (or only s_j = -inf) has out = 0 and lse = -inf.  What is not seen has no influence, NaN and infinities
+ * included: tokens beyond a sequence's length, behind its window, or on pages that are not there may hold anything.
+ * Scores, sums and results are held in fp32; exp(s_j - reference) is rounded to the cache's type for the product with the values.
+ * A common prefix (prefix_len > 0) is read once for all sequences' rows together.
+ *   workspace_dev   at least dc_attention_paged_workspace() bytes, 16-byte aligned (NULL if that is 0); its contents before the
+ *                   call do not matter, and it may be reused once the call's work on the stream is done
+ * Errors: DC_E_ARG, DC_E_CAP (workspace too small), DC_E_HIP.
+ */
+int dc_attention_paged_workspace(const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_attention *attention,
+                                 uint64_t *workspace_bytes);
+int dc_attention_paged(const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_attention *attention, void *workspace_dev,
+                       uint64_t workspace_bytes, void *hip_stream);
+
+/*
  * Plain device copy kernel (reads n bytes, writes n bytes, 16-byte aligned): the denominator for
  * "share of achievable bandwidth" next to the decode kernels (cf. B_gpu in Eq. 11).
  */

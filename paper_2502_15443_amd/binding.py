@@ -21,6 +21,8 @@ FORMAT_ID = 5  # DC_FORMAT_ID of include/dc.h
 CHUNK_RAW = 0x80000000
 STATIC_SCRATCH_BYTES = 16 << 20
 TRACE_DECODED, TRACE_COPIED, TRACE_SKIPPED = 0, 1, 2
+TYPE_BF16, TYPE_F16, TYPE_F32 = 0, 1, 2
+ROPE_HALVES, ROPE_NEIGHBOURS = 0, 1
 CHUNK_DTYPE = np.dtype([("off", "<u8"), ("comp_bytes", "<u4"), ("raw_bytes_flags", "<u4")])
 
 
@@ -77,6 +79,73 @@ class Params:
             self._mask_keepalive = np.ascontiguousarray(self.raw_mask, dtype=np.uint8)
             p.raw_mask = self._mask_keepalive.ctypes.data
         return p
+
+
+def _strides(t, given) -> Tuple[int, int]:
+    """(row stride, head stride) in elements: as given, or those of a tensor [rows, heads, head_dim]."""
+    if given is not None:
+        return int(given[0]), int(given[1])
+    if t is None:
+        return 0, 0
+    if isinstance(t, int) or t.dim() != 3 or t.stride(2) != 1:
+        raise ValueError("rows are a tensor [rows, heads, head_dim] with contiguous heads; for addresses give the strides")
+    return t.stride(0), t.stride(1)
+
+
+class KVCache(C.Structure):
+    """Keys and values in pages (dc_kv_cache).  Made once beside the buffers, which it keeps alive."""
+    _fields_ = [("type", C.c_uint32), ("n_kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("page_tokens", C.c_uint32),
+                ("n_pages", C.c_uint32), ("k_dev", C.c_void_p), ("v_dev", C.c_void_p)]
+
+    def __init__(self, k_dev, v_dev, n_pages: int, n_kv_heads: int, head_dim: int, page_tokens: int, type: int = TYPE_BF16):
+        super().__init__(type, n_kv_heads, head_dim, page_tokens, n_pages, _dev(k_dev) or None, _dev(v_dev) or None)
+        self._buffers = (k_dev, v_dev)
+
+
+class KVBatch(C.Structure):
+    """Sequences and the rows of their new tokens (dc_kv_batch).  The device arrays may be rewritten between calls."""
+    _fields_ = [("n_seqs", C.c_uint32), ("n_rows", C.c_uint32), ("max_new", C.c_uint32), ("max_len", C.c_uint32),
+                ("pages_stride", C.c_uint32), ("prefix_len", C.c_uint32), ("len_dev", C.c_void_p), ("pages_dev", C.c_void_p),
+                ("row_start_dev", C.c_void_p), ("prefix_pages_dev", C.c_void_p)]
+
+    def __init__(self, n_seqs: int, n_rows: int, max_new: int, max_len: int, len_dev, pages_dev, pages_stride: int,
+                 row_start_dev=None, prefix_len: int = 0, prefix_pages_dev=None):
+        super().__init__(n_seqs, n_rows, max_new, max_len, pages_stride, prefix_len, _dev(len_dev) or None, _dev(pages_dev) or None,
+                         _dev(row_start_dev) or None, _dev(prefix_pages_dev) or None)
+        self._buffers = (len_dev, pages_dev, row_start_dev, prefix_pages_dev)
+
+
+class KVRows(C.Structure):
+    """New keys, values and queries (dc_kv_rows): tensors [rows, heads, head_dim] of any strides, or addresses with
+    (row stride, head stride) pairs in elements."""
+    _fields_ = [("type", C.c_uint32), ("n_heads", C.c_uint32), ("rot_dim", C.c_uint32), ("pairing", C.c_uint32),
+                ("n_positions", C.c_uint32), ("k_dev", C.c_void_p), ("v_dev", C.c_void_p), ("q_dev", C.c_void_p),
+                ("q_out_dev", C.c_void_p), ("k_row_stride", C.c_uint64), ("k_head_stride", C.c_uint64),
+                ("v_row_stride", C.c_uint64), ("v_head_stride", C.c_uint64), ("q_row_stride", C.c_uint64),
+                ("q_head_stride", C.c_uint64), ("q_out_row_stride", C.c_uint64), ("q_out_head_stride", C.c_uint64),
+                ("cos_dev", C.c_void_p), ("sin_dev", C.c_void_p), ("position_dev", C.c_void_p)]
+
+    def __init__(self, type: int, n_heads: int, k_dev, v_dev, q_dev=None, q_out_dev=None, *, rot_dim: int = 0,
+                 pairing: int = ROPE_HALVES, cos_dev=None, sin_dev=None, n_positions: int = 0, position_dev=None, k_strides=None,
+                 v_strides=None, q_strides=None, q_out_strides=None):
+        super().__init__(type, n_heads, rot_dim, pairing, n_positions, _dev(k_dev) or None, _dev(v_dev) or None, _dev(q_dev) or None,
+                         _dev(q_out_dev) or None, *_strides(k_dev, k_strides), *_strides(v_dev, v_strides),
+                         *_strides(q_dev, q_strides), *_strides(q_out_dev, q_out_strides), _dev(cos_dev) or None,
+                         _dev(sin_dev) or None, _dev(position_dev) or None)
+        self._buffers = (k_dev, v_dev, q_dev, q_out_dev, cos_dev, sin_dev, position_dev)
+
+
+class Attention(C.Structure):
+    """What dc_attention_paged reads and writes beside the cache (dc_attention): q and out as in KVRows, lse fp32 [rows, heads]."""
+    _fields_ = [("n_heads", C.c_uint32), ("window", C.c_uint32), ("sinks", C.c_uint32), ("scale", C.c_float),
+                ("q_dev", C.c_void_p), ("out_dev", C.c_void_p), ("lse_dev", C.c_void_p), ("q_row_stride", C.c_uint64),
+                ("q_head_stride", C.c_uint64), ("out_row_stride", C.c_uint64), ("out_head_stride", C.c_uint64)]
+
+    def __init__(self, n_heads: int, q_dev, out_dev, lse_dev, scale: float, *, window: int = 0, sinks: int = 0, q_strides=None,
+                 out_strides=None):
+        super().__init__(n_heads, window, sinks, float(scale), _dev(q_dev) or None, _dev(out_dev) or None, _dev(lse_dev) or None,
+                         *_strides(q_dev, q_strides), *_strides(out_dev, out_strides))
+        self._buffers = (q_dev, out_dev, lse_dev)
 
 
 def lib_path() -> str:
@@ -155,6 +224,13 @@ def _load():
     L.dc_gemv_w8a8.argtypes = [vp, vp, u32, u32, vp, C.c_float, vp, vp, vp]
     L.dc_quantize_vector.restype = i32
     L.dc_quantize_vector.argtypes = [vp, u32, vp, vp]
+    pc, pb, pr, pa = C.POINTER(KVCache), C.POINTER(KVBatch), C.POINTER(KVRows), C.POINTER(Attention)
+    L.dc_kv_append.restype = i32
+    L.dc_kv_append.argtypes = [pc, pb, pr, vp]
+    L.dc_attention_paged_workspace.restype = i32
+    L.dc_attention_paged_workspace.argtypes = [pc, pb, pa, pu64]
+    L.dc_attention_paged.restype = i32
+    L.dc_attention_paged.argtypes = [pc, pb, pa, vp, u64, vp]
     L.dc_device_copy.restype = i32
     L.dc_device_copy.argtypes = [vp, vp, u64, vp]
     return L
@@ -399,6 +475,23 @@ def quantize_vector(x: np.ndarray) -> Tuple[np.ndarray, float]:
     sc = np.empty(1, dtype=np.float32)
     _check(_L.dc_quantize_vector(_host(x), x.size, _host(xq), _host(sc)), "dc_quantize_vector")
     return xq, float(sc[0])
+
+
+def kv_append(cache: KVCache, batch: KVBatch, rows: KVRows, stream: int = 0) -> None:
+    """dc_kv_append: turns queries and keys by their positions and puts keys and values into the cache."""
+    _check(_L.dc_kv_append(cache, batch, rows, stream), "dc_kv_append")
+
+
+def attention_paged_workspace(cache: KVCache, batch: KVBatch, attention: Attention) -> int:
+    n = C.c_uint64(0)
+    _check(_L.dc_attention_paged_workspace(cache, batch, attention, C.byref(n)), "dc_attention_paged_workspace")
+    return int(n.value)
+
+
+def attention_paged(cache: KVCache, batch: KVBatch, attention: Attention, workspace_dev=None, workspace_bytes: int = 0,
+                    stream: int = 0) -> None:
+    """dc_attention_paged: attention of the batch's new tokens over the cache."""
+    _check(_L.dc_attention_paged(cache, batch, attention, _dev(workspace_dev), workspace_bytes, stream), "dc_attention_paged")
 
 
 def device_copy(src_dev, dst_dev, nbytes: int, stream: int = 0) -> None:
