@@ -11,19 +11,478 @@
 
 #include <math.h>
 
+#include <algorithm>
+
 using namespace dcpages;
 
 namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr int32_t kNoPosition = -0x40000000; // of a row that is not there: it sees nothing
+
+// One part of the keys that a launch works through, the common prefix or the sequences' own pages, cut into n_splits runs of
+// `chunk` tiles (the last one takes what is left).
+struct Part {
+    uint32_t blocks, n_splits, chunk, first_slot;
+};
 
 struct AttentionArgs {
     Batch batch;
     const void *k_pages, *v_pages, *q;
     void *out;
     float *lse;
+    float *partial;    // [row][head][slot][head_dim]: sums of weight times value of one split, relative to its maximum
+    f32x2 *partial_ml; // [row][head][slot]: that maximum (of scores in powers of two) and the sum of the weights
     uint64_t q_row, q_head, out_row, out_head;
-    uint32_t n_heads, n_kv_heads, group, window, sinks;
-    float scale;
+    uint32_t n_heads, n_kv_heads, group, window, sinks, max_new, n_slots;
+    float scale;       // not negative; with `negate` of queries that are taken with the other sign
+    bool negate, zero; // scale 0: queries are taken as zeros and scale is 1
+    Part prefix, own;
 };
+
+template <typename T> struct Mfma;
+template <> struct Mfma<__bf16> {
+    __device__ static __forceinline__ f32x4 m16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static constexpr uint32_t kExponent = 0x7F80u, kOne = 0x3F80u;
+};
+template <> struct Mfma<_Float16> {
+    __device__ static __forceinline__ f32x4 m16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static constexpr uint32_t kExponent = 0x7C00u, kOne = 0x3C00u;
+};
+
+// Maximum and sum over the lanes with the same number modulo 16 (32).
+__device__ __forceinline__ f32x2 swapped16(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f32x2{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ f32x2 swapped32(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f32x2{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ float max_over_32(float v)
+{
+    const f32x2 r = swapped32(v);
+    return fmaxf(r[0], r[1]);
+}
+__device__ __forceinline__ float max_over_16(float v)
+{
+    const f32x2 r = swapped16(v);
+    return max_over_32(fmaxf(r[0], r[1]));
+}
+__device__ __forceinline__ float sum_over_16(float v)
+{
+    f32x2 r = swapped16(v);
+    r = swapped32(r[0] + r[1]);
+    return r[0] + r[1];
+}
+
+// 2^x; 0 for -infinity.
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+
+// Of a block of 4 rows of 16 values of 16 bits that the 16 lanes name (a quarter of a row each), lane i gets column i.
+__device__ __forceinline__ u32x2 lds_column4(uint32_t addr)
+{
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)addr));
+}
+
+// The tokens of a part that a row at position p sees; positions count from the part's first token.
+struct Seen {
+    int32_t low, high, sinks;
+    Seen() = default;
+    __device__ __forceinline__ Seen(int32_t p, int32_t there, uint32_t window, int64_t sinks_left)
+    {
+        high = max(0, min(there, p + 1));
+        low = window ? (int32_t)min((int64_t)high, max((int64_t)p - (int64_t)window + 1, (int64_t)0)) : 0;
+        sinks = (int32_t)min((int64_t)high, max(sinks_left, (int64_t)0));
+    }
+    __device__ __forceinline__ bool token(int32_t j) const { return (j < high) & ((j >= low) | (j < sinks)); }
+};
+
+// The keys of one part that the rows of a workgroup see, as tiles of TILE tokens: the tiles with sinks, then those from the window's
+// beginning on.  Positions here count from the part's first token.
+template <int TILE> struct Tiles {
+    int32_t low, high, sinks;   // tokens [0, sinks) and [low, high) are seen by some row
+    int32_t low_tile, sink_tiles, count;
+    // p_min, p_max: smallest and largest position of the rows, counted from the part's first token
+    __device__ __forceinline__ Tiles(int32_t p_min, int32_t p_max, int32_t there, uint32_t window, int64_t sinks_left)
+    {
+        high = max(0, min(there, p_max + 1));
+        const int64_t l = window ? (int64_t)p_min - (int64_t)window + 1 : 0;
+        low = (int32_t)min((int64_t)high, max(l, (int64_t)0));
+        sinks = (int32_t)min((int64_t)high, max(sinks_left, (int64_t)0));
+        low_tile = low / TILE;
+        sink_tiles = (sinks + TILE - 1) / TILE;
+        if (low_tile <= sink_tiles) low_tile = 0, sink_tiles = 0;
+        count = sink_tiles + max(0, (high + TILE - 1) / TILE - low_tile);
+    }
+    __device__ __forceinline__ int32_t first_token(int32_t tile) const { return (tile < sink_tiles ? tile : low_tile + tile - sink_tiles) * TILE; }
+};
+
+// Results of a row and head, or what the joining kernel makes them of: v holds four sums of weight times value.
+template <typename T, int D> __device__ __forceinline__ void store_result(const AttentionArgs &a, uint32_t row, uint32_t head, uint32_t slot,
+                                                                          uint32_t at, f32x4 v, float m, float l)
+{
+    if (a.n_slots == 1) {
+        typedef T T4 __attribute__((ext_vector_type(4)));
+        const float r = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+        *reinterpret_cast<T4 *>(static_cast<T *>(a.out) + row * a.out_row + head * a.out_head + at) =
+            __builtin_convertvector(l == 0.0f ? f32x4{} : v * r, T4);
+        if (a.lse && at == 0) a.lse[(uint64_t)row * a.n_heads + head] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    } else {
+        const uint64_t i = ((uint64_t)row * a.n_heads + head) * a.n_slots + slot;
+        *reinterpret_cast<f32x4 *>(a.partial + i * D + at) = v;
+        if (at == 0) a.partial_ml[i] = f32x2{m, l};
+    }
+}
+
+// ---- few rows -------------------------------------------------------------------------------------------------------------
+//
+// At most 16 RT rows (new tokens times the query heads that share a key/value head) read the keys: memory bounds this kernel.  A
+// wavefront takes tiles of 32 tokens.  Scores come as a matrix [token][row] = K Q^T from 16x16x32 products, whose first operand is
+// K as it lies in memory: a lane holds 8 neighbouring values of a token.  In the result a lane holds 4 tokens of one row in each
+// half of the tile, which is already the second operand of [head_dim][row] = V^T P^T if the product's 32 tokens are numbered that way; the
+// first operand, 8 tokens of one value, comes out of the LDS through the transposing read.  So maxima, sums and the scaling of
+// what has been added up stay inside a lane but for two exchanges a tile.  K goes from memory into registers, V through
+// registers into the wavefront's own part of the LDS: no barrier in the loop.  The next tile's loads are under way during the rest of the tile's work.
+template <typename T, int D, int RT> __global__ __launch_bounds__(256) void dc_attention_few_kernel(AttentionArgs a)
+{
+    typedef typename Vec8<T>::type TV;
+    constexpr int kTile = 32, KS = D / 32, DT = D / 16;
+    constexpr int kRowBytes = 2 * D, kChunks = D / 8, kRowsALoad = 64 / kChunks, kLoads = kTile / kRowsALoad;
+    constexpr int kPadded = D + 4;
+    constexpr int kLdsV = 4 * kTile * kRowBytes, kLdsO = 4 * 16 * kPadded * 4;
+    __shared__ __align__(16) uint8_t lds[kLdsV > kLdsO ? kLdsV : kLdsO];
+    __shared__ float lds_m[4][16 * RT], lds_l[4][16 * RT];
+    __shared__ int32_t lds_p[16 * RT];
+
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15u, g = lane >> 4;
+    const bool common = blockIdx.x < a.prefix.blocks;
+    const Part part = common ? a.prefix : a.own;
+    uint32_t item = common ? blockIdx.x : blockIdx.x - a.prefix.blocks;
+    const uint32_t kv = item % a.n_kv_heads;
+    item /= a.n_kv_heads;
+    const uint32_t seq = common ? 0 : item % a.batch.n_seqs, split = common ? item : item / a.batch.n_seqs;
+
+    // rows of this workgroup: row_first + i / group of head kv * group + i % group for i < n
+    uint32_t row_first = 0, n;
+    int32_t p_first = 0, there, base = 0, p_min, p_max;
+    if (common) {
+        n = a.batch.n_rows * a.group;
+        there = (int32_t)a.batch.prefix_len;
+        // positions of the rows, sequence by sequence
+        if (threadIdx.x < 16 * RT) lds_p[threadIdx.x] = kNoPosition;
+        __syncthreads();
+        for (uint32_t b = threadIdx.x; b < a.batch.n_seqs; b += 256) {
+            const uint32_t first = a.batch.first_row(b), end = a.batch.rows_end(b);
+            for (uint32_t r = first; r < end; r++) lds_p[r] = a.batch.length(b) - (int32_t)(end - r);
+        }
+        __syncthreads();
+        p_min = 0x7FFFFFFF, p_max = kNoPosition;
+        for (uint32_t r = 0; r < a.batch.n_rows; r++) {
+            const int32_t p = lds_p[r];
+            if (p != kNoPosition) p_min = min(p_min, p), p_max = max(p_max, p);
+        }
+        p_min = min(p_min, p_max);
+    } else {
+        row_first = a.batch.first_row(seq);
+        const uint32_t end = a.batch.rows_end(seq);
+        if (end <= row_first) return;
+        const uint32_t rows = min(end - row_first, a.max_new);
+        n = rows * a.group;
+        base = (int32_t)a.batch.prefix_len;
+        const int32_t len = a.batch.length(seq);
+        there = min(max(len - base, 0), (int32_t)(a.batch.pages_stride << a.batch.page_shift));
+        p_first = len - (int32_t)(end - row_first);
+        p_min = p_first - base, p_max = p_first + (int32_t)rows - 1 - base;
+    }
+    const Tiles<kTile> tiles(p_min, p_max, there, a.window, (int64_t)a.sinks - base);
+    const int32_t t_begin = (int32_t)min((uint64_t)split * part.chunk, (uint64_t)tiles.count);
+    const int32_t t_end = split + 1 == part.n_splits ? tiles.count : (int32_t)min((uint64_t)t_begin + part.chunk, (uint64_t)tiles.count);
+    const int32_t *table = common ? a.batch.prefix_pages : a.batch.pages + (uint64_t)seq * a.batch.pages_stride;
+
+    // queries, and what the lane's rows see
+    TV q[RT][KS];
+    Seen seen[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) {
+        const uint32_t r = rt * 16 + c;
+        const bool is = r < n;
+        const uint32_t i = r / a.group, head = kv * a.group + r % a.group;
+        seen[rt] = Seen(!is ? kNoPosition : common ? lds_p[i] : p_first + (int32_t)i - base, there, a.window, (int64_t)a.sinks - base);
+        const T *src = static_cast<const T *>(a.q) + (uint64_t)(row_first + i) * a.q_row + head * a.q_head + 8 * g;
+#pragma unroll
+        for (int s = 0; s < KS; s++) {
+            u32x4 x = {};
+            if (is && !a.zero) x = *reinterpret_cast<const u32x4 *>(src + 32 * s);
+            if (a.negate) x ^= 0x80008000u;
+            q[rt][s] = __builtin_bit_cast(TV, x);
+        }
+    }
+
+    f32x4 o[RT][DT];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) {
+        m[rt] = -INFINITY, l[rt] = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++) o[rt][dt] = f32x4{};
+    }
+
+    const uint64_t page_stride = (uint64_t)a.n_kv_heads << a.batch.page_shift;
+    const uint64_t head_at = (uint64_t)kv << a.batch.page_shift;
+    const uint32_t place_mask = (1u << a.batch.page_shift) - 1u;
+    // page of each half of a tile, -1 where there is none
+    auto pages_of = [&](int32_t tile, int32_t (&page)[2]) {
+        const int32_t j = tiles.first_token(tile);
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const int32_t jj = j + 16 * h;
+            int32_t e = -1;
+            if (jj < tiles.high) e = table[(uint32_t)jj >> a.batch.page_shift];
+            page[h] = __builtin_amdgcn_readfirstlane((uint32_t)e < a.batch.n_pages ? e : -1);
+        }
+    };
+    // first value of a half's tokens; where there is no page, of page 0, whose tokens are then taken for hidden
+    auto half_at = [&](int32_t j, int32_t page) {
+        return (page_stride * (uint32_t)max(page, 0) + head_at + ((uint32_t)j & place_mask)) * D;
+    };
+    TV k[2][KS];
+    u32x4 v[kLoads];
+    auto load_k = [&](int32_t j, const int32_t (&page)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const T *src = static_cast<const T *>(a.k_pages) + half_at(j + 16 * h, page[h]) + c * D + 8 * g;
+#pragma unroll
+            for (int s = 0; s < KS; s++) k[h][s] = *reinterpret_cast<const TV *>(src + 32 * s);
+        }
+    };
+    auto load_v = [&](int32_t j, const int32_t (&page)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const T *src = static_cast<const T *>(a.v_pages) + half_at(j + 16 * h, page[h]) + lane * 8;
+#pragma unroll
+            for (int i = 0; i < kLoads / 2; i++) v[h * (kLoads / 2) + i] = *reinterpret_cast<const u32x4 *>(src + i * 512);
+        }
+    };
+    // Rows of V lie in the LDS with their 16-byte chunks exchanged so that 8 rows' pairs of chunks are on different banks.
+    auto swizzle = [](uint32_t row) { return D == 64 ? ((row >> 1) & 3u) << 1 : (row & 7u) << 1; };
+    const uint32_t my_lds = dcdev::lds_address(lds) + wave * (kTile * kRowBytes);
+
+    int32_t page[2], next_page[2];
+    int32_t t = t_begin + (int32_t)wave;
+    if (t < t_end) {
+        pages_of(t, page);
+        const int32_t j = tiles.first_token(t);
+        load_k(j, page);
+        load_v(j, page);
+        pages_of(min(t + 4, t_end - 1), next_page);
+    }
+    for (; t < t_end; t += 4) {
+        const int32_t j = tiles.first_token(t);
+        const bool more = t + 4 < t_end;
+        const int32_t next_j = tiles.first_token(min(t + 4, t_end - 1));
+
+        f32x4 s[RT][2];
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int rt = 0; rt < RT; rt++) {
+                s[rt][h] = f32x4{};
+#pragma unroll
+                for (int i = 0; i < KS; i++) s[rt][h] = Mfma<T>::m16(k[h][i], q[rt][i], s[rt][h]);
+            }
+        if (more) load_k(next_j, next_page);
+
+        // tokens that not all rows see; those that none sees lie in the LDS as zeros
+        const bool edge = page[0] < 0 || page[1] < 0 || j + kTile > p_min + 1 || j + kTile > tiles.high || (j < tiles.low && j + kTile > tiles.sinks) ||
+                          (a.window && j + kTile > tiles.sinks && (int64_t)j <= (int64_t)p_max - a.window);
+        if (edge) {
+#pragma unroll
+            for (int i = 0; i < kLoads; i++) {
+                const int32_t jj = j + i * kRowsALoad + (int32_t)(lane / kChunks);
+                const bool some = (page[i >= kLoads / 2] >= 0) & (jj < tiles.high) & ((jj >= tiles.low) | (jj < tiles.sinks));
+                v[i] = some ? v[i] : u32x4{};
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const uint32_t row = i * kRowsALoad + lane / kChunks, chunk = lane % kChunks;
+            *(lds_u32x4 *)(uintptr_t)(my_lds + row * kRowBytes + ((chunk ^ swizzle(row)) << 4)) = v[i];
+        }
+        if (more) load_v(next_j, next_page);
+
+        TV w[RT];
+        TV is_seen[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; rt++) {
+            uint32_t hidden = 0;
+            if (edge) {
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const bool sees = seen[rt].token(j + 16 * h + 4 * (int32_t)g + i) & (page[h] >= 0);
+                        s[rt][h][i] = sees ? s[rt][h][i] : -INFINITY;
+                        hidden |= sees ? 0u : 1u << (4 * h + i);
+                    }
+            }
+            float top = fmaxf(fmaxf(fmaxf(s[rt][0][0], s[rt][0][1]), fmaxf(s[rt][0][2], s[rt][0][3])),
+                              fmaxf(fmaxf(s[rt][1][0], s[rt][1][1]), fmaxf(s[rt][1][2], s[rt][1][3])));
+            top = fmaxf(m[rt], max_over_16(top));
+            const float ref = top == -INFINITY ? 0.0f : top * a.scale;
+            const float fade = exp2_of(m[rt] * a.scale - ref);
+            m[rt] = top;
+            typedef float f32x8 __attribute__((ext_vector_type(8)));
+            f32x8 e;
+#pragma unroll
+            for (int i = 0; i < 8; i++) e[i] = exp2_of(__builtin_fmaf(s[rt][i / 4][i % 4], a.scale, -ref));
+            l[rt] = l[rt] * fade + (((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
+            w[rt] = __builtin_convertvector(e, TV);
+#pragma unroll
+            for (int dt = 0; dt < DT; dt++) o[rt][dt] *= fade;
+            u32x4 ones;
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                ones[i] = (hidden >> (2 * i) & 1u ? 0u : Mfma<T>::kOne) | (hidden >> (2 * i + 1) & 1u ? 0u : Mfma<T>::kOne << 16);
+            is_seen[rt] = __builtin_bit_cast(TV, ones);
+        }
+        __builtin_amdgcn_wave_barrier();
+        const uint32_t i4 = c >> 2, half8 = (c & 1u) << 3;
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++) {
+            const uint32_t row = 4 * g + i4, chunk = 2 * dt + ((c & 3u) >> 1);
+            const uint32_t at = my_lds + row * kRowBytes + ((chunk ^ swizzle(row)) << 4) + half8;
+            const u32x2 lo = lds_column4(at), hi = lds_column4(at + 16 * kRowBytes);
+            u32x4 x = {lo[0], lo[1], hi[0], hi[1]};
+            if (edge && p_min != p_max) {
+                // A value that is no number must reach only the rows that see its token, and a weight of 0 does not keep it from the
+                // others.  It is taken as 0 here, and added to the rows that see it: how many tokens they are says a product of ones.
+                u32x4 up, down;
+                bool any = false;
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    up[i] = down[i] = 0;
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        const uint32_t y = x[i] >> (16 * h) & 0xFFFFu;
+                        if ((y & Mfma<T>::kExponent) == Mfma<T>::kExponent) {
+                            const bool nan = (y & 0x7FFFu) != Mfma<T>::kExponent;
+                            if (nan || !(y & 0x8000u)) up[i] |= Mfma<T>::kOne << (16 * h);
+                            if (nan || (y & 0x8000u)) down[i] |= Mfma<T>::kOne << (16 * h);
+                            x[i] &= ~(0xFFFFu << (16 * h));
+                            any = true;
+                        }
+                    }
+                }
+                if (__any(any)) {
+#pragma unroll
+                    for (int rt = 0; rt < RT; rt++) {
+                        const f32x4 ups = Mfma<T>::m16(__builtin_bit_cast(TV, up), is_seen[rt], f32x4{});
+                        const f32x4 downs = Mfma<T>::m16(__builtin_bit_cast(TV, down), is_seen[rt], f32x4{});
+#pragma unroll
+                        for (int i = 0; i < 4; i++) {
+                            if (ups[i] > 0.0f) o[rt][dt][i] += INFINITY;
+                            if (downs[i] > 0.0f) o[rt][dt][i] -= INFINITY;
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int rt = 0; rt < RT; rt++) o[rt][dt] = Mfma<T>::m16(__builtin_bit_cast(TV, x), w[rt], o[rt][dt]);
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int h = 0; h < 2; h++) page[h] = next_page[h];
+        if (more) pages_of(min(t + 8, t_end - 1), next_page);
+    }
+
+    // the wavefronts' sums, brought to one maximum and added up in their order
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) {
+        l[rt] = sum_over_16(l[rt]);
+        m[rt] *= a.scale;
+        if (l[rt] != l[rt] && m[rt] == -INFINITY) m[rt] = 0.0f; // saw scores, none of them a number
+        if (g == 0) lds_m[wave][rt * 16 + c] = m[rt], lds_l[wave][rt * 16 + c] = l[rt];
+    }
+    __syncthreads();
+    float *sums = reinterpret_cast<float *>(lds);
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) {
+        const uint32_t r = rt * 16 + c;
+        const float top = fmaxf(fmaxf(lds_m[0][r], lds_m[1][r]), fmaxf(lds_m[2][r], lds_m[3][r]));
+        const float f = m[rt] == -INFINITY ? 0.0f : exp2_of(m[rt] - top);
+        if (rt) __syncthreads();
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++)
+            *reinterpret_cast<f32x4 *>(&sums[(wave * 16 + c) * kPadded + 16 * dt + 4 * g]) = m[rt] == -INFINITY ? f32x4{} : o[rt][dt] * f;
+        __syncthreads();
+        constexpr uint32_t kQuads = D / 4;
+        for (uint32_t i = threadIdx.x; i < 16 * kQuads; i += 256) {
+            const uint32_t col = i / kQuads, at = i % kQuads * 4, rr = rt * 16 + col;
+            if (rr >= n) continue;
+            const float big = fmaxf(fmaxf(lds_m[0][rr], lds_m[1][rr]), fmaxf(lds_m[2][rr], lds_m[3][rr]));
+            f32x4 sum = {};
+            float total = 0.0f;
+#pragma unroll
+            for (int w4 = 0; w4 < 4; w4++) {
+                sum += *reinterpret_cast<const f32x4 *>(&sums[(w4 * 16 + col) * kPadded + at]);
+                if (lds_m[w4][rr] != -INFINITY) total += lds_l[w4][rr] * exp2_of(lds_m[w4][rr] - big);
+            }
+            store_result<T, D>(a, row_first + rr / a.group, kv * a.group + rr % a.group, part.first_slot + split, at, sum, big, total);
+        }
+    }
+}
+
+// Joins the splits of a row and head: each has its sums relative to a maximum of its own.
+template <typename T, int D> __global__ __launch_bounds__(256) void dc_attention_join_kernel(AttentionArgs a)
+{
+    constexpr uint32_t kQuads = D / 4, kSets = 256 / kQuads;
+    __shared__ f32x4 lds_sum[kSets][kQuads];
+    const uint32_t row = blockIdx.x, head = blockIdx.y, at = threadIdx.x % kQuads, set = threadIdx.x / kQuads;
+    const uint32_t seq = a.batch.sequence_of(row);
+    if (seq >= a.batch.n_seqs || row - a.batch.first_row(seq) >= a.max_new) return;
+    const uint64_t first = ((uint64_t)row * a.n_heads + head) * a.n_slots;
+    float top = -INFINITY, total = 0.0f;
+    for (uint32_t i = 0; i < a.n_slots; i += 64) {
+        const uint32_t slot = i + (threadIdx.x & 63u);
+        f32x2 ml = {-INFINITY, 0.0f};
+        if (slot < a.n_slots) ml = a.partial_ml[first + slot];
+        float t = max_over_16(ml[0]);
+#pragma unroll
+        for (int k = 1; k < 16; k <<= 1) t = fmaxf(t, __shfl_xor(t, k));
+        t = fmaxf(t, top);
+        float w = ml[0] == -INFINITY ? 0.0f : ml[1] * exp2_of(ml[0] - t);
+        w = sum_over_16(w);
+#pragma unroll
+        for (int k = 1; k < 16; k <<= 1) w += __shfl_xor(w, k);
+        total = (top == -INFINITY ? 0.0f : total * exp2_of(top - t)) + w;
+        top = t;
+    }
+    f32x4 sum = {};
+    for (uint32_t slot = set; slot < a.n_slots; slot += kSets) {
+        const float m = a.partial_ml[first + slot][0];
+        if (m != -INFINITY) sum += *reinterpret_cast<const f32x4 *>(a.partial + (first + slot) * D + 4 * at) * exp2_of(m - top);
+    }
+    lds_sum[set][at] = sum;
+    __syncthreads();
+    if (set) return;
+#pragma unroll
+    for (uint32_t i = 1; i < kSets; i++) sum += lds_sum[i][at];
+    AttentionArgs whole = a;
+    whole.n_slots = 1;
+    store_result<T, D>(whole, row, head, 0, 4 * at, sum, top, total);
+}
 
 __device__ __forceinline__ float sum_of_lanes(float v)
 {
@@ -44,7 +503,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void dc_attention
     const uint32_t kv = head / a.group;
     float qf[E], o[E], m = -INFINITY, l = 0.0f;
 #pragma unroll
-    for (int i = 0; i < E; i++) qf[i] = (float)q[i] * a.scale, o[i] = 0.0f;
+    for (int i = 0; i < E; i++) qf[i] = a.zero ? 0.0f : (float)q[i] * (a.negate ? -a.scale : a.scale) * kLn2, o[i] = 0.0f;
     for (int32_t j = wave; j <= last; j += 4) {
         if (a.window && (int64_t)j <= (int64_t)p - a.window && (uint32_t)j >= a.sinks) continue;
         const int32_t page = a.batch.page_of(seq, j);
@@ -91,12 +550,59 @@ bool attention_ok(const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_a
            strides_apart(t->out_row_stride, t->out_head_stride, batch->n_rows, t->n_heads, cache->head_dim);
 }
 
+template <typename T, int D> void launch_few(const AttentionArgs &a, uint32_t rows, hipStream_t stream)
+{
+    const dim3 grid(a.prefix.blocks + a.own.blocks);
+    if (rows <= 16) hipLaunchKernelGGL((dc_attention_few_kernel<T, D, 1>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((dc_attention_few_kernel<T, D, 2>), grid, dim3(256), 0, stream, a);
+    if (a.n_slots > 1)
+        hipLaunchKernelGGL((dc_attention_join_kernel<T, D>), dim3(a.batch.n_rows, a.n_heads), dim3(256), 0, stream, a);
+}
+
 template <typename T> void launch(const AttentionArgs &a, uint32_t head_dim, hipStream_t stream)
 {
     const dim3 grid(a.batch.n_rows, a.n_heads);
+    if (a.own.blocks) {
+        const uint32_t rows = a.group * (a.prefix.blocks ? std::max(a.max_new, a.batch.n_rows) : a.max_new);
+        if (head_dim == 64) launch_few<T, 64>(a, rows, stream);
+        else if (head_dim == 128) launch_few<T, 128>(a, rows, stream);
+        else launch_few<T, 256>(a, rows, stream);
+        return;
+    }
     if (head_dim == 64) hipLaunchKernelGGL((dc_attention_rows_kernel<T, 64>), grid, dim3(256), 0, stream, a);
     else if (head_dim == 128) hipLaunchKernelGGL((dc_attention_rows_kernel<T, 128>), grid, dim3(256), 0, stream, a);
     else hipLaunchKernelGGL((dc_attention_rows_kernel<T, 256>), grid, dim3(256), 0, stream, a);
+}
+
+// How a call's keys are cut: fills prefix, own and n_slots, and gives the bytes of workspace.  False for a batch that is too large.
+bool plan(AttentionArgs &a, const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_attention *t, uint64_t *workspace_bytes)
+{
+    *workspace_bytes = 0;
+    const uint32_t group = t->n_heads / cache->n_kv_heads;
+    constexpr uint64_t kTile = 32, kBlocks = 1024, kLeast = 4, kMost = 128;
+    auto cut = [&](uint64_t items, uint64_t tokens, uint32_t first_slot) {
+        const uint64_t n_tiles = (tokens + kTile - 1) / kTile;
+        uint64_t n = std::min((kBlocks + items - 1) / items, (n_tiles + kLeast - 1) / kLeast);
+        n = std::max<uint64_t>(1, std::min(n, kMost));
+        const uint64_t chunk = std::max<uint64_t>(1, (n_tiles + n - 1) / n);
+        n = std::max<uint64_t>(1, (n_tiles + chunk - 1) / chunk);
+        return Part{(uint32_t)(items * n), (uint32_t)n, (uint32_t)chunk, first_slot};
+    };
+    const uint64_t rows = (uint64_t)group * (batch->prefix_len ? std::max(batch->max_new, batch->n_rows) : batch->max_new);
+    a.n_slots = 1;
+    if (rows > (cache->head_dim == 256 ? 16 : 32)) return true;
+    uint64_t own = batch->max_len > batch->prefix_len ? batch->max_len - batch->prefix_len : 1;
+    uint64_t common = batch->prefix_len;
+    if (t->window) {
+        const uint64_t seen = (uint64_t)t->window + batch->max_new + t->sinks + 2 * kTile;
+        own = std::min(own, seen), common = std::min(common, seen);
+    }
+    if (common) a.prefix = cut(cache->n_kv_heads, common, 0);
+    a.own = cut((uint64_t)batch->n_seqs * cache->n_kv_heads, own, a.prefix.n_splits);
+    a.n_slots = a.prefix.n_splits + a.own.n_splits;
+    if ((uint64_t)batch->n_seqs * cache->n_kv_heads * a.own.n_splits + a.prefix.blocks >= 1u << 24) return false;
+    if (a.n_slots > 1) *workspace_bytes = (uint64_t)batch->n_rows * t->n_heads * a.n_slots * (cache->head_dim + 2) * sizeof(float);
+    return true;
 }
 
 } // namespace
@@ -105,8 +611,8 @@ extern "C" int dc_attention_paged_workspace(const dc_kv_cache *cache, const dc_k
                                             uint64_t *workspace_bytes)
 {
     if (!workspace_bytes || !attention_ok(cache, batch, attention)) return DC_E_ARG;
-    *workspace_bytes = 0;
-    return DC_OK;
+    AttentionArgs a = {};
+    return plan(a, cache, batch, attention, workspace_bytes) ? DC_OK : DC_E_ARG;
 }
 
 extern "C" int dc_attention_paged(const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_attention *attention,
@@ -119,7 +625,14 @@ extern "C" int dc_attention_paged(const dc_kv_cache *cache, const dc_kv_batch *b
     a.q_row = attention->q_row_stride, a.q_head = attention->q_head_stride;
     a.out_row = attention->out_row_stride, a.out_head = attention->out_head_stride;
     a.n_heads = attention->n_heads, a.n_kv_heads = cache->n_kv_heads, a.group = a.n_heads / a.n_kv_heads;
-    a.window = attention->window, a.sinks = attention->sinks, a.scale = attention->scale;
+    a.window = attention->window, a.sinks = attention->sinks, a.max_new = batch->max_new;
+    a.negate = attention->scale < 0.0f, a.zero = attention->scale == 0.0f;
+    a.scale = a.zero ? 1.0f : fabsf(attention->scale) * kLog2e;
+    uint64_t needed = 0;
+    if (!plan(a, cache, batch, attention, &needed) || (needed && !workspace_dev)) return DC_E_ARG;
+    if (workspace_bytes < needed) return DC_E_CAP;
+    a.partial = static_cast<float *>(workspace_dev);
+    a.partial_ml = reinterpret_cast<f32x2 *>(a.partial + (uint64_t)batch->n_rows * a.n_heads * a.n_slots * cache->head_dim);
     if (cache->type == DC_TYPE_BF16) launch<__bf16>(a, cache->head_dim, static_cast<hipStream_t>(hip_stream));
     else launch<_Float16>(a, cache->head_dim, static_cast<hipStream_t>(hip_stream));
     return dc_launch_status();

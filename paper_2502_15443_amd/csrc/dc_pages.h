@@ -71,7 +71,7 @@ inline bool cache_ok(const dc_kv_cache *c)
 
 inline bool batch_ok(const dc_kv_cache *c, const dc_kv_batch *b)
 {
-    if (!b || b->n_seqs < 1 || b->n_seqs > 65535 || b->n_rows < 1 || b->n_rows > 0x7FFFFFFFu || b->max_new < 1 ||
+    if (!b || b->n_seqs < 1 || b->n_seqs > 65535 || b->n_rows < 1 || b->n_rows >= 1u << 24 || b->max_new < 1 ||
         b->max_new > b->n_rows || b->max_len < 1 || b->pages_stride < 1 || !b->len_dev || !b->pages_dev)
         return false;
     if (!b->row_start_dev && (b->n_rows != b->n_seqs || b->max_new != 1)) return false;
