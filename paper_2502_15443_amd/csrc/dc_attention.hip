@@ -3,9 +3,6 @@
 //
 // For a row with query q: s_j = scale (q . k_j), out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m) with the running maximum m: one
 // pass over the keys and values, in which a larger maximum scales what has been added up so far.
-//
-// A workgroup owns one row of one query head; its four wavefronts take every fourth key.  A lane holds head_dim / 64 values of the
-// query, the key and the result.
 #include "dc_device.h"
 #include "dc_pages.h"
 
@@ -18,6 +15,8 @@ using namespace dcpages;
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -48,10 +47,12 @@ struct AttentionArgs {
 template <typename T> struct Mfma;
 template <> struct Mfma<__bf16> {
     __device__ static __forceinline__ f32x4 m16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    __device__ static __forceinline__ f32x16 m32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     static constexpr uint32_t kExponent = 0x7F80u, kOne = 0x3F80u;
 };
 template <> struct Mfma<_Float16> {
     __device__ static __forceinline__ f32x4 m16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    __device__ static __forceinline__ f32x16 m32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
     static constexpr uint32_t kExponent = 0x7C00u, kOne = 0x3C00u;
 };
 
@@ -94,6 +95,35 @@ typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 __device__ __forceinline__ u32x2 lds_column4(uint32_t addr)
 {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)addr));
+}
+
+// Eight values of V of which some are no numbers: those become 0, and up and down have ones where +infinity and -infinity (both: NaN) were.
+template <typename T> struct Split {
+    u32x4 finite, up, down;
+    __device__ __forceinline__ explicit Split(const u32x4 &x)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            uint32_t f = 0, u = 0, d = 0;
+#pragma unroll
+            for (int h = 0; h < 32; h += 16) {
+                const uint32_t y = x[i] >> h & 0xFFFFu;
+                const bool odd = (y & Mfma<T>::kExponent) == Mfma<T>::kExponent, nan = odd & ((y & 0x7FFFu) != Mfma<T>::kExponent);
+                const bool minus = (y & 0x8000u) != 0;
+                f |= odd ? 0u : y << h;
+                u |= (odd & (nan | !minus)) ? Mfma<T>::kOne << h : 0u;
+                d |= (odd & (nan | minus)) ? Mfma<T>::kOne << h : 0u;
+            }
+            finite[i] = f, up[i] = u, down[i] = d;
+        }
+    }
+};
+// What is left of a maximum over 16-bit values without their signs says whether one of them was no number.
+__device__ __forceinline__ u16x2 largest(u16x2 m, const u32x4 &x)
+{
+#pragma unroll
+    for (int i = 0; i < 4; i++) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, x[i] & 0x7FFF7FFFu));
+    return m;
 }
 
 // The tokens of a part that a row at position p sees; positions count from the part's first token.
@@ -315,6 +345,13 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256) void dc_a
                 v[i] = some ? v[i] : u32x4{};
             }
         }
+        bool odd = false; // a value that is no number, which some rows see and others do not
+        if (edge && p_min != p_max) {
+            u16x2 most = {};
+#pragma unroll
+            for (int i = 0; i < kLoads; i++) most = largest(most, v[i]);
+            odd = __any((most[0] >= Mfma<T>::kExponent) | (most[1] >= Mfma<T>::kExponent));
+        }
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
             const uint32_t row = i * kRowsALoad + lane / kChunks, chunk = lane % kChunks;
@@ -365,37 +402,17 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256) void dc_a
             const uint32_t at = my_lds + row * kRowBytes + ((chunk ^ swizzle(row)) << 4) + half8;
             const u32x2 lo = lds_column4(at), hi = lds_column4(at + 16 * kRowBytes);
             u32x4 x = {lo[0], lo[1], hi[0], hi[1]};
-            if (edge && p_min != p_max) {
+            if (odd) {
                 // A value that is no number must reach only the rows that see its token, and a weight of 0 does not keep it from the
                 // others.  It is taken as 0 here, and added to the rows that see it: how many tokens they are says a product of ones.
-                u32x4 up, down;
-                bool any = false;
+                const Split<T> y(x);
+                x = y.finite;
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    up[i] = down[i] = 0;
+                for (int rt = 0; rt < RT; rt++) {
+                    const f32x4 ups = Mfma<T>::m16(__builtin_bit_cast(TV, y.up), is_seen[rt], f32x4{});
+                    const f32x4 downs = Mfma<T>::m16(__builtin_bit_cast(TV, y.down), is_seen[rt], f32x4{});
 #pragma unroll
-                    for (int h = 0; h < 2; h++) {
-                        const uint32_t y = x[i] >> (16 * h) & 0xFFFFu;
-                        if ((y & Mfma<T>::kExponent) == Mfma<T>::kExponent) {
-                            const bool nan = (y & 0x7FFFu) != Mfma<T>::kExponent;
-                            if (nan || !(y & 0x8000u)) up[i] |= Mfma<T>::kOne << (16 * h);
-                            if (nan || (y & 0x8000u)) down[i] |= Mfma<T>::kOne << (16 * h);
-                            x[i] &= ~(0xFFFFu << (16 * h));
-                            any = true;
-                        }
-                    }
-                }
-                if (__any(any)) {
-#pragma unroll
-                    for (int rt = 0; rt < RT; rt++) {
-                        const f32x4 ups = Mfma<T>::m16(__builtin_bit_cast(TV, up), is_seen[rt], f32x4{});
-                        const f32x4 downs = Mfma<T>::m16(__builtin_bit_cast(TV, down), is_seen[rt], f32x4{});
-#pragma unroll
-                        for (int i = 0; i < 4; i++) {
-                            if (ups[i] > 0.0f) o[rt][dt][i] += INFINITY;
-                            if (downs[i] > 0.0f) o[rt][dt][i] -= INFINITY;
-                        }
-                    }
+                    for (int i = 0; i < 4; i++) o[rt][dt][i] += (ups[i] > 0.0f ? INFINITY : 0.0f) + (downs[i] > 0.0f ? -INFINITY : 0.0f);
                 }
             }
 #pragma unroll
@@ -444,6 +461,322 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256) void dc_a
     }
 }
 
+// ---- many rows ------------------------------------------------------------------------------------------------------------
+//
+// A workgroup owns 128 QT rows of one key/value head (prompts, or the rows of many sequences behind a common prefix): the matrix
+// units bound this kernel.  Keys and values go through the LDS in tiles that its four wavefronts share, double buffered with one barrier a
+// tile; a wavefront owns 32 QT rows.  The products are those of the kernel for few rows in the 32x32x16 shape: scores as [token][row]
+// = K Q^T, of which a lane holds 16 of 32 tokens of one row, results as [head_dim][row] = V^T P^T; maxima and sums stay in a lane but for one
+// exchange between the halves.
+template <typename T, int D, int QT> __global__ __launch_bounds__(256) void dc_attention_tile_kernel(AttentionArgs a)
+{
+    typedef typename Vec8<T>::type TV;
+    constexpr int kTile = D == 256 ? 32 : 64, KS = D / 16, DT = D / 32, HT = kTile / 32; // HT: 32-token products of a tile
+    constexpr uint32_t kRows = 128 * QT, kRowBytes = 2 * D, kChunks = D / 8, kRowsALoad = 64 / kChunks;
+    constexpr int kTokens = kTile / 4, kLoads = kTokens / (int)kRowsALoad; // tokens that a wavefront brings, in so many loads
+    constexpr uint32_t kBuffer = kTile * kRowBytes;
+    __shared__ __align__(16) uint8_t lds[4 * kBuffer]; // K, K, V, V
+    __shared__ int32_t lds_p[kRows];
+    __shared__ __align__(16) uint32_t lds_flags[2][4];
+
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31u, half = lane >> 5;
+    const bool common = blockIdx.x < a.prefix.blocks;
+    const Part part = common ? a.prefix : a.own;
+    uint32_t item = part.blocks - 1 - (common ? blockIdx.x : blockIdx.x - a.prefix.blocks); // the last rows, which see most, first
+    const uint32_t kv = a.n_kv_heads - 1 - item % a.n_kv_heads;
+    item /= a.n_kv_heads;
+    const uint32_t split = part.n_splits - 1 - item % part.n_splits;
+    uint32_t tile = item / part.n_splits;
+
+    // rows of this workgroup: i_first <= i < n of the sequence's (the batch's) rows, row_first + i / group of head kv * group + i % group
+    uint32_t row_first = 0, n, seq = 0;
+    int32_t there, base = 0;
+    if (common) {
+        n = a.batch.n_rows * a.group;
+        there = (int32_t)a.batch.prefix_len;
+    } else {
+        bool found = false;
+        n = 0;
+        if (a.batch.row_start) {
+            for (uint32_t b = 0; b < a.batch.n_seqs && !found; b += 64) {
+                const uint32_t s = b + lane;
+                uint32_t tiles = 0;
+                if (s < a.batch.n_seqs) {
+                    const uint32_t first = a.batch.first_row(s), end = a.batch.rows_end(s);
+                    tiles = end > first ? (min(end - first, a.max_new) * a.group + kRows - 1) / kRows : 0;
+                }
+                const uint32_t upto = dcdev::lanes_prefix_sum<false>(tiles);
+                const uint64_t beyond = __ballot(upto > tile);
+                if (beyond) {
+                    const uint32_t l = (uint32_t)__builtin_ctzll(beyond);
+                    seq = b + l;
+                    tile -= (uint32_t)__builtin_amdgcn_readlane((int)(upto - tiles), (int)l);
+                    found = true;
+                } else {
+                    tile -= (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+                }
+            }
+        } else {
+            const uint32_t tiles = (a.group + kRows - 1) / kRows;
+            seq = tile / tiles, tile %= tiles;
+            found = seq < a.batch.n_seqs;
+        }
+        if (!found) return;
+        seq = __builtin_amdgcn_readfirstlane(seq), tile = __builtin_amdgcn_readfirstlane(tile);
+        row_first = a.batch.first_row(seq);
+        n = min(a.batch.rows_end(seq) - row_first, a.max_new) * a.group;
+        base = (int32_t)a.batch.prefix_len;
+        there = min(max(a.batch.length(seq) - base, 0), (int32_t)(a.batch.pages_stride << a.batch.page_shift));
+    }
+    const uint32_t i_first = tile * kRows;
+    const int32_t *table = common ? a.batch.prefix_pages : a.batch.pages + (uint64_t)seq * a.batch.pages_stride;
+
+    // positions of the rows, counted from the part's first token
+    if (common) {
+        for (uint32_t i = threadIdx.x; i < kRows; i += 256) lds_p[i] = kNoPosition;
+        __syncthreads();
+        const uint32_t r_low = i_first / a.group, r_high = min((i_first + kRows - 1) / a.group + 1, a.batch.n_rows);
+        for (uint32_t b = threadIdx.x; b < a.batch.n_seqs; b += 256) {
+            const uint32_t first = a.batch.first_row(b), end = a.batch.rows_end(b);
+            const int32_t len = first < end ? a.batch.length(b) : 0;
+            for (uint32_t r = max(first, r_low); r < min(end, r_high); r++)
+                for (uint32_t i = max(r * a.group, i_first); i < min((r + 1) * a.group, i_first + kRows); i++) lds_p[i - i_first] = len - (int32_t)(end - r);
+        }
+    } else {
+        const int32_t p_first = a.batch.length(seq) - (int32_t)(a.batch.rows_end(seq) - row_first) - base;
+        for (uint32_t i = threadIdx.x; i < kRows; i += 256) lds_p[i] = i_first + i < n ? p_first + (int32_t)((i_first + i) / a.group) : kNoPosition;
+    }
+    __syncthreads();
+    auto smallest_largest = [&](uint32_t first, uint32_t count, int32_t &low, int32_t &high) {
+        low = 0x7FFFFFFF, high = kNoPosition;
+        for (uint32_t i = lane; i < count; i += 64) {
+            const int32_t p = lds_p[first + i];
+            if (p != kNoPosition) low = min(low, p), high = max(high, p);
+        }
+#pragma unroll
+        for (int i = 1; i < 64; i <<= 1) low = min(low, __shfl_xor(low, i)), high = max(high, __shfl_xor(high, i));
+        low = __builtin_amdgcn_readfirstlane(min(low, high)), high = __builtin_amdgcn_readfirstlane(high);
+    };
+    const int64_t sinks_left = (int64_t)a.sinks - base;
+    int32_t p_min, p_max;
+    smallest_largest(0, kRows, p_min, p_max);
+    const Tiles<kTile> tiles(p_min, p_max, there, a.window, sinks_left);
+    const int32_t t_begin = (int32_t)min((uint64_t)split * part.chunk, (uint64_t)tiles.count);
+    const int32_t t_end = split + 1 == part.n_splits ? tiles.count : (int32_t)min((uint64_t)t_begin + part.chunk, (uint64_t)tiles.count);
+    const int32_t all_see_high = Seen(p_min, there, a.window, sinks_left).high, all_see_low = Seen(p_max, there, a.window, sinks_left).low;
+    smallest_largest(wave * 32 * QT, 32 * QT, p_min, p_max);
+    const Seen first_sees(p_min, there, a.window, sinks_left), last_sees(p_max, there, a.window, sinks_left);
+
+    TV q[QT][KS];
+    Seen seen[QT];
+    f32x16 o[QT][DT];
+    float m[QT], ref[QT], l[QT];
+#pragma unroll
+    for (int rt = 0; rt < QT; rt++) {
+        const uint32_t at = wave * 32 * QT + 32 * rt + c, i = i_first + at;
+        const bool is = i < n;
+        const uint32_t head = kv * a.group + i % a.group;
+        seen[rt] = Seen(lds_p[at], there, a.window, sinks_left);
+        const T *src = static_cast<const T *>(a.q) + (uint64_t)(row_first + i / a.group) * a.q_row + head * a.q_head + 8 * half;
+#pragma unroll
+        for (int s = 0; s < KS; s++) {
+            u32x4 x = {};
+            if (is && !a.zero) x = *reinterpret_cast<const u32x4 *>(src + 16 * s);
+            if (a.negate) x ^= 0x80008000u;
+            q[rt][s] = __builtin_bit_cast(TV, x);
+        }
+        m[rt] = -INFINITY, ref[rt] = 0.0f, l[rt] = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++) o[rt][dt] = f32x16{};
+    }
+
+    const uint64_t page_stride = (uint64_t)a.n_kv_heads << a.batch.page_shift;
+    const uint64_t head_at = (uint64_t)kv << a.batch.page_shift;
+    const uint32_t place_mask = (1u << a.batch.page_shift) - 1u;
+    // the page of the tokens that this wavefront brings, -1 where there is none
+    auto page_of = [&](int32_t t) {
+        const int32_t j = tiles.first_token(t) + (int32_t)wave * kTokens;
+        int32_t e = -1;
+        if (j < tiles.high) e = table[(uint32_t)j >> a.batch.page_shift];
+        return (int32_t)__builtin_amdgcn_readfirstlane((uint32_t)e < a.batch.n_pages ? e : -1);
+    };
+    u32x4 k_new[kLoads], v_new[kLoads];
+    auto load = [&](int32_t t, int32_t page) {
+        const int32_t j = tiles.first_token(t) + (int32_t)wave * kTokens;
+        const uint64_t at = (page_stride * (uint32_t)max(page, 0) + head_at + ((uint32_t)j & place_mask)) * D + lane * 8;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) k_new[i] = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.k_pages) + at + i * 512);
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) v_new[i] = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.v_pages) + at + i * 512);
+    };
+    // The 16-byte chunks of a token lie exchanged in the LDS, so that 16 tokens' same chunks are on different banks, and the same four of 4 tokens'.
+    auto swizzle = [](uint32_t token) {
+        return D == 64 ? (token >> 1 & 1u) << 2 | (token >> 2 & 3u) : (token & 3u) << 2 | (token >> 2 & 3u);
+    };
+    const uint32_t lds_k = dcdev::lds_address(lds), lds_v = lds_k + 2 * kBuffer;
+    // flags of the tokens that a wavefront brought: 1 they are there, 2 a value of V that not all rows see is no number
+    auto put = [&](int32_t t, int32_t page, uint32_t buffer) {
+        const int32_t j = tiles.first_token(t) + (int32_t)wave * kTokens;
+        uint32_t flags = page >= 0 ? 1u : 0u;
+        if (page < 0 || j + kTokens > all_see_high || j < all_see_low) {
+            u16x2 most = {};
+#pragma unroll
+            for (int i = 0; i < kLoads; i++) {
+                const int32_t jj = j + i * (int32_t)kRowsALoad + (int32_t)(lane / kChunks);
+                const bool some = (page >= 0) & (jj < tiles.high) & ((jj >= tiles.low) | (jj < tiles.sinks));
+                v_new[i] = some ? v_new[i] : u32x4{};
+                most = largest(most, v_new[i]);
+            }
+            if (__any((most[0] >= Mfma<T>::kExponent) | (most[1] >= Mfma<T>::kExponent))) flags |= 2u;
+        }
+        if (lane == 0) lds_flags[buffer][wave] = flags;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const uint32_t token = wave * kTokens + i * kRowsALoad + lane / kChunks, chunk = lane % kChunks;
+            const uint32_t at = buffer * kBuffer + token * kRowBytes + ((chunk ^ swizzle(token)) << 4);
+            *(lds_u32x4 *)(uintptr_t)(lds_k + at) = k_new[i];
+            *(lds_u32x4 *)(uintptr_t)(lds_v + at) = v_new[i];
+        }
+    };
+
+    int32_t page = -1, next_page = -1;
+    if (t_begin < t_end) {
+        page = page_of(t_begin);
+        load(t_begin, page);
+        put(t_begin, page, 0);
+        next_page = page_of(min(t_begin + 1, t_end - 1));
+    }
+    __syncthreads();
+    for (int32_t t = t_begin; t < t_end; t++) {
+        const uint32_t buffer = (uint32_t)(t - t_begin) & 1u;
+        const int32_t j = tiles.first_token(t);
+        const bool more = t + 1 < t_end;
+        if (more) load(t + 1, next_page);
+        const int32_t page_after = page_of(min(t + 2, t_end - 1));
+
+        // a wavefront whose rows see nothing of the tile has nothing to do
+        if (j < last_sees.high && (j + kTile > first_sees.low || j < last_sees.sinks)) {
+            uint32_t there_bits = 0, odd_bits = 0;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint32_t f = __builtin_amdgcn_readfirstlane(lds_flags[buffer][i]);
+                there_bits |= (f & 1u) << i, odd_bits |= f & 2u;
+            }
+            const bool edge = there_bits != 15u || j + kTile > first_sees.high || (j < last_sees.low && j + kTile > first_sees.sinks);
+            const bool odd = edge && odd_bits != 0;
+
+            f32x16 s[QT][HT];
+#pragma unroll
+            for (int h = 0; h < HT; h++) {
+#pragma unroll
+                for (int rt = 0; rt < QT; rt++) s[rt][h] = f32x16{};
+#pragma unroll
+                for (int i = 0; i < KS; i++) {
+                    const uint32_t token = 32 * h + c, chunk = 2 * i + half;
+                    const TV x = __builtin_bit_cast(
+                        TV, *(const lds_u32x4 *)(uintptr_t)(lds_k + buffer * kBuffer + token * kRowBytes + ((chunk ^ swizzle(token)) << 4)));
+#pragma unroll
+                    for (int rt = 0; rt < QT; rt++) s[rt][h] = Mfma<T>::m32(x, q[rt][i], s[rt][h]);
+                }
+            }
+            uint32_t hidden[QT] = {};
+            if (edge) {
+#pragma unroll
+                for (int rt = 0; rt < QT; rt++)
+#pragma unroll
+                    for (int h = 0; h < HT; h++)
+#pragma unroll
+                        for (int i = 0; i < 16; i++) {
+                            const int token = 32 * h + 8 * (i / 4) + i % 4; // of the lower half; the upper half's is 4 further, brought by the same wavefront
+                            const bool sees = seen[rt].token(j + token + 4 * (int32_t)half) & ((there_bits >> (token / kTokens) & 1u) != 0);
+                            s[rt][h][i] = sees ? s[rt][h][i] : -INFINITY;
+                            hidden[rt] |= sees ? 0u : 1u << (16 * h + i);
+                        }
+            }
+            TV w[QT][2 * HT];
+#pragma unroll
+            for (int rt = 0; rt < QT; rt++) {
+                float top = s[rt][0][0];
+#pragma unroll
+                for (int h = 0; h < HT; h++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) top = fmaxf(top, s[rt][h][i]);
+                top = max_over_32(top);
+                // Weights are taken relative to a maximum that moves only when a score is more than a factor of 256 above it: they stay far
+                // inside the range of the type, and what has been added up is scaled now and then, not for every tile.
+                if (__any(top * a.scale > ref[rt] + 8.0f || (m[rt] == -INFINITY && top != -INFINITY))) {
+                    const bool first = m[rt] == -INFINITY;
+                    m[rt] = fmaxf(m[rt], top);
+                    const float next = m[rt] == -INFINITY ? 0.0f : m[rt] * a.scale;
+                    const float fade = first ? 0.0f : exp2_of(ref[rt] - next);
+                    ref[rt] = next;
+                    l[rt] *= fade;
+#pragma unroll
+                    for (int dt = 0; dt < DT; dt++) o[rt][dt] *= fade;
+                }
+                typedef float f32x8 __attribute__((ext_vector_type(8)));
+#pragma unroll
+                for (int u = 0; u < 2 * HT; u++) {
+                    f32x8 e;
+#pragma unroll
+                    for (int i = 0; i < 8; i++) e[i] = exp2_of(__builtin_fmaf(s[rt][u / 2][8 * (u % 2) + i], a.scale, -ref[rt]));
+                    l[rt] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+                    w[rt][u] = __builtin_convertvector(e, TV);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 2 * HT; u++)
+#pragma unroll
+                for (int dt = 0; dt < DT; dt++) {
+                    const uint32_t i16 = lane & 15u, token = 16 * u + 4 * half + (i16 >> 2), chunk = 4 * dt + 2 * (lane >> 4 & 1u) + (i16 >> 1 & 1u);
+                    const uint32_t at = lds_v + buffer * kBuffer + (i16 & 1u) * 8;
+                    const u32x2 lo = lds_column4(at + token * kRowBytes + ((chunk ^ swizzle(token)) << 4));
+                    const u32x2 hi = lds_column4(at + (token + 8) * kRowBytes + ((chunk ^ swizzle(token + 8)) << 4));
+                    u32x4 x = {lo[0], lo[1], hi[0], hi[1]};
+                    if (odd) { // as in the kernel for few rows
+                        const Split<T> y(x);
+                        x = y.finite;
+#pragma unroll
+                        for (int rt = 0; rt < QT; rt++) {
+                            u32x4 ones;
+#pragma unroll
+                            for (int i = 0; i < 4; i++)
+                                ones[i] = (hidden[rt] >> (8 * u + 2 * i) & 1u ? 0u : Mfma<T>::kOne) | (hidden[rt] >> (8 * u + 2 * i + 1) & 1u ? 0u : Mfma<T>::kOne << 16);
+                            const f32x16 ups = Mfma<T>::m32(__builtin_bit_cast(TV, y.up), __builtin_bit_cast(TV, ones), f32x16{});
+                            const f32x16 downs = Mfma<T>::m32(__builtin_bit_cast(TV, y.down), __builtin_bit_cast(TV, ones), f32x16{});
+#pragma unroll
+                            for (int i = 0; i < 16; i++)
+                                o[rt][dt][i] += (ups[i] > 0.0f ? INFINITY : 0.0f) + (downs[i] > 0.0f ? -INFINITY : 0.0f);
+                        }
+                    }
+#pragma unroll
+                    for (int rt = 0; rt < QT; rt++) o[rt][dt] = Mfma<T>::m32(__builtin_bit_cast(TV, x), w[rt][u], o[rt][dt]);
+                }
+        }
+        if (more) put(t + 1, next_page, buffer ^ 1u);
+        page = next_page, next_page = page_after;
+        __syncthreads();
+    }
+
+#pragma unroll
+    for (int rt = 0; rt < QT; rt++) {
+        const f32x2 both = swapped32(l[rt]);
+        const float total = both[0] + both[1];
+        float top = m[rt] == -INFINITY ? -INFINITY : ref[rt];
+        if (total != total && top == -INFINITY) top = 0.0f; // saw scores, none of them a number
+        const uint32_t i = i_first + wave * 32 * QT + 32 * rt + c;
+        if (i >= n) continue;
+        const uint32_t row = row_first + i / a.group, head = kv * a.group + i % a.group;
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+            for (int b = 0; b < 4; b++) {
+                const f32x4 v = {o[rt][dt][4 * b], o[rt][dt][4 * b + 1], o[rt][dt][4 * b + 2], o[rt][dt][4 * b + 3]};
+                store_result<T, D>(a, row, head, part.first_slot + split, 32 * dt + 8 * b + 4 * half, v, top, total);
+            }
+    }
+}
+
 // Joins the splits of a row and head: each has its sums relative to a maximum of its own.
 template <typename T, int D> __global__ __launch_bounds__(256) void dc_attention_join_kernel(AttentionArgs a)
 {
@@ -484,124 +817,82 @@ template <typename T, int D> __global__ __launch_bounds__(256) void dc_attention
     store_result<T, D>(whole, row, head, 0, 4 * at, sum, top, total);
 }
 
-__device__ __forceinline__ float sum_of_lanes(float v)
-{
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) v += __shfl_xor(v, i);
-    return v;
-}
-
-template <typename T, int D> __global__ __launch_bounds__(256) void dc_attention_rows_kernel(AttentionArgs a)
-{
-    constexpr int E = D / 64;
-    const uint32_t row = blockIdx.x, head = blockIdx.y, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    const uint32_t seq = a.batch.sequence_of(row);
-    if (seq >= a.batch.n_seqs) return;
-    const uint32_t end = a.batch.rows_end(seq);
-    const int32_t p = a.batch.length(seq) - (int32_t)(end - row), last = min(p, a.batch.capacity() - 1);
-    const T *q = static_cast<const T *>(a.q) + row * a.q_row + head * a.q_head + lane * E;
-    const uint32_t kv = head / a.group;
-    float qf[E], o[E], m = -INFINITY, l = 0.0f;
-#pragma unroll
-    for (int i = 0; i < E; i++) qf[i] = a.zero ? 0.0f : (float)q[i] * (a.negate ? -a.scale : a.scale) * kLn2, o[i] = 0.0f;
-    for (int32_t j = wave; j <= last; j += 4) {
-        if (a.window && (int64_t)j <= (int64_t)p - a.window && (uint32_t)j >= a.sinks) continue;
-        const int32_t page = a.batch.page_of(seq, j);
-        if (page < 0) continue;
-        const uint64_t at = ((((uint64_t)page * a.n_kv_heads + kv) << a.batch.page_shift) + a.batch.place_in_page(j)) * D + lane * E;
-        const T *k = static_cast<const T *>(a.k_pages) + at, *v = static_cast<const T *>(a.v_pages) + at;
-        float s = 0.0f;
-#pragma unroll
-        for (int i = 0; i < E; i++) s += qf[i] * (float)k[i];
-        s = sum_of_lanes(s);
-        if (s == -INFINITY) continue;
-        const float top = fmaxf(m, s), e = expf(s - top), f = expf(m - top);
-        l = l * f + e;
-#pragma unroll
-        for (int i = 0; i < E; i++) o[i] = o[i] * f + e * (float)v[i];
-        m = top;
-    }
-    __shared__ float ms[4], ls[4], os[4][D];
-    if (lane == 0) ms[wave] = m, ls[wave] = l;
-#pragma unroll
-    for (int i = 0; i < E; i++) os[wave][lane * E + i] = o[i];
-    __syncthreads();
-    if (wave) return;
-    float top = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3])), sum = 0.0f, r[E] = {};
-    for (int w = 0; w < 4; w++) {
-        if (ls[w] == 0.0f) continue;
-        const float f = expf(ms[w] - top);
-        sum += ls[w] * f;
-#pragma unroll
-        for (int i = 0; i < E; i++) r[i] += os[w][lane * E + i] * f;
-    }
-    T *out = static_cast<T *>(a.out) + row * a.out_row + head * a.out_head + lane * E;
-#pragma unroll
-    for (int i = 0; i < E; i++) out[i] = (T)(sum == 0.0f ? 0.0f : r[i] / sum);
-    if (a.lse && lane == 0) a.lse[(uint64_t)row * a.n_heads + head] = sum == 0.0f ? -INFINITY : top + logf(sum);
-}
+// Which kernel works through a part: that for at most 16 rows or 32 rows, or that for many.
+enum Kind { kFew16 = 0, kFew32 = 1, kTile = 2 };
+struct Plan {
+    int prefix_kind, own_kind;
+};
 
 bool attention_ok(const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_attention *t)
 {
     if (!cache_ok(cache) || !batch_ok(cache, batch) || !t) return false;
+    if ((uint64_t)batch->n_rows * t->n_heads >= 0x80000000ull) return false;
     if (t->n_heads < 1 || t->n_heads > 65535 || t->n_heads % cache->n_kv_heads || !isfinite(t->scale)) return false;
     return t->q_dev && t->out_dev && t->q_dev != t->out_dev && aligned16(t->q_dev) && aligned16(t->out_dev) && ((uintptr_t)t->lse_dev & 3u) == 0 &&
            strides_ok(t->q_row_stride, t->q_head_stride) &&
            strides_apart(t->out_row_stride, t->out_head_stride, batch->n_rows, t->n_heads, cache->head_dim);
 }
 
-template <typename T, int D> void launch_few(const AttentionArgs &a, uint32_t rows, hipStream_t stream)
+constexpr uint32_t kTileRows = 128;
+
+template <typename T, int D> void launch(const AttentionArgs &a, const Plan &plan, hipStream_t stream)
 {
-    const dim3 grid(a.prefix.blocks + a.own.blocks);
-    if (rows <= 16) hipLaunchKernelGGL((dc_attention_few_kernel<T, D, 1>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((dc_attention_few_kernel<T, D, 2>), grid, dim3(256), 0, stream, a);
+    // a launch for the parts of a kind
+    for (int kind = 0; kind < 3; kind++) {
+        AttentionArgs b = a;
+        if (plan.prefix_kind != kind) b.prefix.blocks = 0;
+        if (plan.own_kind != kind) b.own.blocks = 0;
+        const dim3 grid(b.prefix.blocks + b.own.blocks);
+        if (grid.x == 0) continue;
+        if (kind == kFew16) hipLaunchKernelGGL((dc_attention_few_kernel<T, D, 1>), grid, dim3(256), 0, stream, b);
+        if constexpr (D < 256) {
+            if (kind == kFew32) hipLaunchKernelGGL((dc_attention_few_kernel<T, D, 2>), grid, dim3(256), 0, stream, b);
+        }
+        if (kind == kTile) hipLaunchKernelGGL((dc_attention_tile_kernel<T, D, kTileRows / 128>), grid, dim3(256), 0, stream, b);
+    }
     if (a.n_slots > 1)
         hipLaunchKernelGGL((dc_attention_join_kernel<T, D>), dim3(a.batch.n_rows, a.n_heads), dim3(256), 0, stream, a);
 }
 
-template <typename T> void launch(const AttentionArgs &a, uint32_t head_dim, hipStream_t stream)
+template <typename T> void launch_d(const AttentionArgs &a, const Plan &plan, uint32_t head_dim, hipStream_t stream)
 {
-    const dim3 grid(a.batch.n_rows, a.n_heads);
-    if (a.own.blocks) {
-        const uint32_t rows = a.group * (a.prefix.blocks ? std::max(a.max_new, a.batch.n_rows) : a.max_new);
-        if (head_dim == 64) launch_few<T, 64>(a, rows, stream);
-        else if (head_dim == 128) launch_few<T, 128>(a, rows, stream);
-        else launch_few<T, 256>(a, rows, stream);
-        return;
-    }
-    if (head_dim == 64) hipLaunchKernelGGL((dc_attention_rows_kernel<T, 64>), grid, dim3(256), 0, stream, a);
-    else if (head_dim == 128) hipLaunchKernelGGL((dc_attention_rows_kernel<T, 128>), grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((dc_attention_rows_kernel<T, 256>), grid, dim3(256), 0, stream, a);
+    if (head_dim == 64) launch<T, 64>(a, plan, stream);
+    else if (head_dim == 128) launch<T, 128>(a, plan, stream);
+    else launch<T, 256>(a, plan, stream);
 }
 
 // How a call's keys are cut: fills prefix, own and n_slots, and gives the bytes of workspace.  False for a batch that is too large.
-bool plan(AttentionArgs &a, const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_attention *t, uint64_t *workspace_bytes)
+bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_attention *t, uint64_t *workspace_bytes)
 {
     *workspace_bytes = 0;
-    const uint32_t group = t->n_heads / cache->n_kv_heads;
-    constexpr uint64_t kTile = 32, kBlocks = 1024, kLeast = 4, kMost = 128;
-    auto cut = [&](uint64_t items, uint64_t tokens, uint32_t first_slot) {
-        const uint64_t n_tiles = (tokens + kTile - 1) / kTile;
-        uint64_t n = std::min((kBlocks + items - 1) / items, (n_tiles + kLeast - 1) / kLeast);
-        n = std::max<uint64_t>(1, std::min(n, kMost));
+    const uint32_t group = t->n_heads / cache->n_kv_heads, d = cache->head_dim;
+    auto kind_of = [&](uint64_t rows) { return rows <= 16 ? kFew16 : rows <= 32 && d < 256 ? kFew32 : kTile; };
+    // items: workgroups that a part has uncut
+    auto cut = [&](Kind kind, uint64_t items, uint64_t tokens, uint32_t first_slot) {
+        const uint64_t tile = kind == kTile && d < 256 ? 64 : 32, blocks = kind == kTile ? 512 : 1024, least = kind == kTile ? 8 : 4, most = 128;
+        const uint64_t n_tiles = (tokens + tile - 1) / tile;
+        uint64_t n = std::min((blocks + items - 1) / items, (n_tiles + least - 1) / least);
+        n = std::max<uint64_t>(1, std::min(n, most));
         const uint64_t chunk = std::max<uint64_t>(1, (n_tiles + n - 1) / n);
         n = std::max<uint64_t>(1, (n_tiles + chunk - 1) / chunk);
-        return Part{(uint32_t)(items * n), (uint32_t)n, (uint32_t)chunk, first_slot};
+        return items * n < 1u << 24 ? Part{(uint32_t)(items * n), (uint32_t)n, (uint32_t)chunk, first_slot} : Part{};
     };
-    const uint64_t rows = (uint64_t)group * (batch->prefix_len ? std::max(batch->max_new, batch->n_rows) : batch->max_new);
-    a.n_slots = 1;
-    if (rows > (cache->head_dim == 256 ? 16 : 32)) return true;
     uint64_t own = batch->max_len > batch->prefix_len ? batch->max_len - batch->prefix_len : 1;
     uint64_t common = batch->prefix_len;
-    if (t->window) {
-        const uint64_t seen = (uint64_t)t->window + batch->max_new + t->sinks + 2 * kTile;
-        own = std::min(own, seen), common = std::min(common, seen);
+    if (t->window) own = std::min(own, (uint64_t)t->window + batch->max_new + t->sinks + 128);
+    const uint64_t all_rows = (uint64_t)batch->n_rows * group;
+    const Kind prefix_kind = kind_of(all_rows), own_kind = kind_of((uint64_t)batch->max_new * group);
+    plan = Plan{prefix_kind, own_kind};
+    if (common) {
+        a.prefix = cut(prefix_kind, cache->n_kv_heads * (prefix_kind == kTile ? (all_rows + kTileRows - 1) / kTileRows : 1), common, 0);
+        if (!a.prefix.blocks) return false;
     }
-    if (common) a.prefix = cut(cache->n_kv_heads, common, 0);
-    a.own = cut((uint64_t)batch->n_seqs * cache->n_kv_heads, own, a.prefix.n_splits);
+    const uint64_t own_tiles = !batch->row_start_dev ? batch->n_seqs * ((uint64_t)(group + kTileRows - 1) / kTileRows)
+                                                     : std::min<uint64_t>(all_rows / kTileRows + batch->n_seqs, all_rows);
+    a.own = cut(own_kind, cache->n_kv_heads * (own_kind == kTile ? own_tiles : batch->n_seqs), own, a.prefix.n_splits);
+    if (!a.own.blocks) return false;
     a.n_slots = a.prefix.n_splits + a.own.n_splits;
-    if ((uint64_t)batch->n_seqs * cache->n_kv_heads * a.own.n_splits + a.prefix.blocks >= 1u << 24) return false;
-    if (a.n_slots > 1) *workspace_bytes = (uint64_t)batch->n_rows * t->n_heads * a.n_slots * (cache->head_dim + 2) * sizeof(float);
+    if (a.n_slots > 1) *workspace_bytes = (uint64_t)batch->n_rows * t->n_heads * a.n_slots * (d + 2) * sizeof(float);
     return true;
 }
 
@@ -612,7 +903,8 @@ extern "C" int dc_attention_paged_workspace(const dc_kv_cache *cache, const dc_k
 {
     if (!workspace_bytes || !attention_ok(cache, batch, attention)) return DC_E_ARG;
     AttentionArgs a = {};
-    return plan(a, cache, batch, attention, workspace_bytes) ? DC_OK : DC_E_ARG;
+    Plan plan;
+    return make_plan(a, plan, cache, batch, attention, workspace_bytes) ? DC_OK : DC_E_ARG;
 }
 
 extern "C" int dc_attention_paged(const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_attention *attention,
@@ -629,11 +921,12 @@ extern "C" int dc_attention_paged(const dc_kv_cache *cache, const dc_kv_batch *b
     a.negate = attention->scale < 0.0f, a.zero = attention->scale == 0.0f;
     a.scale = a.zero ? 1.0f : fabsf(attention->scale) * kLog2e;
     uint64_t needed = 0;
-    if (!plan(a, cache, batch, attention, &needed) || (needed && !workspace_dev)) return DC_E_ARG;
+    Plan plan;
+    if (!make_plan(a, plan, cache, batch, attention, &needed) || (needed && !workspace_dev)) return DC_E_ARG;
     if (workspace_bytes < needed) return DC_E_CAP;
     a.partial = static_cast<float *>(workspace_dev);
     a.partial_ml = reinterpret_cast<f32x2 *>(a.partial + (uint64_t)batch->n_rows * a.n_heads * a.n_slots * cache->head_dim);
-    if (cache->type == DC_TYPE_BF16) launch<__bf16>(a, cache->head_dim, static_cast<hipStream_t>(hip_stream));
-    else launch<_Float16>(a, cache->head_dim, static_cast<hipStream_t>(hip_stream));
+    if (cache->type == DC_TYPE_BF16) launch_d<__bf16>(a, plan, cache->head_dim, static_cast<hipStream_t>(hip_stream));
+    else launch_d<_Float16>(a, plan, cache->head_dim, static_cast<hipStream_t>(hip_stream));
     return dc_launch_status();
 }
