@@ -48,12 +48,12 @@ template <typename T> struct Mfma;
 template <> struct Mfma<__bf16> {
     __device__ static __forceinline__ f32x4 m16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     __device__ static __forceinline__ f32x16 m32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-    static constexpr uint32_t kExponent = 0x7F80u, kOne = 0x3F80u;
+    static constexpr uint32_t kExponent = 0x7F80u;
 };
 template <> struct Mfma<_Float16> {
     __device__ static __forceinline__ f32x4 m16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
     __device__ static __forceinline__ f32x16 m32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
-    static constexpr uint32_t kExponent = 0x7C00u, kOne = 0x3C00u;
+    static constexpr uint32_t kExponent = 0x7C00u;
 };
 
 // Maximum and sum over the lanes with the same number modulo 16 (32).
@@ -97,28 +97,27 @@ __device__ __forceinline__ u32x2 lds_column4(uint32_t addr)
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)addr));
 }
 
-// Eight values of V of which some are no numbers: those become 0, and up and down have ones where +infinity and -infinity (both: NaN) were.
-template <typename T> struct Split {
-    u32x4 finite, up, down;
-    __device__ __forceinline__ explicit Split(const u32x4 &x)
-    {
+// A value of V that is no number (an infinity, NaN) must reach only the rows that see its token, and a weight of 0 does not keep it from the
+// others in a matrix product.  Where rows of one product differ in what they see, such values go into it as 0, and the rows that
+// see their tokens get them by additions, from the cache once more.
+template <typename T> __device__ __forceinline__ bool is_odd(uint32_t value) { return (value & Mfma<T>::kExponent) == Mfma<T>::kExponent; }
+template <typename T> __device__ __forceinline__ u32x4 without_odd(u32x4 x)
+{
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            uint32_t f = 0, u = 0, d = 0;
+    for (int i = 0; i < 4; i++) x[i] = (is_odd<T>(x[i]) ? 0u : x[i] & 0xFFFFu) | (is_odd<T>(x[i] >> 16) ? 0u : x[i] & 0xFFFF0000u);
+    return x;
+}
+// Four neighbouring results of a row, with the values of a token that are no numbers added if the row sees it.
+template <typename T> __device__ __forceinline__ f32x4 with_odd(f32x4 sum, const T *values, bool sees)
+{
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    const u32x2 x = *reinterpret_cast<const u32x2 *>(values);
+    const f32x4 v = __builtin_convertvector(__builtin_bit_cast(T4, x), f32x4);
 #pragma unroll
-            for (int h = 0; h < 32; h += 16) {
-                const uint32_t y = x[i] >> h & 0xFFFFu;
-                const bool odd = (y & Mfma<T>::kExponent) == Mfma<T>::kExponent, nan = odd & ((y & 0x7FFFu) != Mfma<T>::kExponent);
-                const bool minus = (y & 0x8000u) != 0;
-                f |= odd ? 0u : y << h;
-                u |= (odd & (nan | !minus)) ? Mfma<T>::kOne << h : 0u;
-                d |= (odd & (nan | minus)) ? Mfma<T>::kOne << h : 0u;
-            }
-            finite[i] = f, up[i] = u, down[i] = d;
-        }
-    }
-};
-// What is left of a maximum over 16-bit values without their signs says whether one of them was no number.
+    for (int i = 0; i < 4; i++) sum[i] += (sees & is_odd<T>(x[i / 2] >> (16 * (i % 2)))) ? v[i] : 0.0f;
+    return sum;
+}
+// The largest of 16-bit values without their signs says whether one of them is no number.
 __device__ __forceinline__ u16x2 largest(u16x2 m, const u32x4 &x)
 {
 #pragma unroll
@@ -185,7 +184,7 @@ template <typename T, int D> __device__ __forceinline__ void store_result(const 
 // first operand, 8 tokens of one value, comes out of the LDS through the transposing read.  So maxima, sums and the scaling of
 // what has been added up stay inside a lane but for two exchanges a tile.  K goes from memory into registers, V through
 // registers into the wavefront's own part of the LDS: no barrier in the loop.  The next tile's loads are under way during the rest of the tile's work.
-template <typename T, int D, int RT> __global__ __launch_bounds__(256) void dc_attention_few_kernel(AttentionArgs a)
+template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void dc_attention_few_kernel(AttentionArgs a)
 {
     typedef typename Vec8<T>::type TV;
     constexpr int kTile = 32, KS = D / 32, DT = D / 16;
@@ -351,6 +350,10 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256) void dc_a
 #pragma unroll
             for (int i = 0; i < kLoads; i++) most = largest(most, v[i]);
             odd = __any((most[0] >= Mfma<T>::kExponent) | (most[1] >= Mfma<T>::kExponent));
+            if (odd) {
+#pragma unroll
+                for (int i = 0; i < kLoads; i++) v[i] = without_odd<T>(v[i]);
+            }
         }
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
@@ -360,10 +363,8 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256) void dc_a
         if (more) load_v(next_j, next_page);
 
         TV w[RT];
-        TV is_seen[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; rt++) {
-            uint32_t hidden = 0;
             if (edge) {
 #pragma unroll
                 for (int h = 0; h < 2; h++)
@@ -371,7 +372,6 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256) void dc_a
                     for (int i = 0; i < 4; i++) {
                         const bool sees = seen[rt].token(j + 16 * h + 4 * (int32_t)g + i) & (page[h] >= 0);
                         s[rt][h][i] = sees ? s[rt][h][i] : -INFINITY;
-                        hidden |= sees ? 0u : 1u << (4 * h + i);
                     }
             }
             float top = fmaxf(fmaxf(fmaxf(s[rt][0][0], s[rt][0][1]), fmaxf(s[rt][0][2], s[rt][0][3])),
@@ -388,11 +388,6 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256) void dc_a
             w[rt] = __builtin_convertvector(e, TV);
 #pragma unroll
             for (int dt = 0; dt < DT; dt++) o[rt][dt] *= fade;
-            u32x4 ones;
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-                ones[i] = (hidden >> (2 * i) & 1u ? 0u : Mfma<T>::kOne) | (hidden >> (2 * i + 1) & 1u ? 0u : Mfma<T>::kOne << 16);
-            is_seen[rt] = __builtin_bit_cast(TV, ones);
         }
         __builtin_amdgcn_wave_barrier();
         const uint32_t i4 = c >> 2, half8 = (c & 1u) << 3;
@@ -401,22 +396,20 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256) void dc_a
             const uint32_t row = 4 * g + i4, chunk = 2 * dt + ((c & 3u) >> 1);
             const uint32_t at = my_lds + row * kRowBytes + ((chunk ^ swizzle(row)) << 4) + half8;
             const u32x2 lo = lds_column4(at), hi = lds_column4(at + 16 * kRowBytes);
-            u32x4 x = {lo[0], lo[1], hi[0], hi[1]};
-            if (odd) {
-                // A value that is no number must reach only the rows that see its token, and a weight of 0 does not keep it from the
-                // others.  It is taken as 0 here, and added to the rows that see it: how many tokens they are says a product of ones.
-                const Split<T> y(x);
-                x = y.finite;
-#pragma unroll
-                for (int rt = 0; rt < RT; rt++) {
-                    const f32x4 ups = Mfma<T>::m16(__builtin_bit_cast(TV, y.up), is_seen[rt], f32x4{});
-                    const f32x4 downs = Mfma<T>::m16(__builtin_bit_cast(TV, y.down), is_seen[rt], f32x4{});
-#pragma unroll
-                    for (int i = 0; i < 4; i++) o[rt][dt][i] += (ups[i] > 0.0f ? INFINITY : 0.0f) + (downs[i] > 0.0f ? -INFINITY : 0.0f);
-                }
-            }
+            const u32x4 x = {lo[0], lo[1], hi[0], hi[1]};
 #pragma unroll
             for (int rt = 0; rt < RT; rt++) o[rt][dt] = Mfma<T>::m16(__builtin_bit_cast(TV, x), w[rt], o[rt][dt]);
+        }
+        if (odd) {
+#pragma unroll 1
+            for (int i = 0; i < kTile; i++) {
+                if (page[i / 16] < 0) continue;
+                const T *src = static_cast<const T *>(a.v_pages) + half_at(j + i, page[i / 16]) + 4 * g;
+#pragma unroll
+                for (int rt = 0; rt < RT; rt++)
+#pragma unroll
+                    for (int dt = 0; dt < DT; dt++) o[rt][dt] = with_odd<T>(o[rt][dt], src + 16 * dt, seen[rt].token(j + i));
+            }
         }
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -468,7 +461,7 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256) void dc_a
 // tile; a wavefront owns 32 QT rows.  The products are those of the kernel for few rows in the 32x32x16 shape: scores as [token][row]
 // = K Q^T, of which a lane holds 16 of 32 tokens of one row, results as [head_dim][row] = V^T P^T; maxima and sums stay in a lane but for one
 // exchange between the halves.
-template <typename T, int D, int QT> __global__ __launch_bounds__(256) void dc_attention_tile_kernel(AttentionArgs a)
+template <typename T, int D, int QT> __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void dc_attention_tile_kernel(AttentionArgs a)
 {
     typedef typename Vec8<T>::type TV;
     constexpr int kTile = D == 256 ? 32 : 64, KS = D / 16, DT = D / 32, HT = kTile / 32; // HT: 32-token products of a tile
@@ -627,7 +620,11 @@ template <typename T, int D, int QT> __global__ __launch_bounds__(256) void dc_a
                 v_new[i] = some ? v_new[i] : u32x4{};
                 most = largest(most, v_new[i]);
             }
-            if (__any((most[0] >= Mfma<T>::kExponent) | (most[1] >= Mfma<T>::kExponent))) flags |= 2u;
+            if (__any((most[0] >= Mfma<T>::kExponent) | (most[1] >= Mfma<T>::kExponent))) {
+                flags |= 2u;
+#pragma unroll
+                for (int i = 0; i < kLoads; i++) v_new[i] = without_odd<T>(v_new[i]);
+            }
         }
         if (lane == 0) lds_flags[buffer][wave] = flags;
 #pragma unroll
@@ -660,10 +657,9 @@ template <typename T, int D, int QT> __global__ __launch_bounds__(256) void dc_a
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 const uint32_t f = __builtin_amdgcn_readfirstlane(lds_flags[buffer][i]);
-                there_bits |= (f & 1u) << i, odd_bits |= f & 2u;
+                there_bits |= (f & 1u) << i, odd_bits |= (f >> 1) << i;
             }
             const bool edge = there_bits != 15u || j + kTile > first_sees.high || (j < last_sees.low && j + kTile > first_sees.sinks);
-            const bool odd = edge && odd_bits != 0;
 
             f32x16 s[QT][HT];
 #pragma unroll
@@ -679,7 +675,6 @@ template <typename T, int D, int QT> __global__ __launch_bounds__(256) void dc_a
                     for (int rt = 0; rt < QT; rt++) s[rt][h] = Mfma<T>::m32(x, q[rt][i], s[rt][h]);
                 }
             }
-            uint32_t hidden[QT] = {};
             if (edge) {
 #pragma unroll
                 for (int rt = 0; rt < QT; rt++)
@@ -690,7 +685,6 @@ template <typename T, int D, int QT> __global__ __launch_bounds__(256) void dc_a
                             const int token = 32 * h + 8 * (i / 4) + i % 4; // of the lower half; the upper half's is 4 further, brought by the same wavefront
                             const bool sees = seen[rt].token(j + token + 4 * (int32_t)half) & ((there_bits >> (token / kTokens) & 1u) != 0);
                             s[rt][h][i] = sees ? s[rt][h][i] : -INFINITY;
-                            hidden[rt] |= sees ? 0u : 1u << (16 * h + i);
                         }
             }
             TV w[QT][2 * HT];
@@ -732,26 +726,28 @@ template <typename T, int D, int QT> __global__ __launch_bounds__(256) void dc_a
                     const uint32_t at = lds_v + buffer * kBuffer + (i16 & 1u) * 8;
                     const u32x2 lo = lds_column4(at + token * kRowBytes + ((chunk ^ swizzle(token)) << 4));
                     const u32x2 hi = lds_column4(at + (token + 8) * kRowBytes + ((chunk ^ swizzle(token + 8)) << 4));
-                    u32x4 x = {lo[0], lo[1], hi[0], hi[1]};
-                    if (odd) { // as in the kernel for few rows
-                        const Split<T> y(x);
-                        x = y.finite;
-#pragma unroll
-                        for (int rt = 0; rt < QT; rt++) {
-                            u32x4 ones;
-#pragma unroll
-                            for (int i = 0; i < 4; i++)
-                                ones[i] = (hidden[rt] >> (8 * u + 2 * i) & 1u ? 0u : Mfma<T>::kOne) | (hidden[rt] >> (8 * u + 2 * i + 1) & 1u ? 0u : Mfma<T>::kOne << 16);
-                            const f32x16 ups = Mfma<T>::m32(__builtin_bit_cast(TV, y.up), __builtin_bit_cast(TV, ones), f32x16{});
-                            const f32x16 downs = Mfma<T>::m32(__builtin_bit_cast(TV, y.down), __builtin_bit_cast(TV, ones), f32x16{});
-#pragma unroll
-                            for (int i = 0; i < 16; i++)
-                                o[rt][dt][i] += (ups[i] > 0.0f ? INFINITY : 0.0f) + (downs[i] > 0.0f ? -INFINITY : 0.0f);
-                        }
-                    }
+                    const u32x4 x = {lo[0], lo[1], hi[0], hi[1]};
 #pragma unroll
                     for (int rt = 0; rt < QT; rt++) o[rt][dt] = Mfma<T>::m32(__builtin_bit_cast(TV, x), w[rt][u], o[rt][dt]);
                 }
+            if (odd_bits) {
+#pragma unroll 1
+                for (int i = 0; i < kTile; i++) {
+                    if (!(odd_bits >> (i / kTokens) & 1u)) continue;
+                    const int32_t page = table[(uint32_t)(j + i) >> a.batch.page_shift]; // there, or nothing of it would be odd
+                    const T *src = static_cast<const T *>(a.v_pages) + (page_stride * (uint32_t)page + head_at + ((uint32_t)(j + i) & place_mask)) * D + 4 * half;
+#pragma unroll
+                    for (int rt = 0; rt < QT; rt++)
+#pragma unroll
+                        for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+                            for (int b = 0; b < 4; b++) {
+                                f32x4 v = {o[rt][dt][4 * b], o[rt][dt][4 * b + 1], o[rt][dt][4 * b + 2], o[rt][dt][4 * b + 3]};
+                                v = with_odd<T>(v, src + 32 * dt + 8 * b, seen[rt].token(j + i));
+                                o[rt][dt][4 * b] = v[0], o[rt][dt][4 * b + 1] = v[1], o[rt][dt][4 * b + 2] = v[2], o[rt][dt][4 * b + 3] = v[3];
+                            }
+                }
+            }
         }
         if (more) put(t + 1, next_page, buffer ^ 1u);
         page = next_page, next_page = page_after;
