@@ -182,8 +182,8 @@ template <typename T, int D> __device__ __forceinline__ void store_result(const 
 // K as it lies in memory: a lane holds 8 neighbouring values of a token.  In the result a lane holds 4 tokens of one row in each
 // half of the tile, which is already the second operand of [head_dim][row] = V^T P^T if the product's 32 tokens are numbered that way; the
 // first operand, 8 tokens of one value, comes out of the LDS through the transposing read.  So maxima, sums and the scaling of
-// what has been added up stay inside a lane but for two exchanges a tile.  K goes from memory into registers, V through
-// registers into the wavefront's own part of the LDS: no barrier in the loop.  The next tile's loads are under way during the rest of the tile's work.
+// what has been added up stay inside a lane but for two exchanges a tile.  K and then V go through registers into the wavefront's
+// own part of the LDS: no barrier in the loop.  The next tile's loads are under way during the rest of the tile's work.
 template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void dc_attention_few_kernel(AttentionArgs a)
 {
     typedef typename Vec8<T>::type TV;
@@ -202,6 +202,20 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
     const uint32_t kv = item % a.n_kv_heads;
     item /= a.n_kv_heads;
     const uint32_t seq = common ? 0 : item % a.batch.n_seqs, split = common ? item : item / a.batch.n_seqs;
+    const int32_t *table = common ? a.batch.prefix_pages : a.batch.pages + (uint64_t)seq * a.batch.pages_stride;
+    const uint32_t table_entries = common ? (a.batch.prefix_len + (1u << a.batch.page_shift) - 1) >> a.batch.page_shift : a.batch.pages_stride;
+    // entries of a tile's two halves
+    auto entries_at = [&](uint32_t j, int32_t (&entry)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const uint32_t i = (j + 16 * h) >> a.batch.page_shift;
+            entry[h] = i < table_entries ? table[i] : -1;
+        }
+    };
+    // Without a window it is known at once where a wavefront's first tile is: its pages are asked for together with the sequence's length.
+    int32_t first_entry[2] = {-1, -1};
+    const uint64_t first_tile = (uint64_t)split * part.chunk + wave;
+    if (!a.window && first_tile < 1u << 26) entries_at((uint32_t)first_tile * kTile, first_entry);
 
     // rows of this workgroup: row_first + i / group of head kv * group + i % group for i < n
     uint32_t row_first = 0, n;
@@ -226,11 +240,11 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
     } else {
         row_first = a.batch.first_row(seq);
         const uint32_t end = a.batch.rows_end(seq);
+        const int32_t len = a.batch.length(seq);
         if (end <= row_first) return;
         const uint32_t rows = min(end - row_first, a.max_new);
         n = rows * a.group;
         base = (int32_t)a.batch.prefix_len;
-        const int32_t len = a.batch.length(seq);
         there = min(max(len - base, 0), (int32_t)(a.batch.pages_stride << a.batch.page_shift));
         p_first = len - (int32_t)(end - row_first);
         p_min = p_first - base, p_max = p_first + (int32_t)rows - 1 - base;
@@ -238,7 +252,6 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
     const Tiles<kTile> tiles(p_min, p_max, there, a.window, (int64_t)a.sinks - base);
     const int32_t t_begin = (int32_t)min((uint64_t)split * part.chunk, (uint64_t)tiles.count);
     const int32_t t_end = split + 1 == part.n_splits ? tiles.count : (int32_t)min((uint64_t)t_begin + part.chunk, (uint64_t)tiles.count);
-    const int32_t *table = common ? a.batch.prefix_pages : a.batch.pages + (uint64_t)seq * a.batch.pages_stride;
 
     // queries, and what the lane's rows see
     TV q[RT][KS];
@@ -272,49 +285,49 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
     const uint64_t head_at = (uint64_t)kv << a.batch.page_shift;
     const uint32_t place_mask = (1u << a.batch.page_shift) - 1u;
     // page of each half of a tile, -1 where there is none
-    auto pages_of = [&](int32_t tile, int32_t (&page)[2]) {
-        const int32_t j = tiles.first_token(tile);
+    auto pages_from = [&](const int32_t (&entry)[2], int32_t (&page)[2]) {
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const int32_t jj = j + 16 * h;
-            int32_t e = -1;
-            if (jj < tiles.high) e = table[(uint32_t)jj >> a.batch.page_shift];
-            page[h] = __builtin_amdgcn_readfirstlane((uint32_t)e < a.batch.n_pages ? e : -1);
-        }
+        for (int h = 0; h < 2; h++) page[h] = __builtin_amdgcn_readfirstlane((uint32_t)entry[h] < a.batch.n_pages ? entry[h] : -1);
+    };
+    auto pages_of = [&](int32_t tile, int32_t (&page)[2]) {
+        int32_t entry[2];
+        entries_at((uint32_t)tiles.first_token(tile), entry);
+        pages_from(entry, page);
     };
     // first value of a half's tokens; where there is no page, of page 0, whose tokens are then taken for hidden
     auto half_at = [&](int32_t j, int32_t page) {
         return (page_stride * (uint32_t)max(page, 0) + head_at + ((uint32_t)j & place_mask)) * D;
     };
-    TV k[2][KS];
-    u32x4 v[kLoads];
-    auto load_k = [&](int32_t j, const int32_t (&page)[2]) {
+    u32x4 k[kLoads], v[kLoads];
+    // A tile's keys or values in the order of memory, whole tokens side by side; nothing else will ask for them.
+    auto load = [&](u32x4 (&to)[kLoads], const void *pages, int32_t j, const int32_t (&page)[2]) {
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            const T *src = static_cast<const T *>(a.k_pages) + half_at(j + 16 * h, page[h]) + c * D + 8 * g;
+            const T *src = static_cast<const T *>(pages) + half_at(j + 16 * h, page[h]) + lane * 8;
 #pragma unroll
-            for (int s = 0; s < KS; s++) k[h][s] = *reinterpret_cast<const TV *>(src + 32 * s);
+            for (int i = 0; i < kLoads / 2; i++) to[h * (kLoads / 2) + i] = dcdev::load16_stream(src + i * 512);
         }
     };
-    auto load_v = [&](int32_t j, const int32_t (&page)[2]) {
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const T *src = static_cast<const T *>(a.v_pages) + half_at(j + 16 * h, page[h]) + lane * 8;
-#pragma unroll
-            for (int i = 0; i < kLoads / 2; i++) v[h * (kLoads / 2) + i] = *reinterpret_cast<const u32x4 *>(src + i * 512);
-        }
-    };
-    // Rows of V lie in the LDS with their 16-byte chunks exchanged so that 8 rows' pairs of chunks are on different banks.
+    // Tokens lie in the LDS with their 16-byte chunks exchanged so that 8 tokens' same chunks, and pairs of chunks, are on different banks.
     auto swizzle = [](uint32_t row) { return D == 64 ? ((row >> 1) & 3u) << 1 : (row & 7u) << 1; };
     const uint32_t my_lds = dcdev::lds_address(lds) + wave * (kTile * kRowBytes);
+    auto put = [&](const u32x4 (&from)[kLoads]) {
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const uint32_t row = i * kRowsALoad + lane / kChunks, chunk = lane % kChunks;
+            *(lds_u32x4 *)(uintptr_t)(my_lds + row * kRowBytes + ((chunk ^ swizzle(row)) << 4)) = from[i];
+        }
+        __builtin_amdgcn_wave_barrier();
+    };
 
     int32_t page[2], next_page[2];
     int32_t t = t_begin + (int32_t)wave;
     if (t < t_end) {
-        pages_of(t, page);
+        if (a.window) pages_of(t, page);
+        else pages_from(first_entry, page);
         const int32_t j = tiles.first_token(t);
-        load_k(j, page);
-        load_v(j, page);
+        load(k, a.k_pages, j, page);
+        load(v, a.v_pages, j, page);
         pages_of(min(t + 4, t_end - 1), next_page);
     }
     for (; t < t_end; t += 4) {
@@ -322,16 +335,22 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
         const bool more = t + 4 < t_end;
         const int32_t next_j = tiles.first_token(min(t + 4, t_end - 1));
 
+        put(k);
+        if (more) load(k, a.k_pages, next_j, next_page);
         f32x4 s[RT][2];
 #pragma unroll
-        for (int h = 0; h < 2; h++)
+        for (int h = 0; h < 2; h++) {
 #pragma unroll
-            for (int rt = 0; rt < RT; rt++) {
-                s[rt][h] = f32x4{};
+            for (int rt = 0; rt < RT; rt++) s[rt][h] = f32x4{};
 #pragma unroll
-                for (int i = 0; i < KS; i++) s[rt][h] = Mfma<T>::m16(k[h][i], q[rt][i], s[rt][h]);
+            for (int i = 0; i < KS; i++) {
+                const uint32_t row = 16 * h + c, chunk = 4 * i + g;
+                const TV x = __builtin_bit_cast(TV, *(const lds_u32x4 *)(uintptr_t)(my_lds + row * kRowBytes + ((chunk ^ swizzle(row)) << 4)));
+#pragma unroll
+                for (int rt = 0; rt < RT; rt++) s[rt][h] = Mfma<T>::m16(x, q[rt][i], s[rt][h]);
             }
-        if (more) load_k(next_j, next_page);
+        }
+        __builtin_amdgcn_wave_barrier();
 
         // tokens that not all rows see; those that none sees lie in the LDS as zeros
         const bool edge = page[0] < 0 || page[1] < 0 || j + kTile > p_min + 1 || j + kTile > tiles.high || (j < tiles.low && j + kTile > tiles.sinks) ||
@@ -355,12 +374,8 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
                 for (int i = 0; i < kLoads; i++) v[i] = without_odd<T>(v[i]);
             }
         }
-#pragma unroll
-        for (int i = 0; i < kLoads; i++) {
-            const uint32_t row = i * kRowsALoad + lane / kChunks, chunk = lane % kChunks;
-            *(lds_u32x4 *)(uintptr_t)(my_lds + row * kRowBytes + ((chunk ^ swizzle(row)) << 4)) = v[i];
-        }
-        if (more) load_v(next_j, next_page);
+        put(v);
+        if (more) load(v, a.v_pages, next_j, next_page);
 
         TV w[RT];
 #pragma unroll
@@ -389,7 +404,6 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
 #pragma unroll
             for (int dt = 0; dt < DT; dt++) o[rt][dt] *= fade;
         }
-        __builtin_amdgcn_wave_barrier();
         const uint32_t i4 = c >> 2, half8 = (c & 1u) << 3;
 #pragma unroll
         for (int dt = 0; dt < DT; dt++) {
@@ -773,35 +787,48 @@ template <typename T, int D, int QT> __global__ __launch_bounds__(256, D == 256 
     }
 }
 
-// Joins the splits of a row and head: each has its sums relative to a maximum of its own.
+// Joins the splits of a row and head: each has its sums relative to a maximum of its own.  The weights of the splits first, into the LDS; then
+// 4 D / 1024 of the threads go through every so many splits with several loads under way.
+constexpr uint32_t kMostSlots = 256;
 template <typename T, int D> __global__ __launch_bounds__(256) void dc_attention_join_kernel(AttentionArgs a)
 {
-    constexpr uint32_t kQuads = D / 4, kSets = 256 / kQuads;
+    constexpr uint32_t kQuads = D / 4, kSets = 256 / kQuads, kAtOnce = 4;
     __shared__ f32x4 lds_sum[kSets][kQuads];
+    __shared__ float lds_weight[kMostSlots], lds_top[4], lds_total[4];
     const uint32_t row = blockIdx.x, head = blockIdx.y, at = threadIdx.x % kQuads, set = threadIdx.x / kQuads;
+    const uint64_t first = ((uint64_t)row * a.n_heads + head) * a.n_slots;
+    f32x2 ml = {-INFINITY, 0.0f};
+    if (threadIdx.x < a.n_slots) ml = a.partial_ml[first + threadIdx.x];
     const uint32_t seq = a.batch.sequence_of(row);
     if (seq >= a.batch.n_seqs || row - a.batch.first_row(seq) >= a.max_new) return;
-    const uint64_t first = ((uint64_t)row * a.n_heads + head) * a.n_slots;
-    float top = -INFINITY, total = 0.0f;
-    for (uint32_t i = 0; i < a.n_slots; i += 64) {
-        const uint32_t slot = i + (threadIdx.x & 63u);
-        f32x2 ml = {-INFINITY, 0.0f};
-        if (slot < a.n_slots) ml = a.partial_ml[first + slot];
-        float t = max_over_16(ml[0]);
+    float top = max_over_16(ml[0]);
 #pragma unroll
-        for (int k = 1; k < 16; k <<= 1) t = fmaxf(t, __shfl_xor(t, k));
-        t = fmaxf(t, top);
-        float w = ml[0] == -INFINITY ? 0.0f : ml[1] * exp2_of(ml[0] - t);
-        w = sum_over_16(w);
+    for (int k = 1; k < 16; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
+    if ((threadIdx.x & 63u) == 0) lds_top[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(lds_top[0], lds_top[1]), fmaxf(lds_top[2], lds_top[3]));
+    const float weight = ml[0] == -INFINITY ? 0.0f : exp2_of(ml[0] - top);
+    lds_weight[threadIdx.x] = ml[0] == -INFINITY ? -1.0f : weight;
+    float total = sum_over_16(ml[0] == -INFINITY ? 0.0f : ml[1] * weight);
 #pragma unroll
-        for (int k = 1; k < 16; k <<= 1) w += __shfl_xor(w, k);
-        total = (top == -INFINITY ? 0.0f : total * exp2_of(top - t)) + w;
-        top = t;
-    }
+    for (int k = 1; k < 16; k <<= 1) total += __shfl_xor(total, k);
+    if ((threadIdx.x & 63u) == 0) lds_total[threadIdx.x >> 6] = total;
+    __syncthreads();
+    total = (lds_total[0] + lds_total[1]) + (lds_total[2] + lds_total[3]);
     f32x4 sum = {};
-    for (uint32_t slot = set; slot < a.n_slots; slot += kSets) {
-        const float m = a.partial_ml[first + slot][0];
-        if (m != -INFINITY) sum += *reinterpret_cast<const f32x4 *>(a.partial + (first + slot) * D + 4 * at) * exp2_of(m - top);
+    const float *src = a.partial + first * D + 4 * at;
+    for (uint32_t slot = set; slot < a.n_slots; slot += kSets * kAtOnce) {
+        f32x4 v[kAtOnce];
+        float w[kAtOnce];
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; i++) {
+            const uint32_t k = slot + i * kSets;
+            w[i] = k < a.n_slots ? lds_weight[k] : -1.0f; // a split that saw nothing has left nothing to add
+            v[i] = f32x4{};
+            if (w[i] >= 0.0f || w[i] != w[i]) v[i] = *reinterpret_cast<const f32x4 *>(src + (uint64_t)k * D);
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; i++) sum += v[i] * w[i];
     }
     lds_sum[set][at] = sum;
     __syncthreads();
@@ -865,10 +892,20 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     auto kind_of = [&](uint64_t rows) { return rows <= 16 ? kFew16 : rows <= 32 && d < 256 ? kFew32 : kTile; };
     // items: workgroups that a part has uncut
     auto cut = [&](Kind kind, uint64_t items, uint64_t tokens, uint32_t first_slot) {
-        const uint64_t tile = kind == kTile && d < 256 ? 64 : 32, blocks = kind == kTile ? 512 : 1024, least = kind == kTile ? 8 : 4, most = 128;
-        const uint64_t n_tiles = (tokens + tile - 1) / tile;
-        uint64_t n = std::min((blocks + items - 1) / items, (n_tiles + least - 1) / least);
-        n = std::max<uint64_t>(1, std::min(n, most));
+        const uint64_t tile = kind == kTile && d < 256 ? 64 : 32, least = kind == kTile ? 8 : 4;
+        const uint64_t n_tiles = (tokens + tile - 1) / tile, most = std::max<uint64_t>(1, std::min<uint64_t>((n_tiles + least - 1) / least, kMostSlots / 2));
+        uint64_t n = 1;
+        if (kind == kTile) {
+            // two workgroups on each of 256 compute units
+            n = std::min((512 + items - 1) / items, most);
+        } else {
+            // As few workgroups as give every compute unit the same number, to a tenth: a long run of keys is read faster by one workgroup
+            // (256 of 8 heads' and 32 sequences' runs of 8000 tokens: 161 us, 512 halves of them 168, 1024 quarters 176), but an uneven number
+            // leaves units idle (320 runs of 4100 tokens: 124 us, 960 thirds 108).
+            while (n < most && (items * n + 255) / 256 * 256 * 10 > items * n * 11) n++;
+            // Where little is to be read, its latency counts: two workgroups to a unit (one token over 1999, 32 heads: 12.0 us with 256, 11.6 with 512).
+            if (!batch->prefix_len && items * n <= 256 && (n_tiles + n - 1) / n <= 16) n = std::min(2 * n, most);
+        }
         const uint64_t chunk = std::max<uint64_t>(1, (n_tiles + n - 1) / n);
         n = std::max<uint64_t>(1, (n_tiles + chunk - 1) / chunk);
         return items * n < 1u << 24 ? Part{(uint32_t)(items * n), (uint32_t)n, (uint32_t)chunk, first_slot} : Part{};
