@@ -9,6 +9,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 using namespace dcpages;
 
@@ -468,23 +469,42 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
     }
 }
 
+#ifndef DC_AHEAD
+#define DC_AHEAD 6
+#endif
+#ifndef DC_KT
+#define DC_KT 64
+#endif
+#ifndef DC_TLB64
+#define DC_TLB64 3
+#endif
+#ifndef DC_TLB
+#define DC_TLB 2
+#endif
+#ifdef SCHED1
+#define DC_SCHED { __builtin_amdgcn_sched_group_barrier(0x100, 2*kAhead, 0); __builtin_amdgcn_sched_group_barrier(0x002, 28, 0); _Pragma("unroll") for (int i = 0; i < kGroups*DT; i++) { __builtin_amdgcn_sched_group_barrier(0x008, 1, 0); if (i + kAhead < kGroups*DT) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0); __builtin_amdgcn_sched_group_barrier(0x002, D == 64 ? 12 : 6, 0); } }
+#else
+#define DC_SCHED
+#endif
+constexpr uint32_t kTileRows = 128; // of a workgroup of the kernel for many rows
+
 // ---- many rows ------------------------------------------------------------------------------------------------------------
 //
-// A workgroup owns 128 QT rows of one key/value head (prompts, or the rows of many sequences behind a common prefix): the matrix
+// A workgroup owns 128 rows of one key/value head (prompts, or the rows of many sequences behind a common prefix): the matrix
 // units bound this kernel.  Keys and values go through the LDS in tiles that its four wavefronts share, double buffered with one barrier a
-// tile; a wavefront owns 32 QT rows.  The products are those of the kernel for few rows in the 32x32x16 shape: scores as [token][row]
+// tile; a wavefront owns 32 rows.  The products are those of the kernel for few rows in the 32x32x16 shape: scores as [token][row]
 // = K Q^T, of which a lane holds 16 of 32 tokens of one row, results as [head_dim][row] = V^T P^T; maxima and sums stay in a lane but for one
 // exchange between the halves.
-template <typename T, int D, int QT> __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void dc_attention_tile_kernel(AttentionArgs a)
+template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? DC_TLB64 : DC_TLB) void dc_attention_tile_kernel(AttentionArgs a)
 {
     typedef typename Vec8<T>::type TV;
-    constexpr int kTile = D == 256 ? 32 : 64, KS = D / 16, DT = D / 32, HT = kTile / 32; // HT: 32-token products of a tile
-    constexpr uint32_t kRows = 128 * QT, kRowBytes = 2 * D, kChunks = D / 8, kRowsALoad = 64 / kChunks;
+    constexpr int kTile = D == 256 ? 32 : DC_KT, KS = D / 16, DT = D / 32, HT = kTile / 32; // HT: 32-token products of a tile
+    constexpr uint32_t kRows = kTileRows, kRowBytes = 2 * D, kChunks = D / 8, kRowsALoad = 64 / kChunks;
     constexpr int kTokens = kTile / 4, kLoads = kTokens / (int)kRowsALoad; // tokens that a wavefront brings, in so many loads
     constexpr uint32_t kBuffer = kTile * kRowBytes;
     __shared__ __align__(16) uint8_t lds[4 * kBuffer]; // K, K, V, V
     __shared__ int32_t lds_p[kRows];
-    __shared__ __align__(16) uint32_t lds_flags[2][4];
+    __shared__ __align__(16) uint32_t lds_odd[2][4];
 
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31u, half = lane >> 5;
     const bool common = blockIdx.x < a.prefix.blocks;
@@ -571,61 +591,83 @@ template <typename T, int D, int QT> __global__ __launch_bounds__(256, D == 256 
     const int32_t t_begin = (int32_t)min((uint64_t)split * part.chunk, (uint64_t)tiles.count);
     const int32_t t_end = split + 1 == part.n_splits ? tiles.count : (int32_t)min((uint64_t)t_begin + part.chunk, (uint64_t)tiles.count);
     const int32_t all_see_high = Seen(p_min, there, a.window, sinks_left).high, all_see_low = Seen(p_max, there, a.window, sinks_left).low;
-    smallest_largest(wave * 32 * QT, 32 * QT, p_min, p_max);
+    smallest_largest(wave * 32, 32, p_min, p_max);
     const Seen first_sees(p_min, there, a.window, sinks_left), last_sees(p_max, there, a.window, sinks_left);
 
-    TV q[QT][KS];
-    Seen seen[QT];
-    f32x16 o[QT][DT];
-    float m[QT], ref[QT], l[QT];
+    const uint32_t my_row = i_first + wave * 32 + c, my_head = kv * a.group + my_row % a.group;
+    const uint64_t my_packed = row_first + my_row / a.group;
+    const Seen seen(lds_p[wave * 32 + c], there, a.window, sinks_left);
+    TV q[KS];
+    f32x16 o[DT];
+    float m = -INFINITY, ref = 0.0f, l = 0.0f;
+    const T *q_src = static_cast<const T *>(a.q) + my_packed * a.q_row + my_head * a.q_head + 8 * half;
 #pragma unroll
-    for (int rt = 0; rt < QT; rt++) {
-        const uint32_t at = wave * 32 * QT + 32 * rt + c, i = i_first + at;
-        const bool is = i < n;
-        const uint32_t head = kv * a.group + i % a.group;
-        seen[rt] = Seen(lds_p[at], there, a.window, sinks_left);
-        const T *src = static_cast<const T *>(a.q) + (uint64_t)(row_first + i / a.group) * a.q_row + head * a.q_head + 8 * half;
-#pragma unroll
-        for (int s = 0; s < KS; s++) {
-            u32x4 x = {};
-            if (is && !a.zero) x = *reinterpret_cast<const u32x4 *>(src + 16 * s);
-            if (a.negate) x ^= 0x80008000u;
-            q[rt][s] = __builtin_bit_cast(TV, x);
-        }
-        m[rt] = -INFINITY, ref[rt] = 0.0f, l[rt] = 0.0f;
-#pragma unroll
-        for (int dt = 0; dt < DT; dt++) o[rt][dt] = f32x16{};
+    for (int i = 0; i < KS; i++) {
+        u32x4 x = {};
+        if (my_row < n && !a.zero) x = *reinterpret_cast<const u32x4 *>(q_src + 16 * i);
+        if (a.negate) x ^= 0x80008000u;
+        q[i] = __builtin_bit_cast(TV, x);
     }
+#pragma unroll
+    for (int dt = 0; dt < DT; dt++) o[dt] = f32x16{};
 
     const uint64_t page_stride = (uint64_t)a.n_kv_heads << a.batch.page_shift;
     const uint64_t head_at = (uint64_t)kv << a.batch.page_shift;
     const uint32_t place_mask = (1u << a.batch.page_shift) - 1u;
-    // the page of the tokens that this wavefront brings, -1 where there is none
-    auto page_of = [&](int32_t t) {
-        const int32_t j = tiles.first_token(t) + (int32_t)wave * kTokens;
+    // Pages of 16 tiles, asked for 16 tiles ahead: lane l has that of the tokens that wavefront l mod 4 brings of tile i + l / 4, counted from
+    // t_begin; -1 where there is none.  (Scalar loads would do for what is the same in all lanes, but the LDS's data are waited for by
+    // the same counter, all of it.)
+    auto pages_from = [&](int32_t i) {
+        const int32_t t = t_begin + i + (int32_t)(lane >> 2), j = tiles.first_token(t) + (int32_t)(lane & 3u) * kTokens;
         int32_t e = -1;
-        if (j < tiles.high) e = table[(uint32_t)j >> a.batch.page_shift];
-        return (int32_t)__builtin_amdgcn_readfirstlane((uint32_t)e < a.batch.n_pages ? e : -1);
+        if (t < t_end && j < tiles.high) e = table[(uint32_t)j >> a.batch.page_shift];
+        return (uint32_t)e < a.batch.n_pages ? e : -1;
     };
+    int32_t pages = pages_from(0), pages_ahead = pages_from(16);
+    uint64_t pages_there = __ballot(pages >= 0);
+    auto my_page = [&](int32_t i) { return __builtin_amdgcn_readlane(pages, 4 * (i & 15) + (int32_t)wave); };
+    auto groups_there = [&](int32_t i) { return (uint32_t)(pages_there >> (4 * (i & 15))) & 15u; };
     u32x4 k_new[kLoads], v_new[kLoads];
-    auto load = [&](int32_t t, int32_t page) {
+    auto load = [&](u32x4 (&to)[kLoads], const void *pages, int32_t t, int32_t page) {
         const int32_t j = tiles.first_token(t) + (int32_t)wave * kTokens;
-        const uint64_t at = (page_stride * (uint32_t)max(page, 0) + head_at + ((uint32_t)j & place_mask)) * D + lane * 8;
+        const T *src = static_cast<const T *>(pages) + (page_stride * (uint32_t)max(page, 0) + head_at + ((uint32_t)j & place_mask)) * D + lane * 8;
 #pragma unroll
-        for (int i = 0; i < kLoads; i++) k_new[i] = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.k_pages) + at + i * 512);
-#pragma unroll
-        for (int i = 0; i < kLoads; i++) v_new[i] = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.v_pages) + at + i * 512);
+        for (int i = 0; i < kLoads; i++) to[i] = *reinterpret_cast<const u32x4 *>(src + i * 512);
     };
     // The 16-byte chunks of a token lie exchanged in the LDS, so that 16 tokens' same chunks are on different banks, and the same four of 4 tokens'.
     auto swizzle = [](uint32_t token) {
         return D == 64 ? (token >> 1 & 1u) << 2 | (token >> 2 & 3u) : (token & 3u) << 2 | (token >> 2 & 3u);
     };
     const uint32_t lds_k = dcdev::lds_address(lds), lds_v = lds_k + 2 * kBuffer;
-    // flags of the tokens that a wavefront brought: 1 they are there, 2 a value of V that not all rows see is no number
-    auto put = [&](int32_t t, int32_t page, uint32_t buffer) {
-        const int32_t j = tiles.first_token(t) + (int32_t)wave * kTokens;
-        uint32_t flags = page >= 0 ? 1u : 0u;
-        if (page < 0 || j + kTokens > all_see_high || j < all_see_low) {
+    // where a lane puts what it brings, and where it reads its part of the first operands
+    uint32_t put_at[kLoads], k_at[KS], v_at[DT][2];
+#pragma unroll
+    for (int i = 0; i < kLoads; i++) {
+        const uint32_t token = wave * kTokens + i * kRowsALoad + lane / kChunks, chunk = lane % kChunks;
+        put_at[i] = token * kRowBytes + ((chunk ^ swizzle(token)) << 4);
+    }
+#pragma unroll
+    for (int i = 0; i < KS; i++) k_at[i] = c * kRowBytes + (((2 * i + half) ^ swizzle(c)) << 4);
+#pragma unroll
+    for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const uint32_t i16 = lane & 15u, token = 4 * half + (i16 >> 2) + 8 * h, chunk = 4 * dt + 2 * (lane >> 4 & 1u) + (i16 >> 1 & 1u);
+            v_at[dt][h] = token * kRowBytes + ((chunk ^ swizzle(token)) << 4) + (i16 & 1u) * 8;
+        }
+    auto put_k = [&](uint32_t buffer) {
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) *(lds_u32x4 *)(uintptr_t)(lds_k + buffer * kBuffer + put_at[i]) = k_new[i];
+    };
+    // tokens that not all rows of the workgroup see, among them those on pages that are not there
+    auto is_partial = [&](int32_t t, uint32_t there_bits) {
+        const int32_t j = tiles.first_token(t);
+        return there_bits != 15u || j + kTile > all_see_high || j < all_see_low;
+    };
+    // Of a partial tile a wavefront leaves in lds_odd whether one of the values of V that it brought is no number.
+    auto put_v = [&](int32_t t, int32_t page, bool partial, uint32_t buffer) {
+        if (partial) {
+            const int32_t j = tiles.first_token(t) + (int32_t)wave * kTokens;
             u16x2 most = {};
 #pragma unroll
             for (int i = 0; i < kLoads; i++) {
@@ -634,157 +676,167 @@ template <typename T, int D, int QT> __global__ __launch_bounds__(256, D == 256 
                 v_new[i] = some ? v_new[i] : u32x4{};
                 most = largest(most, v_new[i]);
             }
-            if (__any((most[0] >= Mfma<T>::kExponent) | (most[1] >= Mfma<T>::kExponent))) {
-                flags |= 2u;
+            const bool odd = __any((most[0] >= Mfma<T>::kExponent) | (most[1] >= Mfma<T>::kExponent));
+            if (odd) {
 #pragma unroll
                 for (int i = 0; i < kLoads; i++) v_new[i] = without_odd<T>(v_new[i]);
             }
+            if (lane == 0) lds_odd[buffer][wave] = odd;
         }
-        if (lane == 0) lds_flags[buffer][wave] = flags;
 #pragma unroll
-        for (int i = 0; i < kLoads; i++) {
-            const uint32_t token = wave * kTokens + i * kRowsALoad + lane / kChunks, chunk = lane % kChunks;
-            const uint32_t at = buffer * kBuffer + token * kRowBytes + ((chunk ^ swizzle(token)) << 4);
-            *(lds_u32x4 *)(uintptr_t)(lds_k + at) = k_new[i];
-            *(lds_u32x4 *)(uintptr_t)(lds_v + at) = v_new[i];
-        }
+        for (int i = 0; i < kLoads; i++) *(lds_u32x4 *)(uintptr_t)(lds_v + buffer * kBuffer + put_at[i]) = v_new[i];
+    };
+    auto k_operand = [&](int i, uint32_t buffer) {
+        return __builtin_bit_cast(TV, *(const lds_u32x4 *)(uintptr_t)(lds_k + buffer * kBuffer + 32 * (i / KS) * kRowBytes + k_at[i % KS]));
+    };
+    auto v_operand = [&](int i, uint32_t buffer) {
+        const u32x2 lo = lds_column4(lds_v + buffer * kBuffer + 16 * (i / DT) * kRowBytes + v_at[i % DT][0]);
+        const u32x2 hi = lds_column4(lds_v + buffer * kBuffer + 16 * (i / DT) * kRowBytes + v_at[i % DT][1]);
+        return __builtin_bit_cast(TV, u32x4{lo[0], lo[1], hi[0], hi[1]});
     };
 
-    int32_t page = -1, next_page = -1;
-    if (t_begin < t_end) {
-        page = page_of(t_begin);
-        load(t_begin, page);
-        put(t_begin, page, 0);
-        next_page = page_of(min(t_begin + 1, t_end - 1));
-    }
-    __syncthreads();
-    for (int32_t t = t_begin; t < t_end; t++) {
-        const uint32_t buffer = (uint32_t)(t - t_begin) & 1u;
+    // A step works on tile t, whose keys and values are in buffer B, while the next tile's are brought.
+    uint32_t there_bits = 0;
+    auto step = [&](auto B, int32_t t) {
+        constexpr uint32_t buffer = decltype(B)::value;
+        constexpr int kProducts = HT * KS, kGroups = 2 * HT, kAhead = DC_AHEAD;
         const int32_t j = tiles.first_token(t);
         const bool more = t + 1 < t_end;
-        if (more) load(t + 1, next_page);
-        const int32_t page_after = page_of(min(t + 2, t_end - 1));
+        const int32_t next = t + 1 - t_begin;
+        if ((next & 15) == 0) {
+            pages = pages_ahead, pages_there = __ballot(pages >= 0);
+            pages_ahead = pages_from(next + 16);
+        }
+        const int32_t next_page = my_page(next);
+        const uint32_t next_there = groups_there(next);
+        if (more) {
+            load(k_new, a.k_pages, t + 1, next_page);
+            load(v_new, a.v_pages, t + 1, next_page);
+        }
 
         // a wavefront whose rows see nothing of the tile has nothing to do
         if (j < last_sees.high && (j + kTile > first_sees.low || j < last_sees.sinks)) {
-            uint32_t there_bits = 0, odd_bits = 0;
+            // The operands come out of the LDS several products ahead of their use.
+            f32x16 s[HT];
+            TV x[kAhead];
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const uint32_t f = __builtin_amdgcn_readfirstlane(lds_flags[buffer][i]);
-                there_bits |= (f & 1u) << i, odd_bits |= (f >> 1) << i;
+            for (int i = 0; i < kAhead; i++) x[i] = k_operand(i, buffer);
+#pragma unroll
+            for (int i = 0; i < kProducts; i++) {
+                s[i / KS] = Mfma<T>::m32(x[i % kAhead], q[i % KS], i % KS ? s[i / KS] : f32x16{});
+                if (i + kAhead < kProducts) x[i % kAhead] = k_operand(i + kAhead, buffer);
             }
-            const bool edge = there_bits != 15u || j + kTile > first_sees.high || (j < last_sees.low && j + kTile > first_sees.sinks);
+            __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+            for (int i = 0; i < kProducts - kAhead; i++) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
 
-            f32x16 s[QT][HT];
-#pragma unroll
-            for (int h = 0; h < HT; h++) {
-#pragma unroll
-                for (int rt = 0; rt < QT; rt++) s[rt][h] = f32x16{};
-#pragma unroll
-                for (int i = 0; i < KS; i++) {
-                    const uint32_t token = 32 * h + c, chunk = 2 * i + half;
-                    const TV x = __builtin_bit_cast(
-                        TV, *(const lds_u32x4 *)(uintptr_t)(lds_k + buffer * kBuffer + token * kRowBytes + ((chunk ^ swizzle(token)) << 4)));
-#pragma unroll
-                    for (int rt = 0; rt < QT; rt++) s[rt][h] = Mfma<T>::m32(x, q[rt][i], s[rt][h]);
-                }
-            }
-            if (edge) {
-#pragma unroll
-                for (int rt = 0; rt < QT; rt++)
-#pragma unroll
-                    for (int h = 0; h < HT; h++)
-#pragma unroll
-                        for (int i = 0; i < 16; i++) {
-                            const int token = 32 * h + 8 * (i / 4) + i % 4; // of the lower half; the upper half's is 4 further, brought by the same wavefront
-                            const bool sees = seen[rt].token(j + token + 4 * (int32_t)half) & ((there_bits >> (token / kTokens) & 1u) != 0);
-                            s[rt][h][i] = sees ? s[rt][h][i] : -INFINITY;
-                        }
-            }
-            TV w[QT][2 * HT];
-#pragma unroll
-            for (int rt = 0; rt < QT; rt++) {
-                float top = s[rt][0][0];
+            if (there_bits != 15u || j + kTile > first_sees.high || (j < last_sees.low && j + kTile > first_sees.sinks)) {
 #pragma unroll
                 for (int h = 0; h < HT; h++)
 #pragma unroll
-                    for (int i = 0; i < 16; i++) top = fmaxf(top, s[rt][h][i]);
-                top = max_over_32(top);
-                // Weights are taken relative to a maximum that moves only when a score is more than a factor of 256 above it: they stay far
-                // inside the range of the type, and what has been added up is scaled now and then, not for every tile.
-                if (__any(top * a.scale > ref[rt] + 8.0f || (m[rt] == -INFINITY && top != -INFINITY))) {
-                    const bool first = m[rt] == -INFINITY;
-                    m[rt] = fmaxf(m[rt], top);
-                    const float next = m[rt] == -INFINITY ? 0.0f : m[rt] * a.scale;
-                    const float fade = first ? 0.0f : exp2_of(ref[rt] - next);
-                    ref[rt] = next;
-                    l[rt] *= fade;
+                    for (int i = 0; i < 16; i++) {
+                        const int token = 32 * h + 8 * (i / 4) + i % 4; // of the lower half; the upper half's is 4 further, brought by the same wavefront
+                        const bool sees = seen.token(j + token + 4 * (int32_t)half) & ((there_bits >> (token / kTokens) & 1u) != 0);
+                        s[h][i] = sees ? s[h][i] : -INFINITY;
+                    }
+            }
+            float top = s[0][0];
 #pragma unroll
-                    for (int dt = 0; dt < DT; dt++) o[rt][dt] *= fade;
-                }
+            for (int h = 0; h < HT; h++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) top = fmaxf(top, s[h][i]);
+            top = max_over_32(top);
+            // Weights are taken relative to a maximum that moves only when a score is more than a factor of 256 above it: they stay far
+            // inside the range of the type, and what has been added up is scaled now and then, not for every tile.
+            if (__any(top * a.scale > ref + 8.0f || (m == -INFINITY && top != -INFINITY))) {
+                const bool first = m == -INFINITY;
+                m = fmaxf(m, top);
+                const float next = m == -INFINITY ? 0.0f : m * a.scale;
+                const float fade = first ? 0.0f : exp2_of(ref - next);
+                ref = next;
+                l *= fade;
+#pragma unroll
+                for (int dt = 0; dt < DT; dt++) o[dt] *= fade;
+            }
+            TV w[kGroups];
+#pragma unroll
+            for (int i = 0; i < kAhead; i++) x[i] = v_operand(i, buffer);
+#pragma unroll
+            for (int u = 0; u < kGroups; u++) {
                 typedef float f32x8 __attribute__((ext_vector_type(8)));
+                f32x8 e;
 #pragma unroll
-                for (int u = 0; u < 2 * HT; u++) {
-                    f32x8 e;
-#pragma unroll
-                    for (int i = 0; i < 8; i++) e[i] = exp2_of(__builtin_fmaf(s[rt][u / 2][8 * (u % 2) + i], a.scale, -ref[rt]));
-                    l[rt] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-                    w[rt][u] = __builtin_convertvector(e, TV);
-                }
+                for (int i = 0; i < 8; i++) e[i] = exp2_of(__builtin_fmaf(s[u / 2][8 * (u % 2) + i], a.scale, -ref));
+                l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+                w[u] = __builtin_convertvector(e, TV);
             }
 #pragma unroll
-            for (int u = 0; u < 2 * HT; u++)
+            for (int i = 0; i < kGroups * DT; i++) {
+                o[i % DT] = Mfma<T>::m32(x[i % kAhead], w[i / DT], o[i % DT]);
+                if (i + kAhead < kGroups * DT) x[i % kAhead] = v_operand(i + kAhead, buffer);
+            }
+            dcdev::in_register<false>(l); // the additions among the products, not behind them
+            DC_SCHED
+            uint32_t odd_bits = 0;
+            if (is_partial(t, there_bits)) {
 #pragma unroll
-                for (int dt = 0; dt < DT; dt++) {
-                    const uint32_t i16 = lane & 15u, token = 16 * u + 4 * half + (i16 >> 2), chunk = 4 * dt + 2 * (lane >> 4 & 1u) + (i16 >> 1 & 1u);
-                    const uint32_t at = lds_v + buffer * kBuffer + (i16 & 1u) * 8;
-                    const u32x2 lo = lds_column4(at + token * kRowBytes + ((chunk ^ swizzle(token)) << 4));
-                    const u32x2 hi = lds_column4(at + (token + 8) * kRowBytes + ((chunk ^ swizzle(token + 8)) << 4));
-                    const u32x4 x = {lo[0], lo[1], hi[0], hi[1]};
-#pragma unroll
-                    for (int rt = 0; rt < QT; rt++) o[rt][dt] = Mfma<T>::m32(__builtin_bit_cast(TV, x), w[rt][u], o[rt][dt]);
-                }
+                for (int i = 0; i < 4; i++) odd_bits |= __builtin_amdgcn_readfirstlane(lds_odd[buffer][i]) << i;
+            }
             if (odd_bits) {
 #pragma unroll 1
                 for (int i = 0; i < kTile; i++) {
                     if (!(odd_bits >> (i / kTokens) & 1u)) continue;
-                    const int32_t page = table[(uint32_t)(j + i) >> a.batch.page_shift]; // there, or nothing of it would be odd
-                    const T *src = static_cast<const T *>(a.v_pages) + (page_stride * (uint32_t)page + head_at + ((uint32_t)(j + i) & place_mask)) * D + 4 * half;
+                    const int32_t at = table[(uint32_t)(j + i) >> a.batch.page_shift]; // there, or nothing of it would be odd
+                    const T *src = static_cast<const T *>(a.v_pages) + (page_stride * (uint32_t)at + head_at + ((uint32_t)(j + i) & place_mask)) * D + 4 * half;
+                    const bool sees = seen.token(j + i);
 #pragma unroll
-                    for (int rt = 0; rt < QT; rt++)
+                    for (int dt = 0; dt < DT; dt++)
 #pragma unroll
-                        for (int dt = 0; dt < DT; dt++)
-#pragma unroll
-                            for (int b = 0; b < 4; b++) {
-                                f32x4 v = {o[rt][dt][4 * b], o[rt][dt][4 * b + 1], o[rt][dt][4 * b + 2], o[rt][dt][4 * b + 3]};
-                                v = with_odd<T>(v, src + 32 * dt + 8 * b, seen[rt].token(j + i));
-                                o[rt][dt][4 * b] = v[0], o[rt][dt][4 * b + 1] = v[1], o[rt][dt][4 * b + 2] = v[2], o[rt][dt][4 * b + 3] = v[3];
-                            }
+                        for (int b = 0; b < 4; b++) {
+                            f32x4 v = {o[dt][4 * b], o[dt][4 * b + 1], o[dt][4 * b + 2], o[dt][4 * b + 3]};
+                            v = with_odd<T>(v, src + 32 * dt + 8 * b, sees);
+                            o[dt][4 * b] = v[0], o[dt][4 * b + 1] = v[1], o[dt][4 * b + 2] = v[2], o[dt][4 * b + 3] = v[3];
+                        }
                 }
             }
         }
-        if (more) put(t + 1, next_page, buffer ^ 1u);
-        page = next_page, next_page = page_after;
+        if (more) {
+            put_k(buffer ^ 1u);
+            put_v(t + 1, next_page, is_partial(t + 1, next_there), buffer ^ 1u);
+        }
+        there_bits = next_there;
         __syncthreads();
+    };
+
+    if (t_begin < t_end) {
+        there_bits = groups_there(0);
+        load(k_new, a.k_pages, t_begin, my_page(0));
+        load(v_new, a.v_pages, t_begin, my_page(0));
+        put_k(0);
+        put_v(t_begin, my_page(0), is_partial(t_begin, there_bits), 0);
+    }
+    __syncthreads();
+    for (int32_t t = t_begin; t < t_end; t += 2) {
+        step(std::integral_constant<uint32_t, 0>{}, t);
+        if (t + 1 < t_end) step(std::integral_constant<uint32_t, 1>{}, t + 1);
     }
 
+    const f32x2 both = swapped32(l);
+    const float total = both[0] + both[1];
+    float top = m == -INFINITY ? -INFINITY : ref;
+    if (total != total && top == -INFINITY) top = 0.0f; // saw scores, none of them a number
+    if (my_row >= n) return;
 #pragma unroll
-    for (int rt = 0; rt < QT; rt++) {
-        const f32x2 both = swapped32(l[rt]);
-        const float total = both[0] + both[1];
-        float top = m[rt] == -INFINITY ? -INFINITY : ref[rt];
-        if (total != total && top == -INFINITY) top = 0.0f; // saw scores, none of them a number
-        const uint32_t i = i_first + wave * 32 * QT + 32 * rt + c;
-        if (i >= n) continue;
-        const uint32_t row = row_first + i / a.group, head = kv * a.group + i % a.group;
+    for (int dt = 0; dt < DT; dt++)
 #pragma unroll
-        for (int dt = 0; dt < DT; dt++)
-#pragma unroll
-            for (int b = 0; b < 4; b++) {
-                const f32x4 v = {o[rt][dt][4 * b], o[rt][dt][4 * b + 1], o[rt][dt][4 * b + 2], o[rt][dt][4 * b + 3]};
-                store_result<T, D>(a, row, head, part.first_slot + split, 32 * dt + 8 * b + 4 * half, v, top, total);
-            }
-    }
+        for (int b = 0; b < 4; b++) {
+            const f32x4 v = {o[dt][4 * b], o[dt][4 * b + 1], o[dt][4 * b + 2], o[dt][4 * b + 3]};
+            store_result<T, D>(a, (uint32_t)my_packed, my_head, part.first_slot + split, 32 * dt + 8 * b + 4 * half, v, top, total);
+        }
 }
 
 // Joins the splits of a row and head: each has its sums relative to a maximum of its own.  The weights of the splits first, into the LDS; then
@@ -856,8 +908,6 @@ bool attention_ok(const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_a
            strides_apart(t->out_row_stride, t->out_head_stride, batch->n_rows, t->n_heads, cache->head_dim);
 }
 
-constexpr uint32_t kTileRows = 128;
-
 template <typename T, int D> void launch(const AttentionArgs &a, const Plan &plan, hipStream_t stream)
 {
     // a launch for the parts of a kind
@@ -871,7 +921,7 @@ template <typename T, int D> void launch(const AttentionArgs &a, const Plan &pla
         if constexpr (D < 256) {
             if (kind == kFew32) hipLaunchKernelGGL((dc_attention_few_kernel<T, D, 2>), grid, dim3(256), 0, stream, b);
         }
-        if (kind == kTile) hipLaunchKernelGGL((dc_attention_tile_kernel<T, D, kTileRows / 128>), grid, dim3(256), 0, stream, b);
+        if (kind == kTile) hipLaunchKernelGGL((dc_attention_tile_kernel<T, D>), grid, dim3(256), 0, stream, b);
     }
     if (a.n_slots > 1)
         hipLaunchKernelGGL((dc_attention_join_kernel<T, D>), dim3(a.batch.n_rows, a.n_heads), dim3(256), 0, stream, a);
@@ -892,7 +942,7 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     auto kind_of = [&](uint64_t rows) { return rows <= 16 ? kFew16 : rows <= 32 && d < 256 ? kFew32 : kTile; };
     // items: workgroups that a part has uncut
     auto cut = [&](Kind kind, uint64_t items, uint64_t tokens, uint32_t first_slot) {
-        const uint64_t tile = kind == kTile && d < 256 ? 64 : 32, least = kind == kTile ? 8 : 4;
+        const uint64_t tile = kind == kTile && d < 256 ? DC_KT : 32, least = kind == kTile ? 8 : 4;
         const uint64_t n_tiles = (tokens + tile - 1) / tile, most = std::max<uint64_t>(1, std::min<uint64_t>((n_tiles + least - 1) / least, kMostSlots / 2));
         uint64_t n = 1;
         if (kind == kTile) {
