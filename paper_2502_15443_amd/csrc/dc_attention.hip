@@ -599,7 +599,9 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
     const Seen seen(lds_p[wave * 32 + c], there, a.window, sinks_left);
     TV q[KS];
     f32x16 o[DT];
-    float m = -INFINITY, ref = 0.0f, l = 0.0f;
+    f32x16 below = f32x16{}; // the reference with the other sign, in every value
+    bool any = false;        // a score has been seen
+    float l = 0.0f;
     const T *q_src = static_cast<const T *>(a.q) + my_packed * a.q_row + my_head * a.q_head + 8 * half;
 #pragma unroll
     for (int i = 0; i < KS; i++) {
@@ -628,11 +630,13 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
     auto my_page = [&](int32_t i) { return __builtin_amdgcn_readlane(pages, 4 * (i & 15) + (int32_t)wave); };
     auto groups_there = [&](int32_t i) { return (uint32_t)(pages_there >> (4 * (i & 15))) & 15u; };
     u32x4 k_new[kLoads], v_new[kLoads];
-    auto load = [&](u32x4 (&to)[kLoads], const void *pages, int32_t t, int32_t page) {
+    auto bring = [&](int32_t t, int32_t page) {
         const int32_t j = tiles.first_token(t) + (int32_t)wave * kTokens;
-        const T *src = static_cast<const T *>(pages) + (page_stride * (uint32_t)max(page, 0) + head_at + ((uint32_t)j & place_mask)) * D + lane * 8;
+        const uint64_t at = (page_stride * (uint32_t)max(page, 0) + head_at + ((uint32_t)j & place_mask)) * D + lane * 8;
 #pragma unroll
-        for (int i = 0; i < kLoads; i++) to[i] = *reinterpret_cast<const u32x4 *>(src + i * 512);
+        for (int i = 0; i < kLoads; i++) k_new[i] = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.k_pages) + at + i * 512);
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) v_new[i] = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.v_pages) + at + i * 512);
     };
     // The 16-byte chunks of a token lie exchanged in the LDS, so that 16 tokens' same chunks are on different banks, and the same four of 4 tokens'.
     auto swizzle = [](uint32_t token) {
@@ -665,14 +669,15 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
         return there_bits != 15u || j + kTile > all_see_high || j < all_see_low;
     };
     // Of a partial tile a wavefront leaves in lds_odd whether one of the values of V that it brought is no number.
-    auto put_v = [&](int32_t t, int32_t page, bool partial, uint32_t buffer) {
+    auto put_v = [&](int32_t t, uint32_t there_bits, uint32_t buffer) {
+        const bool partial = is_partial(t, there_bits), is_there = (there_bits >> wave & 1u) != 0;
         if (partial) {
             const int32_t j = tiles.first_token(t) + (int32_t)wave * kTokens;
             u16x2 most = {};
 #pragma unroll
             for (int i = 0; i < kLoads; i++) {
                 const int32_t jj = j + i * (int32_t)kRowsALoad + (int32_t)(lane / kChunks);
-                const bool some = (page >= 0) & (jj < tiles.high) & ((jj >= tiles.low) | (jj < tiles.sinks));
+                const bool some = is_there & (jj < tiles.high) & ((jj >= tiles.low) | (jj < tiles.sinks));
                 v_new[i] = some ? v_new[i] : u32x4{};
                 most = largest(most, v_new[i]);
             }
@@ -695,24 +700,24 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
         return __builtin_bit_cast(TV, u32x4{lo[0], lo[1], hi[0], hi[1]});
     };
 
-    // A step works on tile t, whose keys and values are in buffer B, while the next tile's are brought.
-    uint32_t there_bits = 0;
+    // A step works on tile t, whose keys and values are in buffer B, while the next tile's go from registers into the other buffer and those
+    // of the tile behind it are asked for.
+    uint32_t there_bits = 0, next_there = 0;
     auto step = [&](auto B, int32_t t) {
         constexpr uint32_t buffer = decltype(B)::value;
         constexpr int kProducts = HT * KS, kGroups = 2 * HT, kAhead = DC_AHEAD;
         const int32_t j = tiles.first_token(t);
-        const bool more = t + 1 < t_end;
-        const int32_t next = t + 1 - t_begin;
+        const int32_t next = t + 2 - t_begin;
+        if (t + 1 < t_end) {
+            put_k(buffer ^ 1u);
+            put_v(t + 1, next_there, buffer ^ 1u);
+        }
         if ((next & 15) == 0) {
             pages = pages_ahead, pages_there = __ballot(pages >= 0);
             pages_ahead = pages_from(next + 16);
         }
-        const int32_t next_page = my_page(next);
-        const uint32_t next_there = groups_there(next);
-        if (more) {
-            load(k_new, a.k_pages, t + 1, next_page);
-            load(v_new, a.v_pages, t + 1, next_page);
-        }
+        const uint32_t there_after = groups_there(next);
+        if (t + 2 < t_end) bring(t + 2, my_page(next));
 
         // a wavefront whose rows see nothing of the tile has nothing to do
         if (j < last_sees.high && (j + kTile > first_sees.low || j < last_sees.sinks)) {
@@ -723,7 +728,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
             for (int i = 0; i < kAhead; i++) x[i] = k_operand(i, buffer);
 #pragma unroll
             for (int i = 0; i < kProducts; i++) {
-                s[i / KS] = Mfma<T>::m32(x[i % kAhead], q[i % KS], i % KS ? s[i / KS] : f32x16{});
+                s[i / KS] = Mfma<T>::m32(x[i % kAhead], q[i % KS], i % KS ? s[i / KS] : below);
                 if (i + kAhead < kProducts) x[i % kAhead] = k_operand(i + kAhead, buffer);
             }
             __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
@@ -750,17 +755,19 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
 #pragma unroll
                 for (int i = 0; i < 16; i++) top = fmaxf(top, s[h][i]);
             top = max_over_32(top);
-            // Weights are taken relative to a maximum that moves only when a score is more than a factor of 256 above it: they stay far
-            // inside the range of the type, and what has been added up is scaled now and then, not for every tile.
-            if (__any(top * a.scale > ref + 8.0f || (m == -INFINITY && top != -INFINITY))) {
-                const bool first = m == -INFINITY;
-                m = fmaxf(m, top);
-                const float next = m == -INFINITY ? 0.0f : m * a.scale;
-                const float fade = first ? 0.0f : exp2_of(ref - next);
-                ref = next;
+            // Scores come out of the products less a reference, with which the sums begin.  It moves, to the largest score so far, only when one
+            // is so far above it that its weight would exceed 256: weights stay far inside the range of the type, and what has been added
+            // up is scaled now and then, not for every tile.
+            if (__any(top * a.scale > 8.0f || (!any && top != -INFINITY))) {
+                const float rise = any ? fmaxf(top, 0.0f) : top == -INFINITY ? 0.0f : top;
+                const float fade = any ? exp2_of(-rise * a.scale) : 0.0f;
+                any = any || top != -INFINITY;
                 l *= fade;
 #pragma unroll
                 for (int dt = 0; dt < DT; dt++) o[dt] *= fade;
+#pragma unroll
+                for (int h = 0; h < HT; h++) s[h] -= rise;
+                below -= rise;
             }
             TV w[kGroups];
 #pragma unroll
@@ -770,7 +777,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
                 typedef float f32x8 __attribute__((ext_vector_type(8)));
                 f32x8 e;
 #pragma unroll
-                for (int i = 0; i < 8; i++) e[i] = exp2_of(__builtin_fmaf(s[u / 2][8 * (u % 2) + i], a.scale, -ref));
+                for (int i = 0; i < 8; i++) e[i] = exp2_of(s[u / 2][8 * (u % 2) + i] * a.scale);
                 l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
                 w[u] = __builtin_convertvector(e, TV);
             }
@@ -804,20 +811,16 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
                 }
             }
         }
-        if (more) {
-            put_k(buffer ^ 1u);
-            put_v(t + 1, next_page, is_partial(t + 1, next_there), buffer ^ 1u);
-        }
-        there_bits = next_there;
+        there_bits = next_there, next_there = there_after;
         __syncthreads();
     };
 
     if (t_begin < t_end) {
-        there_bits = groups_there(0);
-        load(k_new, a.k_pages, t_begin, my_page(0));
-        load(v_new, a.v_pages, t_begin, my_page(0));
+        there_bits = groups_there(0), next_there = groups_there(1);
+        bring(t_begin, my_page(0));
         put_k(0);
-        put_v(t_begin, my_page(0), is_partial(t_begin, there_bits), 0);
+        put_v(t_begin, there_bits, 0);
+        if (t_begin + 1 < t_end) bring(t_begin + 1, my_page(1));
     }
     __syncthreads();
     for (int32_t t = t_begin; t < t_end; t += 2) {
@@ -827,8 +830,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
 
     const f32x2 both = swapped32(l);
     const float total = both[0] + both[1];
-    float top = m == -INFINITY ? -INFINITY : ref;
-    if (total != total && top == -INFINITY) top = 0.0f; // saw scores, none of them a number
+    const float top = any || total != total ? -below[0] * a.scale : -INFINITY; // (also if it saw scores and none was a number)
     if (my_row >= n) return;
 #pragma unroll
     for (int dt = 0; dt < DT; dt++)
