@@ -616,22 +616,49 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
     const uint64_t page_stride = (uint64_t)a.n_kv_heads << a.batch.page_shift;
     const uint64_t head_at = (uint64_t)kv << a.batch.page_shift;
     const uint32_t place_mask = (1u << a.batch.page_shift) - 1u;
-    // Pages of 16 tiles, asked for 16 tiles ahead: lane l has that of the tokens that wavefront l mod 4 brings of tile i + l / 4, counted from
-    // t_begin; -1 where there is none.  (Scalar loads would do for what is the same in all lanes, but the LDS's data are waited for by
-    // the same counter, all of it.)
+    // What there is to know of 16 tiles, 16 tiles ahead.  Lane l has the page of the tokens that wavefront l mod 4 brings of tile i + l / 4, counted
+    // from t_begin (-1: not there), and a bit in each of: their being there; the tile being partial, which is to say that not all rows of the
+    // workgroup see all of it; this wavefront's rows seeing some of it; and not all of it.  A tile's step takes its own with a lane's
+    // value and shifts.  (Scalar loads would do for the pages, but the LDS's data are waited for by the same counter, all of it.)
+    struct Known {
+        int32_t page, at;
+        uint64_t there, partial, some, edge;
+    };
     auto pages_from = [&](int32_t i) {
         const int32_t t = t_begin + i + (int32_t)(lane >> 2), j = tiles.first_token(t) + (int32_t)(lane & 3u) * kTokens;
         int32_t e = -1;
         if (t < t_end && j < tiles.high) e = table[(uint32_t)j >> a.batch.page_shift];
         return (uint32_t)e < a.batch.n_pages ? e : -1;
     };
-    int32_t pages = pages_from(0), pages_ahead = pages_from(16);
-    uint64_t pages_there = __ballot(pages >= 0);
-    auto my_page = [&](int32_t i) { return __builtin_amdgcn_readlane(pages, 4 * (i & 15) + (int32_t)wave); };
-    auto groups_there = [&](int32_t i) { return (uint32_t)(pages_there >> (4 * (i & 15))) & 15u; };
+    auto known_from = [&](int32_t i, int32_t page) {
+        Known k;
+        const int32_t j = tiles.first_token(t_begin + i + (int32_t)(lane >> 2));
+        k.page = page;
+        k.at = j;
+        k.there = __ballot(page >= 0);
+        const bool whole = ((uint32_t)(k.there >> (lane & 60u)) & 15u) == 15u;
+        k.partial = __ballot(!whole || j + kTile > all_see_high || j < all_see_low);
+        k.some = __ballot(j < last_sees.high && (j + kTile > first_sees.low || j < last_sees.sinks));
+        k.edge = __ballot(!whole || j + kTile > first_sees.high || (j < last_sees.low && j + kTile > first_sees.sinks));
+        return k;
+    };
+    int32_t pages_ahead = pages_from(0);
+    Known known = known_from(0, pages_ahead);
+    pages_ahead = pages_from(16);
+    // a tile as its step wants it
+    struct Tile {
+        int32_t j;
+        uint32_t there;
+        bool partial, some, edge;
+    };
+    auto tile_of = [&](int32_t i) {
+        const int32_t l = 4 * (i & 15);
+        return Tile{__builtin_amdgcn_readlane(known.at, l), (uint32_t)(known.there >> l) & 15u, (known.partial >> l & 1u) != 0, (known.some >> l & 1u) != 0,
+                    (known.edge >> l & 1u) != 0};
+    };
     u32x4 k_new[kLoads], v_new[kLoads];
-    auto bring = [&](int32_t t, int32_t page) {
-        const int32_t j = tiles.first_token(t) + (int32_t)wave * kTokens;
+    auto bring = [&](int32_t i, const Tile &tile) {
+        const int32_t page = __builtin_amdgcn_readlane(known.page, 4 * (i & 15) + (int32_t)wave), j = tile.j + (int32_t)wave * kTokens;
         const uint64_t at = (page_stride * (uint32_t)max(page, 0) + head_at + ((uint32_t)j & place_mask)) * D + lane * 8;
 #pragma unroll
         for (int i = 0; i < kLoads; i++) k_new[i] = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.k_pages) + at + i * 512);
@@ -663,16 +690,11 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
 #pragma unroll
         for (int i = 0; i < kLoads; i++) *(lds_u32x4 *)(uintptr_t)(lds_k + buffer * kBuffer + put_at[i]) = k_new[i];
     };
-    // tokens that not all rows of the workgroup see, among them those on pages that are not there
-    auto is_partial = [&](int32_t t, uint32_t there_bits) {
-        const int32_t j = tiles.first_token(t);
-        return there_bits != 15u || j + kTile > all_see_high || j < all_see_low;
-    };
     // Of a partial tile a wavefront leaves in lds_odd whether one of the values of V that it brought is no number.
-    auto put_v = [&](int32_t t, uint32_t there_bits, uint32_t buffer) {
-        const bool partial = is_partial(t, there_bits), is_there = (there_bits >> wave & 1u) != 0;
-        if (partial) {
-            const int32_t j = tiles.first_token(t) + (int32_t)wave * kTokens;
+    auto put_v = [&](const Tile &tile, uint32_t buffer) {
+        if (tile.partial) {
+            const bool is_there = (tile.there >> wave & 1u) != 0;
+            const int32_t j = tile.j + (int32_t)wave * kTokens;
             u16x2 most = {};
 #pragma unroll
             for (int i = 0; i < kLoads; i++) {
@@ -702,25 +724,25 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
 
     // A step works on tile t, whose keys and values are in buffer B, while the next tile's go from registers into the other buffer and those
     // of the tile behind it are asked for.
-    uint32_t there_bits = 0, next_there = 0;
+    Tile now = {}, next = {};
     auto step = [&](auto B, int32_t t) {
         constexpr uint32_t buffer = decltype(B)::value;
         constexpr int kProducts = HT * KS, kGroups = 2 * HT, kAhead = DC_AHEAD;
-        const int32_t j = tiles.first_token(t);
-        const int32_t next = t + 2 - t_begin;
+        const int32_t j = now.j;
         if (t + 1 < t_end) {
             put_k(buffer ^ 1u);
-            put_v(t + 1, next_there, buffer ^ 1u);
+            put_v(next, buffer ^ 1u);
         }
-        if ((next & 15) == 0) {
-            pages = pages_ahead, pages_there = __ballot(pages >= 0);
-            pages_ahead = pages_from(next + 16);
+        const int32_t i_after = t + 2 - t_begin;
+        if ((i_after & 15) == 0) {
+            known = known_from(i_after, pages_ahead);
+            pages_ahead = pages_from(i_after + 16);
         }
-        const uint32_t there_after = groups_there(next);
-        if (t + 2 < t_end) bring(t + 2, my_page(next));
+        const Tile after = tile_of(i_after);
+        if (t + 2 < t_end) bring(i_after, after);
 
         // a wavefront whose rows see nothing of the tile has nothing to do
-        if (j < last_sees.high && (j + kTile > first_sees.low || j < last_sees.sinks)) {
+        if (now.some) {
             // The operands come out of the LDS several products ahead of their use.
             f32x16 s[HT];
             TV x[kAhead];
@@ -739,13 +761,13 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
             }
             __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
 
-            if (there_bits != 15u || j + kTile > first_sees.high || (j < last_sees.low && j + kTile > first_sees.sinks)) {
+            if (now.edge) {
 #pragma unroll
                 for (int h = 0; h < HT; h++)
 #pragma unroll
                     for (int i = 0; i < 16; i++) {
                         const int token = 32 * h + 8 * (i / 4) + i % 4; // of the lower half; the upper half's is 4 further, brought by the same wavefront
-                        const bool sees = seen.token(j + token + 4 * (int32_t)half) & ((there_bits >> (token / kTokens) & 1u) != 0);
+                        const bool sees = seen.token(j + token + 4 * (int32_t)half) & ((now.there >> (token / kTokens) & 1u) != 0);
                         s[h][i] = sees ? s[h][i] : -INFINITY;
                     }
             }
@@ -789,7 +811,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
             dcdev::in_register<false>(l); // the additions among the products, not behind them
             DC_SCHED
             uint32_t odd_bits = 0;
-            if (is_partial(t, there_bits)) {
+            if (now.partial) {
 #pragma unroll
                 for (int i = 0; i < 4; i++) odd_bits |= __builtin_amdgcn_readfirstlane(lds_odd[buffer][i]) << i;
             }
@@ -811,16 +833,16 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
                 }
             }
         }
-        there_bits = next_there, next_there = there_after;
+        now = next, next = after;
         __syncthreads();
     };
 
     if (t_begin < t_end) {
-        there_bits = groups_there(0), next_there = groups_there(1);
-        bring(t_begin, my_page(0));
+        now = tile_of(0), next = tile_of(1);
+        bring(0, now);
         put_k(0);
-        put_v(t_begin, there_bits, 0);
-        if (t_begin + 1 < t_end) bring(t_begin + 1, my_page(1));
+        put_v(now, 0);
+        if (t_begin + 1 < t_end) bring(1, next);
     }
     __syncthreads();
     for (int32_t t = t_begin; t < t_end; t += 2) {
