@@ -185,21 +185,24 @@ template <typename T, int D> __device__ __forceinline__ void store_result(const 
 // first operand, 8 tokens of one value, comes out of the LDS through the transposing read.  So maxima, sums and the scaling of
 // what has been added up stay inside a lane but for two exchanges a tile.  K and then V go through registers into the wavefront's
 // own part of the LDS: no barrier in the loop.  The next tile's loads are under way during the rest of the tile's work.
-template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void dc_attention_few_kernel(AttentionArgs a)
+template <int D, int RT> struct FewLds {
+    static constexpr int kPadded = D + 4; // floats of a row's sums
+    union {
+        uint8_t tokens[4][32 * 2 * D]; // of each wavefront: a tile's keys, then its values
+        float sums[4][16][kPadded];
+    };
+    float m[4][16 * RT], l[4][16 * RT];
+    int32_t p[16 * RT];
+};
+
+template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(const AttentionArgs &a, FewLds<D, RT> &lds, bool common, uint32_t item)
 {
     typedef typename Vec8<T>::type TV;
     constexpr int kTile = 32, KS = D / 32, DT = D / 16;
     constexpr int kRowBytes = 2 * D, kChunks = D / 8, kRowsALoad = 64 / kChunks, kLoads = kTile / kRowsALoad;
-    constexpr int kPadded = D + 4;
-    constexpr int kLdsV = 4 * kTile * kRowBytes, kLdsO = 4 * 16 * kPadded * 4;
-    __shared__ __align__(16) uint8_t lds[kLdsV > kLdsO ? kLdsV : kLdsO];
-    __shared__ float lds_m[4][16 * RT], lds_l[4][16 * RT];
-    __shared__ int32_t lds_p[16 * RT];
 
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15u, g = lane >> 4;
-    const bool common = blockIdx.x < a.prefix.blocks;
-    const Part part = common ? a.prefix : a.own;
-    uint32_t item = common ? blockIdx.x : blockIdx.x - a.prefix.blocks;
+    const Part &part = common ? a.prefix : a.own;
     const uint32_t kv = item % a.n_kv_heads;
     item /= a.n_kv_heads;
     const uint32_t seq = common ? 0 : item % a.batch.n_seqs, split = common ? item : item / a.batch.n_seqs;
@@ -225,16 +228,16 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
         n = a.batch.n_rows * a.group;
         there = (int32_t)a.batch.prefix_len;
         // positions of the rows, sequence by sequence
-        if (threadIdx.x < 16 * RT) lds_p[threadIdx.x] = kNoPosition;
+        if (threadIdx.x < 16 * RT) lds.p[threadIdx.x] = kNoPosition;
         __syncthreads();
         for (uint32_t b = threadIdx.x; b < a.batch.n_seqs; b += 256) {
             const uint32_t first = a.batch.first_row(b), end = a.batch.rows_end(b);
-            for (uint32_t r = first; r < end; r++) lds_p[r] = a.batch.length(b) - (int32_t)(end - r);
+            for (uint32_t r = first; r < end; r++) lds.p[r] = a.batch.length(b) - (int32_t)(end - r);
         }
         __syncthreads();
         p_min = 0x7FFFFFFF, p_max = kNoPosition;
         for (uint32_t r = 0; r < a.batch.n_rows; r++) {
-            const int32_t p = lds_p[r];
+            const int32_t p = lds.p[r];
             if (p != kNoPosition) p_min = min(p_min, p), p_max = max(p_max, p);
         }
         p_min = min(p_min, p_max);
@@ -262,7 +265,7 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
         const uint32_t r = rt * 16 + c;
         const bool is = r < n;
         const uint32_t i = r / a.group, head = kv * a.group + r % a.group;
-        seen[rt] = Seen(!is ? kNoPosition : common ? lds_p[i] : p_first + (int32_t)i - base, there, a.window, (int64_t)a.sinks - base);
+        seen[rt] = Seen(!is ? kNoPosition : common ? lds.p[i] : p_first + (int32_t)i - base, there, a.window, (int64_t)a.sinks - base);
         const T *src = static_cast<const T *>(a.q) + (uint64_t)(row_first + i) * a.q_row + head * a.q_head + 8 * g;
 #pragma unroll
         for (int s = 0; s < KS; s++) {
@@ -311,7 +314,7 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
     };
     // Tokens lie in the LDS with their 16-byte chunks exchanged so that 8 tokens' same chunks, and pairs of chunks, are on different banks.
     auto swizzle = [](uint32_t row) { return D == 64 ? ((row >> 1) & 3u) << 1 : (row & 7u) << 1; };
-    const uint32_t my_lds = dcdev::lds_address(lds) + wave * (kTile * kRowBytes);
+    const uint32_t my_lds = dcdev::lds_address(lds.tokens[wave]);
     auto put = [&](const u32x4 (&from)[kLoads]) {
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
@@ -438,54 +441,44 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
         l[rt] = sum_over_16(l[rt]);
         m[rt] *= a.scale;
         if (l[rt] != l[rt] && m[rt] == -INFINITY) m[rt] = 0.0f; // saw scores, none of them a number
-        if (g == 0) lds_m[wave][rt * 16 + c] = m[rt], lds_l[wave][rt * 16 + c] = l[rt];
+        if (g == 0) lds.m[wave][rt * 16 + c] = m[rt], lds.l[wave][rt * 16 + c] = l[rt];
     }
     __syncthreads();
-    float *sums = reinterpret_cast<float *>(lds);
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) {
         const uint32_t r = rt * 16 + c;
-        const float top = fmaxf(fmaxf(lds_m[0][r], lds_m[1][r]), fmaxf(lds_m[2][r], lds_m[3][r]));
+        const float top = fmaxf(fmaxf(lds.m[0][r], lds.m[1][r]), fmaxf(lds.m[2][r], lds.m[3][r]));
         const float f = m[rt] == -INFINITY ? 0.0f : exp2_of(m[rt] - top);
         if (rt) __syncthreads();
 #pragma unroll
         for (int dt = 0; dt < DT; dt++)
-            *reinterpret_cast<f32x4 *>(&sums[(wave * 16 + c) * kPadded + 16 * dt + 4 * g]) = m[rt] == -INFINITY ? f32x4{} : o[rt][dt] * f;
+            *reinterpret_cast<f32x4 *>(&lds.sums[wave][c][16 * dt + 4 * g]) = m[rt] == -INFINITY ? f32x4{} : o[rt][dt] * f;
         __syncthreads();
         constexpr uint32_t kQuads = D / 4;
         for (uint32_t i = threadIdx.x; i < 16 * kQuads; i += 256) {
             const uint32_t col = i / kQuads, at = i % kQuads * 4, rr = rt * 16 + col;
             if (rr >= n) continue;
-            const float big = fmaxf(fmaxf(lds_m[0][rr], lds_m[1][rr]), fmaxf(lds_m[2][rr], lds_m[3][rr]));
+            const float big = fmaxf(fmaxf(lds.m[0][rr], lds.m[1][rr]), fmaxf(lds.m[2][rr], lds.m[3][rr]));
             f32x4 sum = {};
             float total = 0.0f;
 #pragma unroll
             for (int w4 = 0; w4 < 4; w4++) {
-                sum += *reinterpret_cast<const f32x4 *>(&sums[(w4 * 16 + col) * kPadded + at]);
-                if (lds_m[w4][rr] != -INFINITY) total += lds_l[w4][rr] * exp2_of(lds_m[w4][rr] - big);
+                sum += *reinterpret_cast<const f32x4 *>(&lds.sums[w4][col][at]);
+                if (lds.m[w4][rr] != -INFINITY) total += lds.l[w4][rr] * exp2_of(lds.m[w4][rr] - big);
             }
             store_result<T, D>(a, row_first + rr / a.group, kv * a.group + rr % a.group, part.first_slot + split, at, sum, big, total);
         }
     }
 }
 
-#ifndef DC_AHEAD
-#define DC_AHEAD 6
-#endif
-#ifndef DC_KT
-#define DC_KT 64
-#endif
-#ifndef DC_TLB64
-#define DC_TLB64 3
-#endif
-#ifndef DC_TLB
-#define DC_TLB 2
-#endif
-#ifdef SCHED1
-#define DC_SCHED { __builtin_amdgcn_sched_group_barrier(0x100, 2*kAhead, 0); __builtin_amdgcn_sched_group_barrier(0x002, 28, 0); _Pragma("unroll") for (int i = 0; i < kGroups*DT; i++) { __builtin_amdgcn_sched_group_barrier(0x008, 1, 0); if (i + kAhead < kGroups*DT) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0); __builtin_amdgcn_sched_group_barrier(0x002, D == 64 ? 12 : 6, 0); } }
-#else
-#define DC_SCHED
-#endif
+template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void dc_attention_few_kernel(AttentionArgs a)
+{
+    __shared__ __align__(16) FewLds<D, RT> lds;
+    const bool common = blockIdx.x < a.prefix.blocks;
+    few_rows<T, D, RT>(a, lds, common, common ? blockIdx.x : blockIdx.x - a.prefix.blocks);
+}
+
+
 constexpr uint32_t kTileRows = 128; // of a workgroup of the kernel for many rows
 
 // ---- many rows ------------------------------------------------------------------------------------------------------------
@@ -495,21 +488,24 @@ constexpr uint32_t kTileRows = 128; // of a workgroup of the kernel for many row
 // tile; a wavefront owns 32 rows.  The products are those of the kernel for few rows in the 32x32x16 shape: scores as [token][row]
 // = K Q^T, of which a lane holds 16 of 32 tokens of one row, results as [head_dim][row] = V^T P^T; maxima and sums stay in a lane but for one
 // exchange between the halves.
-template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 ? DC_TLB64 : DC_TLB) void dc_attention_tile_kernel(AttentionArgs a)
+template <int D> struct TileLds {
+    static constexpr int kTile = D == 256 ? 32 : 64; // tokens
+    uint8_t k[2][kTile * 2 * D], v[2][kTile * 2 * D];
+    int32_t p[kTileRows];
+    uint32_t odd[2][4];
+};
+
+template <typename T, int D> __device__ __forceinline__ void many_rows(const AttentionArgs &a, TileLds<D> &lds, bool common, uint32_t block)
 {
     typedef typename Vec8<T>::type TV;
-    constexpr int kTile = D == 256 ? 32 : DC_KT, KS = D / 16, DT = D / 32, HT = kTile / 32; // HT: 32-token products of a tile
+    constexpr int kTile = TileLds<D>::kTile, KS = D / 16, DT = D / 32, HT = kTile / 32; // HT: 32-token products of a tile
     constexpr uint32_t kRows = kTileRows, kRowBytes = 2 * D, kChunks = D / 8, kRowsALoad = 64 / kChunks;
     constexpr int kTokens = kTile / 4, kLoads = kTokens / (int)kRowsALoad; // tokens that a wavefront brings, in so many loads
     constexpr uint32_t kBuffer = kTile * kRowBytes;
-    __shared__ __align__(16) uint8_t lds[4 * kBuffer]; // K, K, V, V
-    __shared__ int32_t lds_p[kRows];
-    __shared__ __align__(16) uint32_t lds_odd[2][4];
 
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31u, half = lane >> 5;
-    const bool common = blockIdx.x < a.prefix.blocks;
-    const Part part = common ? a.prefix : a.own;
-    uint32_t item = part.blocks - 1 - (common ? blockIdx.x : blockIdx.x - a.prefix.blocks); // the last rows, which see most, first
+    const Part &part = common ? a.prefix : a.own;
+    uint32_t item = part.blocks - 1 - block; // the last rows, which see most, first
     const uint32_t kv = a.n_kv_heads - 1 - item % a.n_kv_heads;
     item /= a.n_kv_heads;
     const uint32_t split = part.n_splits - 1 - item % part.n_splits;
@@ -560,24 +556,24 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
 
     // positions of the rows, counted from the part's first token
     if (common) {
-        for (uint32_t i = threadIdx.x; i < kRows; i += 256) lds_p[i] = kNoPosition;
+        for (uint32_t i = threadIdx.x; i < kRows; i += 256) lds.p[i] = kNoPosition;
         __syncthreads();
         const uint32_t r_low = i_first / a.group, r_high = min((i_first + kRows - 1) / a.group + 1, a.batch.n_rows);
         for (uint32_t b = threadIdx.x; b < a.batch.n_seqs; b += 256) {
             const uint32_t first = a.batch.first_row(b), end = a.batch.rows_end(b);
             const int32_t len = first < end ? a.batch.length(b) : 0;
             for (uint32_t r = max(first, r_low); r < min(end, r_high); r++)
-                for (uint32_t i = max(r * a.group, i_first); i < min((r + 1) * a.group, i_first + kRows); i++) lds_p[i - i_first] = len - (int32_t)(end - r);
+                for (uint32_t i = max(r * a.group, i_first); i < min((r + 1) * a.group, i_first + kRows); i++) lds.p[i - i_first] = len - (int32_t)(end - r);
         }
     } else {
         const int32_t p_first = a.batch.length(seq) - (int32_t)(a.batch.rows_end(seq) - row_first) - base;
-        for (uint32_t i = threadIdx.x; i < kRows; i += 256) lds_p[i] = i_first + i < n ? p_first + (int32_t)((i_first + i) / a.group) : kNoPosition;
+        for (uint32_t i = threadIdx.x; i < kRows; i += 256) lds.p[i] = i_first + i < n ? p_first + (int32_t)((i_first + i) / a.group) : kNoPosition;
     }
     __syncthreads();
     auto smallest_largest = [&](uint32_t first, uint32_t count, int32_t &low, int32_t &high) {
         low = 0x7FFFFFFF, high = kNoPosition;
         for (uint32_t i = lane; i < count; i += 64) {
-            const int32_t p = lds_p[first + i];
+            const int32_t p = lds.p[first + i];
             if (p != kNoPosition) low = min(low, p), high = max(high, p);
         }
 #pragma unroll
@@ -596,7 +592,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
 
     const uint32_t my_row = i_first + wave * 32 + c, my_head = kv * a.group + my_row % a.group;
     const uint64_t my_packed = row_first + my_row / a.group;
-    const Seen seen(lds_p[wave * 32 + c], there, a.window, sinks_left);
+    const Seen seen(lds.p[wave * 32 + c], there, a.window, sinks_left);
     TV q[KS];
     f32x16 o[DT];
     f32x16 below = f32x16{}; // the reference with the other sign, in every value
@@ -669,7 +665,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
     auto swizzle = [](uint32_t token) {
         return D == 64 ? (token >> 1 & 1u) << 2 | (token >> 2 & 3u) : (token & 3u) << 2 | (token >> 2 & 3u);
     };
-    const uint32_t lds_k = dcdev::lds_address(lds), lds_v = lds_k + 2 * kBuffer;
+    const uint32_t lds_k = dcdev::lds_address(lds.k), lds_v = dcdev::lds_address(lds.v);
     // where a lane puts what it brings, and where it reads its part of the first operands
     uint32_t put_at[kLoads], k_at[KS], v_at[DT][2];
 #pragma unroll
@@ -690,7 +686,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
 #pragma unroll
         for (int i = 0; i < kLoads; i++) *(lds_u32x4 *)(uintptr_t)(lds_k + buffer * kBuffer + put_at[i]) = k_new[i];
     };
-    // Of a partial tile a wavefront leaves in lds_odd whether one of the values of V that it brought is no number.
+    // Of a partial tile a wavefront leaves in lds.odd whether one of the values of V that it brought is no number.
     auto put_v = [&](const Tile &tile, uint32_t buffer) {
         if (tile.partial) {
             const bool is_there = (tile.there >> wave & 1u) != 0;
@@ -708,7 +704,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
 #pragma unroll
                 for (int i = 0; i < kLoads; i++) v_new[i] = without_odd<T>(v_new[i]);
             }
-            if (lane == 0) lds_odd[buffer][wave] = odd;
+            if (lane == 0) lds.odd[buffer][wave] = odd;
         }
 #pragma unroll
         for (int i = 0; i < kLoads; i++) *(lds_u32x4 *)(uintptr_t)(lds_v + buffer * kBuffer + put_at[i]) = v_new[i];
@@ -727,7 +723,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
     Tile now = {}, next = {};
     auto step = [&](auto B, int32_t t) {
         constexpr uint32_t buffer = decltype(B)::value;
-        constexpr int kProducts = HT * KS, kGroups = 2 * HT, kAhead = DC_AHEAD;
+        constexpr int kProducts = HT * KS, kGroups = 2 * HT, kAhead = 6;
         const int32_t j = now.j;
         if (t + 1 < t_end) {
             put_k(buffer ^ 1u);
@@ -809,11 +805,10 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
                 if (i + kAhead < kGroups * DT) x[i % kAhead] = v_operand(i + kAhead, buffer);
             }
             dcdev::in_register<false>(l); // the additions among the products, not behind them
-            DC_SCHED
             uint32_t odd_bits = 0;
             if (now.partial) {
 #pragma unroll
-                for (int i = 0; i < 4; i++) odd_bits |= __builtin_amdgcn_readfirstlane(lds_odd[buffer][i]) << i;
+                for (int i = 0; i < 4; i++) odd_bits |= __builtin_amdgcn_readfirstlane(lds.odd[buffer][i]) << i;
             }
             if (odd_bits) {
 #pragma unroll 1
@@ -861,6 +856,34 @@ template <typename T, int D> __global__ __launch_bounds__(256, D == 256 ? 1 : D 
             const f32x4 v = {o[dt][4 * b], o[dt][4 * b + 1], o[dt][4 * b + 2], o[dt][4 * b + 3]};
             store_result<T, D>(a, (uint32_t)my_packed, my_head, part.first_slot + split, 32 * dt + 8 * b + 4 * half, v, top, total);
         }
+}
+
+template <int D> constexpr int workgroups_a_unit() { return D == 256 ? 1 : D == 64 ? 3 : 2; }
+template <typename T, int D> __global__ __launch_bounds__(256, workgroups_a_unit<D>()) void dc_attention_tile_kernel(AttentionArgs a)
+{
+    __shared__ __align__(16) TileLds<D> lds;
+    const bool common = blockIdx.x < a.prefix.blocks;
+    many_rows<T, D>(a, lds, common, common ? blockIdx.x : blockIdx.x - a.prefix.blocks);
+}
+
+// A common prefix with many rows and few rows in each sequence: the first is bound by the matrix units, the second by memory, and the two
+// kinds of workgroups lie in one launch in turn, so that a compute unit has some of each (64 sequences behind 16384 tokens: 67 us instead of 72
+// in two launches).
+// In turn by eights: a workgroup's XCD is its number modulo 8, and those of one key/value head's prefix stay on one.
+template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void dc_attention_both_kernel(AttentionArgs a)
+{
+    __shared__ __align__(16) union {
+        FewLds<D, RT> few;
+        TileLds<D> many;
+    } lds;
+    const uint32_t eight = blockIdx.x >> 3, prefix_eights = (a.prefix.blocks + 7) / 8, own_eights = (a.own.blocks + 7) / 8, less = min(prefix_eights, own_eights);
+    const bool common = eight < 2 * less ? (eight & 1u) == 0 : prefix_eights > own_eights;
+    const uint32_t block = (eight < 2 * less ? eight / 2 : eight - less) * 8 + (blockIdx.x & 7u);
+    if (common) {
+        if (block < a.prefix.blocks) many_rows<T, D>(a, lds.many, true, block);
+    } else {
+        if (block < a.own.blocks) few_rows<T, D, RT>(a, lds.few, false, block);
+    }
 }
 
 // Joins the splits of a row and head: each has its sums relative to a maximum of its own.  The weights of the splits first, into the LDS; then
@@ -919,7 +942,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void dc_attention
 // Which kernel works through a part: that for at most 16 rows or 32 rows, or that for many.
 enum Kind { kFew16 = 0, kFew32 = 1, kTile = 2 };
 struct Plan {
-    int prefix_kind, own_kind;
+    Kind prefix_kind, own_kind;
 };
 
 bool attention_ok(const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_attention *t)
@@ -934,21 +957,20 @@ bool attention_ok(const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_a
 
 template <typename T, int D> void launch(const AttentionArgs &a, const Plan &plan, hipStream_t stream)
 {
-    // a launch for the parts of a kind
-    for (int kind = 0; kind < 3; kind++) {
-        AttentionArgs b = a;
-        if (plan.prefix_kind != kind) b.prefix.blocks = 0;
-        if (plan.own_kind != kind) b.own.blocks = 0;
-        const dim3 grid(b.prefix.blocks + b.own.blocks);
-        if (grid.x == 0) continue;
-        if (kind == kFew16) hipLaunchKernelGGL((dc_attention_few_kernel<T, D, 1>), grid, dim3(256), 0, stream, b);
-        if constexpr (D < 256) {
-            if (kind == kFew32) hipLaunchKernelGGL((dc_attention_few_kernel<T, D, 2>), grid, dim3(256), 0, stream, b);
-        }
-        if (kind == kTile) hipLaunchKernelGGL((dc_attention_tile_kernel<T, D>), grid, dim3(256), 0, stream, b);
+    const dim3 threads(256);
+    if (a.prefix.blocks && plan.prefix_kind == kTile && plan.own_kind != kTile) {
+        const dim3 grid(8 * ((a.prefix.blocks + 7) / 8 + (a.own.blocks + 7) / 8));
+        if (plan.own_kind == kFew16) hipLaunchKernelGGL((dc_attention_both_kernel<T, D, 1>), grid, threads, 0, stream, a);
+        else if constexpr (D < 256) hipLaunchKernelGGL((dc_attention_both_kernel<T, D, 2>), grid, threads, 0, stream, a);
+    } else { // a sequence's rows are never more than the batch's: both parts are of the kind of their rows together, or the prefix is alone
+        const Kind kind = a.prefix.blocks ? std::max(plan.prefix_kind, plan.own_kind) : plan.own_kind;
+        const dim3 grid(a.prefix.blocks + a.own.blocks);
+        if (kind == kFew16) hipLaunchKernelGGL((dc_attention_few_kernel<T, D, 1>), grid, threads, 0, stream, a);
+        else if (kind == kTile) hipLaunchKernelGGL((dc_attention_tile_kernel<T, D>), grid, threads, 0, stream, a);
+        else if constexpr (D < 256) hipLaunchKernelGGL((dc_attention_few_kernel<T, D, 2>), grid, threads, 0, stream, a);
     }
     if (a.n_slots > 1)
-        hipLaunchKernelGGL((dc_attention_join_kernel<T, D>), dim3(a.batch.n_rows, a.n_heads), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((dc_attention_join_kernel<T, D>), dim3(a.batch.n_rows, a.n_heads), threads, 0, stream, a);
 }
 
 template <typename T> void launch_d(const AttentionArgs &a, const Plan &plan, uint32_t head_dim, hipStream_t stream)
@@ -964,14 +986,17 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     *workspace_bytes = 0;
     const uint32_t group = t->n_heads / cache->n_kv_heads, d = cache->head_dim;
     auto kind_of = [&](uint64_t rows) { return rows <= 16 ? kFew16 : rows <= 32 && d < 256 ? kFew32 : kTile; };
+    const uint64_t all_rows = (uint64_t)batch->n_rows * group;
+    const Kind prefix_kind = kind_of(all_rows), own_kind = kind_of((uint64_t)batch->max_new * group);
     // items: workgroups that a part has uncut
     auto cut = [&](Kind kind, uint64_t items, uint64_t tokens, uint32_t first_slot) {
-        const uint64_t tile = kind == kTile && d < 256 ? DC_KT : 32, least = kind == kTile ? 8 : 4;
+        const uint64_t tile = kind == kTile && d < 256 ? 64 : 32, least = kind == kTile ? 8 : 4;
         const uint64_t n_tiles = (tokens + tile - 1) / tile, most = std::max<uint64_t>(1, std::min<uint64_t>((n_tiles + least - 1) / least, kMostSlots / 2));
         uint64_t n = 1;
         if (kind == kTile) {
-            // two workgroups on each of 256 compute units
-            n = std::min((512 + items - 1) / items, most);
+            // two workgroups on each of 256 compute units, or one beside the others' (64 sequences behind 16384 tokens: 62 us with 256, 67 with 512)
+            const uint64_t blocks = first_slot == 0 && batch->prefix_len && own_kind != kTile ? 256 : 512;
+            n = std::min((blocks + items - 1) / items, most);
         } else {
             // As few workgroups as give every compute unit the same number, to a tenth: a long run of keys is read faster by one workgroup
             // (256 of 8 heads' and 32 sequences' runs of 8000 tokens: 161 us, 512 halves of them 168, 1024 quarters 176), but an uneven number
@@ -987,8 +1012,6 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     uint64_t own = batch->max_len > batch->prefix_len ? batch->max_len - batch->prefix_len : 1;
     uint64_t common = batch->prefix_len;
     if (t->window) own = std::min(own, (uint64_t)t->window + batch->max_new + t->sinks + 128);
-    const uint64_t all_rows = (uint64_t)batch->n_rows * group;
-    const Kind prefix_kind = kind_of(all_rows), own_kind = kind_of((uint64_t)batch->max_new * group);
     plan = Plan{prefix_kind, own_kind};
     if (common) {
         a.prefix = cut(prefix_kind, cache->n_kv_heads * (prefix_kind == kTile ? (all_rows + kTileRows - 1) / kTileRows : 1), common, 0);
