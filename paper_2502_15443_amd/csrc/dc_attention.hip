@@ -42,6 +42,7 @@ struct AttentionArgs {
     uint32_t n_heads, n_kv_heads, group, window, sinks, max_new, n_slots;
     float scale;       // not negative; with `negate` of queries that are taken with the other sign
     bool negate, zero; // scale 0: queries are taken as zeros and scale is 1
+    bool whole;        // the prefix is read with the sequences' own pages, not as a part of its own
     Part prefix, own;
 };
 
@@ -513,10 +514,9 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
 
     // rows of this workgroup: i_first <= i < n of the sequence's (the batch's) rows, row_first + i / group of head kv * group + i % group
     uint32_t row_first = 0, n, seq = 0;
-    int32_t there, base = 0;
+    int32_t there = (int32_t)a.batch.prefix_len; // positions below it are, or may be, in the cache
     if (common) {
         n = a.batch.n_rows * a.group;
-        there = (int32_t)a.batch.prefix_len;
     } else {
         bool found = false;
         n = 0;
@@ -548,13 +548,11 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
         seq = __builtin_amdgcn_readfirstlane(seq), tile = __builtin_amdgcn_readfirstlane(tile);
         row_first = a.batch.first_row(seq);
         n = min(a.batch.rows_end(seq) - row_first, a.max_new) * a.group;
-        base = (int32_t)a.batch.prefix_len;
-        there = min(max(a.batch.length(seq) - base, 0), (int32_t)(a.batch.pages_stride << a.batch.page_shift));
+        there = max(there, min(a.batch.length(seq), a.batch.capacity()));
     }
     const uint32_t i_first = tile * kRows;
-    const int32_t *table = common ? a.batch.prefix_pages : a.batch.pages + (uint64_t)seq * a.batch.pages_stride;
 
-    // positions of the rows, counted from the part's first token
+    // positions of the rows
     if (common) {
         for (uint32_t i = threadIdx.x; i < kRows; i += 256) lds.p[i] = kNoPosition;
         __syncthreads();
@@ -566,7 +564,7 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
                 for (uint32_t i = max(r * a.group, i_first); i < min((r + 1) * a.group, i_first + kRows); i++) lds.p[i - i_first] = len - (int32_t)(end - r);
         }
     } else {
-        const int32_t p_first = a.batch.length(seq) - (int32_t)(a.batch.rows_end(seq) - row_first) - base;
+        const int32_t p_first = a.batch.length(seq) - (int32_t)(a.batch.rows_end(seq) - row_first);
         for (uint32_t i = threadIdx.x; i < kRows; i += 256) lds.p[i] = i_first + i < n ? p_first + (int32_t)((i_first + i) / a.group) : kNoPosition;
     }
     __syncthreads();
@@ -580,19 +578,25 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
         for (int i = 1; i < 64; i <<= 1) low = min(low, __shfl_xor(low, i)), high = max(high, __shfl_xor(high, i));
         low = __builtin_amdgcn_readfirstlane(min(low, high)), high = __builtin_amdgcn_readfirstlane(high);
     };
-    const int64_t sinks_left = (int64_t)a.sinks - base;
     int32_t p_min, p_max;
     smallest_largest(0, kRows, p_min, p_max);
-    const Tiles<kTile> tiles(p_min, p_max, there, a.window, sinks_left);
-    const int32_t t_begin = (int32_t)min((uint64_t)split * part.chunk, (uint64_t)tiles.count);
-    const int32_t t_end = split + 1 == part.n_splits ? tiles.count : (int32_t)min((uint64_t)t_begin + part.chunk, (uint64_t)tiles.count);
-    const int32_t all_see_high = Seen(p_min, there, a.window, sinks_left).high, all_see_low = Seen(p_max, there, a.window, sinks_left).low;
+    // The tiles of the common prefix, if it is this launch's to read here, and behind them those of the sequence's own pages, whose first token
+    // is at `base`.  Positions count from the sequence's first token, but in the two tables of pages.
+    const int32_t base = (int32_t)a.batch.prefix_len;
+    auto beyond = [&](int32_t p) { return (int32_t)max((int64_t)p - base, (int64_t)-1); };
+    const Tiles<kTile> prefix_tiles(p_min, p_max, common || a.whole ? base : 0, a.window, a.sinks);
+    const Tiles<kTile> own_tiles(beyond(p_min), beyond(p_max), common ? 0 : there - base, a.window, (int64_t)a.sinks - base);
+    const int32_t count = prefix_tiles.count + own_tiles.count;
+    const int32_t t_begin = (int32_t)min((uint64_t)split * part.chunk, (uint64_t)count);
+    const int32_t t_end = split + 1 == part.n_splits ? count : (int32_t)min((uint64_t)t_begin + part.chunk, (uint64_t)count);
+    auto first_token = [&](int32_t t) { return t < prefix_tiles.count ? prefix_tiles.first_token(t) : base + own_tiles.first_token(t - prefix_tiles.count); };
+    const Seen all_first(p_min, there, a.window, a.sinks), all_last(p_max, there, a.window, a.sinks); // of the workgroup's rows
     smallest_largest(wave * 32, 32, p_min, p_max);
-    const Seen first_sees(p_min, there, a.window, sinks_left), last_sees(p_max, there, a.window, sinks_left);
+    const Seen first_sees(p_min, there, a.window, a.sinks), last_sees(p_max, there, a.window, a.sinks); // of the wavefront's
 
     const uint32_t my_row = i_first + wave * 32 + c, my_head = kv * a.group + my_row % a.group;
     const uint64_t my_packed = row_first + my_row / a.group;
-    const Seen seen(lds.p[wave * 32 + c], there, a.window, sinks_left);
+    const Seen seen(lds.p[wave * 32 + c], there, a.window, a.sinks);
     TV q[KS];
     f32x16 o[DT];
     f32x16 below = f32x16{}; // the reference with the other sign, in every value
@@ -609,6 +613,7 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
 #pragma unroll
     for (int dt = 0; dt < DT; dt++) o[dt] = f32x16{};
 
+    const int32_t *prefix_table = a.batch.prefix_pages, *own_table = a.batch.pages + (uint64_t)seq * a.batch.pages_stride;
     const uint64_t page_stride = (uint64_t)a.n_kv_heads << a.batch.page_shift;
     const uint64_t head_at = (uint64_t)kv << a.batch.page_shift;
     const uint32_t place_mask = (1u << a.batch.page_shift) - 1u;
@@ -617,23 +622,26 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
     // workgroup see all of it; this wavefront's rows seeing some of it; and not all of it.  A tile's step takes its own with a lane's
     // value and shifts.  (Scalar loads would do for the pages, but the LDS's data are waited for by the same counter, all of it.)
     struct Known {
-        int32_t page, at;
-        uint64_t there, partial, some, edge;
+        int32_t page, at, place; // place: of the lane's wavefront's tokens in their page
+        uint64_t there, prefix, partial, some, edge;
     };
     auto pages_from = [&](int32_t i) {
-        const int32_t t = t_begin + i + (int32_t)(lane >> 2), j = tiles.first_token(t) + (int32_t)(lane & 3u) * kTokens;
+        const int32_t t = t_begin + i + (int32_t)(lane >> 2), j = first_token(t) + (int32_t)(lane & 3u) * kTokens;
+        const bool in_prefix = t < prefix_tiles.count;
         int32_t e = -1;
-        if (t < t_end && j < tiles.high) e = table[(uint32_t)j >> a.batch.page_shift];
+        if (t < t_end && j < (in_prefix ? base : all_last.high)) e = in_prefix ? prefix_table[(uint32_t)j >> a.batch.page_shift] : own_table[(uint32_t)(j - base) >> a.batch.page_shift];
         return (uint32_t)e < a.batch.n_pages ? e : -1;
     };
     auto known_from = [&](int32_t i, int32_t page) {
         Known k;
-        const int32_t j = tiles.first_token(t_begin + i + (int32_t)(lane >> 2));
+        const int32_t t = t_begin + i + (int32_t)(lane >> 2), j = first_token(t);
         k.page = page;
         k.at = j;
+        k.place = (int32_t)((uint32_t)(j + (int32_t)(lane & 3u) * kTokens - (t < prefix_tiles.count ? 0 : base)) & place_mask);
         k.there = __ballot(page >= 0);
-        const bool whole = ((uint32_t)(k.there >> (lane & 60u)) & 15u) == 15u;
-        k.partial = __ballot(!whole || j + kTile > all_see_high || j < all_see_low);
+        k.prefix = __ballot(t < prefix_tiles.count);
+        const bool whole = ((uint32_t)(k.there >> (lane & 60u)) & 15u) == 15u && (t >= prefix_tiles.count || j + kTile <= base);
+        k.partial = __ballot(!whole || j + kTile > all_first.high || j < all_last.low);
         k.some = __ballot(j < last_sees.high && (j + kTile > first_sees.low || j < last_sees.sinks));
         k.edge = __ballot(!whole || j + kTile > first_sees.high || (j < last_sees.low && j + kTile > first_sees.sinks));
         return k;
@@ -645,17 +653,18 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
     struct Tile {
         int32_t j;
         uint32_t there;
-        bool partial, some, edge;
+        bool prefix, partial, some, edge;
     };
+    // tokens from here on are not of the tile's table
+    auto end_of = [&](const Tile &tile) { return tile.prefix ? base : 0x7FFFFFFF; };
     auto tile_of = [&](int32_t i) {
         const int32_t l = 4 * (i & 15);
-        return Tile{__builtin_amdgcn_readlane(known.at, l), (uint32_t)(known.there >> l) & 15u, (known.partial >> l & 1u) != 0, (known.some >> l & 1u) != 0,
-                    (known.edge >> l & 1u) != 0};
+        return Tile{__builtin_amdgcn_readlane(known.at, l), (uint32_t)(known.there >> l) & 15u, (known.prefix >> l & 1u) != 0, (known.partial >> l & 1u) != 0, (known.some >> l & 1u) != 0, (known.edge >> l & 1u) != 0};
     };
     u32x4 k_new[kLoads], v_new[kLoads];
-    auto bring = [&](int32_t i, const Tile &tile) {
-        const int32_t page = __builtin_amdgcn_readlane(known.page, 4 * (i & 15) + (int32_t)wave), j = tile.j + (int32_t)wave * kTokens;
-        const uint64_t at = (page_stride * (uint32_t)max(page, 0) + head_at + ((uint32_t)j & place_mask)) * D + lane * 8;
+    auto bring = [&](int32_t i) {
+        const int32_t l = 4 * (i & 15) + (int32_t)wave, page = __builtin_amdgcn_readlane(known.page, l);
+        const uint64_t at = (page_stride * (uint32_t)max(page, 0) + head_at + (uint32_t)__builtin_amdgcn_readlane(known.place, l)) * D + lane * 8;
 #pragma unroll
         for (int i = 0; i < kLoads; i++) k_new[i] = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.k_pages) + at + i * 512);
 #pragma unroll
@@ -695,7 +704,7 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
 #pragma unroll
             for (int i = 0; i < kLoads; i++) {
                 const int32_t jj = j + i * (int32_t)kRowsALoad + (int32_t)(lane / kChunks);
-                const bool some = is_there & (jj < tiles.high) & ((jj >= tiles.low) | (jj < tiles.sinks));
+                const bool some = is_there & (jj < min(end_of(tile), all_last.high)) & ((jj >= all_first.low) | (jj < all_last.sinks));
                 v_new[i] = some ? v_new[i] : u32x4{};
                 most = largest(most, v_new[i]);
             }
@@ -735,7 +744,7 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
             pages_ahead = pages_from(i_after + 16);
         }
         const Tile after = tile_of(i_after);
-        if (t + 2 < t_end) bring(i_after, after);
+        if (t + 2 < t_end) bring(i_after);
 
         // a wavefront whose rows see nothing of the tile has nothing to do
         if (now.some) {
@@ -758,12 +767,14 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
             __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
 
             if (now.edge) {
+                Seen here = seen;
+                here.high = min(here.high, end_of(now));
 #pragma unroll
                 for (int h = 0; h < HT; h++)
 #pragma unroll
                     for (int i = 0; i < 16; i++) {
                         const int token = 32 * h + 8 * (i / 4) + i % 4; // of the lower half; the upper half's is 4 further, brought by the same wavefront
-                        const bool sees = seen.token(j + token + 4 * (int32_t)half) & ((now.there >> (token / kTokens) & 1u) != 0);
+                        const bool sees = here.token(j + token + 4 * (int32_t)half) & ((now.there >> (token / kTokens) & 1u) != 0);
                         s[h][i] = sees ? s[h][i] : -INFINITY;
                     }
             }
@@ -814,8 +825,10 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
 #pragma unroll 1
                 for (int i = 0; i < kTile; i++) {
                     if (!(odd_bits >> (i / kTokens) & 1u)) continue;
-                    const int32_t at = table[(uint32_t)(j + i) >> a.batch.page_shift]; // there, or nothing of it would be odd
-                    const T *src = static_cast<const T *>(a.v_pages) + (page_stride * (uint32_t)at + head_at + ((uint32_t)(j + i) & place_mask)) * D + 4 * half;
+                    if (j + i >= end_of(now)) continue;
+                    const uint32_t place = (uint32_t)(j + i - (now.prefix ? 0 : base));
+                    const int32_t at = (now.prefix ? prefix_table : own_table)[place >> a.batch.page_shift]; // there, or nothing of it would be odd
+                    const T *src = static_cast<const T *>(a.v_pages) + (page_stride * (uint32_t)at + head_at + (place & place_mask)) * D + 4 * half;
                     const bool sees = seen.token(j + i);
 #pragma unroll
                     for (int dt = 0; dt < DT; dt++)
@@ -834,10 +847,10 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
 
     if (t_begin < t_end) {
         now = tile_of(0), next = tile_of(1);
-        bring(0, now);
+        bring(0);
         put_k(0);
         put_v(now, 0);
-        if (t_begin + 1 < t_end) bring(1, next);
+        if (t_begin + 1 < t_end) bring(1);
     }
     __syncthreads();
     for (int32_t t = t_begin; t < t_end; t += 2) {
@@ -984,43 +997,75 @@ template <typename T> void launch_d(const AttentionArgs &a, const Plan &plan, ui
 bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_attention *t, uint64_t *workspace_bytes)
 {
     *workspace_bytes = 0;
-    const uint32_t group = t->n_heads / cache->n_kv_heads, d = cache->head_dim;
+    const uint64_t group = t->n_heads / cache->n_kv_heads, d = cache->head_dim, prefix_len = batch->prefix_len;
     auto kind_of = [&](uint64_t rows) { return rows <= 16 ? kFew16 : rows <= 32 && d < 256 ? kFew32 : kTile; };
-    const uint64_t all_rows = (uint64_t)batch->n_rows * group;
-    const Kind prefix_kind = kind_of(all_rows), own_kind = kind_of((uint64_t)batch->max_new * group);
-    // items: workgroups that a part has uncut
-    auto cut = [&](Kind kind, uint64_t items, uint64_t tokens, uint32_t first_slot) {
-        const uint64_t tile = kind == kTile && d < 256 ? 64 : 32, least = kind == kTile ? 8 : 4;
+    const uint64_t all_rows = batch->n_rows * group, seq_rows = batch->max_new * group;
+    const Kind prefix_kind = kind_of(all_rows), own_kind = kind_of(seq_rows);
+    plan = Plan{prefix_kind, own_kind};
+    const uint64_t own_len = batch->max_len > prefix_len ? batch->max_len - prefix_len : 1;
+    const uint64_t seq_tiles = (seq_rows + kTileRows - 1) / kTileRows; // workgroups to a sequence's rows
+    // upper bound of the workgroups' number, as the kernel counts them off
+    const uint64_t row_tiles = !batch->row_start_dev ? batch->n_seqs * seq_tiles : std::min<uint64_t>(all_rows / kTileRows + batch->n_seqs, all_rows);
+    // A sequence's many rows read the prefix along with their own pages: there is nothing to join then.  Unless that takes more than twice
+    // the workgroups that all sequences' rows together take for the prefix, and no window hides most of it.
+    a.whole = prefix_len && own_kind == kTile && (t->window || batch->n_seqs * seq_tiles <= 2 * ((all_rows + kTileRows - 1) / kTileRows));
+
+    // Of the kernel for few rows: items are workgroups uncut.
+    auto cut_few = [&](uint64_t items, uint64_t tokens) {
+        constexpr uint64_t tile = 32, least = 4;
         const uint64_t n_tiles = (tokens + tile - 1) / tile, most = std::max<uint64_t>(1, std::min<uint64_t>((n_tiles + least - 1) / least, kMostSlots / 2));
         uint64_t n = 1;
-        if (kind == kTile) {
-            // two workgroups on each of 256 compute units, or one beside the others' (64 sequences behind 16384 tokens: 62 us with 256, 67 with 512)
-            const uint64_t blocks = first_slot == 0 && batch->prefix_len && own_kind != kTile ? 256 : 512;
-            n = std::min((blocks + items - 1) / items, most);
-        } else {
-            // As few workgroups as give every compute unit the same number, to a tenth: a long run of keys is read faster by one workgroup
-            // (256 of 8 heads' and 32 sequences' runs of 8000 tokens: 161 us, 512 halves of them 168, 1024 quarters 176), but an uneven number
-            // leaves units idle (320 runs of 4100 tokens: 124 us, 960 thirds 108).
-            while (n < most && (items * n + 255) / 256 * 256 * 10 > items * n * 11) n++;
-            // Where little is to be read, its latency counts: two workgroups to a unit (one token over 1999, 32 heads: 12.0 us with 256, 11.6 with 512).
-            if (!batch->prefix_len && items * n <= 256 && (n_tiles + n - 1) / n <= 16) n = std::min(2 * n, most);
+        // As few workgroups as give every compute unit the same number, to a tenth: a long run of keys is read faster by one workgroup
+        // (256 of 8 heads' and 32 sequences' runs of 8000 tokens: 161 us, 512 halves of them 168, 1024 quarters 176), but an uneven number
+        // leaves units idle (320 runs of 4100 tokens: 124 us, 960 thirds 108).
+        while (n < most && (items * n + 255) / 256 * 256 * 10 > items * n * 11) n++;
+        // Where little is to be read, its latency counts: two workgroups to a unit (one token over 1999, 32 heads: 12.0 us with 256, 11.6 with 512).
+        if (!prefix_len && items * n <= 256 && (n_tiles + n - 1) / n <= 16) n = std::min(2 * n, most);
+        return n;
+    };
+    // Of the kernel for many rows: the number of parts with the least estimate of the time, in us.  A tile's step takes `step` where a workgroup
+    // has its compute unit to itself, and a unit does `rate` steps a us where it is full; joining costs a launch and the parts' way to
+    // memory and back.
+    auto cut_many = [&](uint64_t items, uint64_t tokens, uint64_t fewer_tokens, bool joined_anyway) {
+        const double tile = d == 256 ? 32 : 64, step = d == 64 ? 1.2 : d == 128 ? 1.4 : 1.8, rate = d == 64 ? 1.5 : d == 128 ? 0.87 : 0.55;
+        const double most = std::max(1.0, ceil(tokens / tile)), mean = std::max(1.0, (tokens + fewer_tokens) / 2 / tile);
+        uint64_t best = 1;
+        double least = 1e30;
+        for (uint64_t n = 1; n <= std::min<uint64_t>((uint64_t)most, kMostSlots / 2); n += n < 8 ? 1 : n / 4) {
+            const double join = n > 1 || joined_anyway ? 4 + all_rows * cache->n_kv_heads * n * (8e-6 * d) / 2 : 0;
+            const double time = std::max(ceil(most / n) * std::max(step, ceil(items * n / 256.0) / rate), items * mean / (256 * rate)) + join;
+            if (time < least) least = time, best = n;
         }
-        const uint64_t chunk = std::max<uint64_t>(1, (n_tiles + n - 1) / n);
-        n = std::max<uint64_t>(1, (n_tiles + chunk - 1) / chunk);
+        return best;
+    };
+    auto part = [&](uint64_t items, uint64_t tokens, uint64_t tile, uint64_t n, uint32_t first_slot) {
+        const uint64_t n_tiles = std::max<uint64_t>(1, (tokens + tile - 1) / tile), chunk = (n_tiles + n - 1) / n;
+        n = (n_tiles + chunk - 1) / chunk;
         return items * n < 1u << 24 ? Part{(uint32_t)(items * n), (uint32_t)n, (uint32_t)chunk, first_slot} : Part{};
     };
-    uint64_t own = batch->max_len > batch->prefix_len ? batch->max_len - batch->prefix_len : 1;
-    uint64_t common = batch->prefix_len;
-    if (t->window) own = std::min(own, (uint64_t)t->window + batch->max_new + t->sinks + 128);
-    plan = Plan{prefix_kind, own_kind};
-    if (common) {
-        a.prefix = cut(prefix_kind, cache->n_kv_heads * (prefix_kind == kTile ? (all_rows + kTileRows - 1) / kTileRows : 1), common, 0);
+    const uint64_t tile_many = d == 256 ? 32 : 64;
+    if (prefix_len && !a.whole) {
+        const uint64_t tokens = prefix_len;
+        if (prefix_kind == kTile) {
+            const uint64_t items = cache->n_kv_heads * ((all_rows + kTileRows - 1) / kTileRows);
+            a.prefix = part(items, tokens, tile_many, cut_many(items, tokens, tokens, true), 0);
+        } else {
+            a.prefix = part(cache->n_kv_heads, tokens, 32, cut_few(cache->n_kv_heads, t->window ? std::min<uint64_t>(tokens, (uint64_t)t->window + t->sinks + 64) : tokens), 0);
+        }
         if (!a.prefix.blocks) return false;
     }
-    const uint64_t own_tiles = !batch->row_start_dev ? batch->n_seqs * ((uint64_t)(group + kTileRows - 1) / kTileRows)
-                                                     : std::min<uint64_t>(all_rows / kTileRows + batch->n_seqs, all_rows);
-    a.own = cut(own_kind, cache->n_kv_heads * (own_kind == kTile ? own_tiles : batch->n_seqs), own, a.prefix.n_splits);
-    if (!a.own.blocks) return false;
+    // what a row, or a workgroup's rows, can see
+    auto seen = [&](uint64_t tokens, uint64_t rows) { return t->window ? std::min(tokens, (uint64_t)t->window + rows + t->sinks + 64) : tokens; };
+    if (own_kind == kTile) {
+        const uint64_t longest = a.whole ? prefix_len + own_len : own_len, rows = kTileRows / group + 1;
+        const uint64_t tokens = seen(longest, rows), fewer = seen(longest > batch->max_new ? longest - batch->max_new : 1, rows);
+        const uint64_t filled = std::max<uint64_t>(1, all_rows / kTileRows); // of the workgroups counted off, about
+        a.own = part(cache->n_kv_heads * row_tiles, tokens, tile_many, cut_many(cache->n_kv_heads * filled, tokens, fewer, a.prefix.blocks != 0), a.prefix.n_splits);
+    } else {
+        const uint64_t tokens = seen(own_len, batch->max_new), items = (uint64_t)cache->n_kv_heads * batch->n_seqs;
+        a.own = part(items, tokens, 32, cut_few(items, tokens), a.prefix.n_splits);
+    }
+    if (!a.own.blocks || (uint64_t)a.own.blocks + a.prefix.blocks >= 1u << 24) return false;
     a.n_slots = a.prefix.n_splits + a.own.n_splits;
     if (a.n_slots > 1) *workspace_bytes = (uint64_t)batch->n_rows * t->n_heads * a.n_slots * (d + 2) * sizeof(float);
     return true;
