@@ -160,16 +160,21 @@ template <int TILE> struct Tiles {
     __device__ __forceinline__ int32_t first_token(int32_t tile) const { return (tile < sink_tiles ? tile : low_tile + tile - sink_tiles) * TILE; }
 };
 
-// Results of a row and head, or what the joining kernel makes them of: v holds four sums of weight times value.
+// Results of a row and head: v holds four sums of weight times value, relative to the maximum m, l the sum of the weights.
+template <typename T> __device__ __forceinline__ void store_whole(const AttentionArgs &a, uint32_t row, uint32_t head, uint32_t at, f32x4 v, float m, float l)
+{
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    const float r = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+    *reinterpret_cast<T4 *>(static_cast<T *>(a.out) + row * a.out_row + head * a.out_head + at) =
+        __builtin_convertvector(l == 0.0f ? f32x4{} : v * r, T4);
+    if (a.lse && at == 0) a.lse[(uint64_t)row * a.n_heads + head] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+// The same, or if it is one of several splits what they are joined from.
 template <typename T, int D> __device__ __forceinline__ void store_result(const AttentionArgs &a, uint32_t row, uint32_t head, uint32_t slot,
                                                                           uint32_t at, f32x4 v, float m, float l)
 {
     if (a.n_slots == 1) {
-        typedef T T4 __attribute__((ext_vector_type(4)));
-        const float r = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-        *reinterpret_cast<T4 *>(static_cast<T *>(a.out) + row * a.out_row + head * a.out_head + at) =
-            __builtin_convertvector(l == 0.0f ? f32x4{} : v * r, T4);
-        if (a.lse && at == 0) a.lse[(uint64_t)row * a.n_heads + head] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+        store_whole<T>(a, row, head, at, v, m, l);
     } else {
         const uint64_t i = ((uint64_t)row * a.n_heads + head) * a.n_slots + slot;
         *reinterpret_cast<f32x4 *>(a.partial + i * D + at) = v;
@@ -513,27 +518,30 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
     uint32_t tile = item / part.n_splits;
 
     // rows of this workgroup: i_first <= i < n of the sequence's (the batch's) rows, row_first + i / group of head kv * group + i % group
-    uint32_t row_first = 0, n, seq = 0;
+    uint32_t row_first = 0, n = 0, seq = 0;
     int32_t there = (int32_t)a.batch.prefix_len; // positions below it are, or may be, in the cache
+    int32_t p_first = 0;                         // of the sequence's first row
     if (common) {
         n = a.batch.n_rows * a.group;
     } else {
+        // a lane to a sequence: how many workgroups it has, and so whose this one is
         bool found = false;
-        n = 0;
+        uint32_t end = 0;
+        int32_t len = 0;
         if (a.batch.row_start) {
             for (uint32_t b = 0; b < a.batch.n_seqs && !found; b += 64) {
-                const uint32_t s = b + lane;
-                uint32_t tiles = 0;
-                if (s < a.batch.n_seqs) {
-                    const uint32_t first = a.batch.first_row(s), end = a.batch.rows_end(s);
-                    tiles = end > first ? (min(end - first, a.max_new) * a.group + kRows - 1) / kRows : 0;
-                }
+                const uint32_t s = min(b + lane, a.batch.n_seqs - 1), first_s = a.batch.first_row(s), end_s = a.batch.rows_end(s);
+                const int32_t len_s = a.batch.length(s);
+                const uint32_t tiles = b + lane < a.batch.n_seqs && end_s > first_s ? (min(end_s - first_s, a.max_new) * a.group + kRows - 1) / kRows : 0;
                 const uint32_t upto = dcdev::lanes_prefix_sum<false>(tiles);
                 const uint64_t beyond = __ballot(upto > tile);
                 if (beyond) {
-                    const uint32_t l = (uint32_t)__builtin_ctzll(beyond);
-                    seq = b + l;
-                    tile -= (uint32_t)__builtin_amdgcn_readlane((int)(upto - tiles), (int)l);
+                    const int l = __builtin_ctzll(beyond);
+                    seq = b + (uint32_t)l;
+                    tile -= (uint32_t)__builtin_amdgcn_readlane((int)(upto - tiles), l);
+                    row_first = (uint32_t)__builtin_amdgcn_readlane((int)first_s, l);
+                    end = (uint32_t)__builtin_amdgcn_readlane((int)end_s, l);
+                    len = __builtin_amdgcn_readlane(len_s, l);
                     found = true;
                 } else {
                     tile -= (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
@@ -543,16 +551,19 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
             const uint32_t tiles = (a.group + kRows - 1) / kRows;
             seq = tile / tiles, tile %= tiles;
             found = seq < a.batch.n_seqs;
+            if (found) row_first = seq, end = seq + 1, len = a.batch.length(seq);
         }
         if (!found) return;
         seq = __builtin_amdgcn_readfirstlane(seq), tile = __builtin_amdgcn_readfirstlane(tile);
-        row_first = a.batch.first_row(seq);
-        n = min(a.batch.rows_end(seq) - row_first, a.max_new) * a.group;
-        there = max(there, min(a.batch.length(seq), a.batch.capacity()));
+        n = min(end - row_first, a.max_new) * a.group;
+        p_first = len - (int32_t)(end - row_first);
+        there = max(there, min(len, a.batch.capacity()));
     }
     const uint32_t i_first = tile * kRows;
 
-    // positions of the rows
+    // positions of the rows: of a sequence they follow from one another; of the batch they are gathered, sequence by sequence
+    int32_t p_min, p_max, wave_p_min, wave_p_max, my_p;
+    const uint32_t my_row = i_first + wave * 32 + c;
     if (common) {
         for (uint32_t i = threadIdx.x; i < kRows; i += 256) lds.p[i] = kNoPosition;
         __syncthreads();
@@ -563,23 +574,27 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
             for (uint32_t r = max(first, r_low); r < min(end, r_high); r++)
                 for (uint32_t i = max(r * a.group, i_first); i < min((r + 1) * a.group, i_first + kRows); i++) lds.p[i - i_first] = len - (int32_t)(end - r);
         }
-    } else {
-        const int32_t p_first = a.batch.length(seq) - (int32_t)(a.batch.rows_end(seq) - row_first);
-        for (uint32_t i = threadIdx.x; i < kRows; i += 256) lds.p[i] = i_first + i < n ? p_first + (int32_t)((i_first + i) / a.group) : kNoPosition;
-    }
-    __syncthreads();
-    auto smallest_largest = [&](uint32_t first, uint32_t count, int32_t &low, int32_t &high) {
-        low = 0x7FFFFFFF, high = kNoPosition;
-        for (uint32_t i = lane; i < count; i += 64) {
-            const int32_t p = lds.p[first + i];
-            if (p != kNoPosition) low = min(low, p), high = max(high, p);
-        }
+        __syncthreads();
+        auto smallest_largest = [&](uint32_t first, uint32_t count, int32_t &low, int32_t &high) {
+            low = 0x7FFFFFFF, high = kNoPosition;
+            for (uint32_t i = lane; i < count; i += 64) {
+                const int32_t p = lds.p[first + i];
+                if (p != kNoPosition) low = min(low, p), high = max(high, p);
+            }
 #pragma unroll
-        for (int i = 1; i < 64; i <<= 1) low = min(low, __shfl_xor(low, i)), high = max(high, __shfl_xor(high, i));
-        low = __builtin_amdgcn_readfirstlane(min(low, high)), high = __builtin_amdgcn_readfirstlane(high);
-    };
-    int32_t p_min, p_max;
-    smallest_largest(0, kRows, p_min, p_max);
+            for (int i = 1; i < 64; i <<= 1) low = min(low, __shfl_xor(low, i)), high = max(high, __shfl_xor(high, i));
+            low = __builtin_amdgcn_readfirstlane(min(low, high)), high = __builtin_amdgcn_readfirstlane(high);
+        };
+        smallest_largest(0, kRows, p_min, p_max);
+        smallest_largest(wave * 32, 32, wave_p_min, wave_p_max);
+        my_p = lds.p[wave * 32 + c];
+    } else {
+        auto position = [&](uint32_t i) { return i < n ? p_first + (int32_t)(i / a.group) : kNoPosition; };
+        const uint32_t wave_first = i_first + wave * 32;
+        p_min = position(i_first), p_max = position(min(i_first + kRows, n) - 1);
+        wave_p_min = position(wave_first), wave_p_max = wave_first < n ? position(min(wave_first + 32, n) - 1) : kNoPosition;
+        my_p = position(my_row);
+    }
     // The tiles of the common prefix, if it is this launch's to read here, and behind them those of the sequence's own pages, whose first token
     // is at `base`.  Positions count from the sequence's first token, but in the two tables of pages.
     const int32_t base = (int32_t)a.batch.prefix_len;
@@ -591,12 +606,11 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
     const int32_t t_end = split + 1 == part.n_splits ? count : (int32_t)min((uint64_t)t_begin + part.chunk, (uint64_t)count);
     auto first_token = [&](int32_t t) { return t < prefix_tiles.count ? prefix_tiles.first_token(t) : base + own_tiles.first_token(t - prefix_tiles.count); };
     const Seen all_first(p_min, there, a.window, a.sinks), all_last(p_max, there, a.window, a.sinks); // of the workgroup's rows
-    smallest_largest(wave * 32, 32, p_min, p_max);
-    const Seen first_sees(p_min, there, a.window, a.sinks), last_sees(p_max, there, a.window, a.sinks); // of the wavefront's
+    const Seen first_sees(wave_p_min, there, a.window, a.sinks), last_sees(wave_p_max, there, a.window, a.sinks); // of the wavefront's
 
-    const uint32_t my_row = i_first + wave * 32 + c, my_head = kv * a.group + my_row % a.group;
+    const uint32_t my_head = kv * a.group + my_row % a.group;
     const uint64_t my_packed = row_first + my_row / a.group;
-    const Seen seen(lds.p[wave * 32 + c], there, a.window, a.sinks);
+    const Seen seen(my_p, there, a.window, a.sinks);
     TV q[KS];
     f32x16 o[DT];
     f32x16 below = f32x16{}; // the reference with the other sign, in every value
@@ -732,7 +746,7 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
     Tile now = {}, next = {};
     auto step = [&](auto B, int32_t t) {
         constexpr uint32_t buffer = decltype(B)::value;
-        constexpr int kProducts = HT * KS, kGroups = 2 * HT, kAhead = 6;
+        constexpr int kProducts = HT * KS, kGroups = 2 * HT, kAhead = 4;
         const int32_t j = now.j;
         if (t + 1 < t_end) {
             put_k(buffer ^ 1u);
@@ -901,7 +915,7 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
 
 // Joins the splits of a row and head: each has its sums relative to a maximum of its own.  The weights of the splits first, into the LDS; then
 // 4 D / 1024 of the threads go through every so many splits with several loads under way.
-constexpr uint32_t kMostSlots = 256;
+constexpr uint32_t kMostSplits = 128, kMostSlots = 2 * kMostSplits; // of a part, of both parts
 template <typename T, int D> __global__ __launch_bounds__(256) void dc_attention_join_kernel(AttentionArgs a)
 {
     constexpr uint32_t kQuads = D / 4, kSets = 256 / kQuads, kAtOnce = 4;
@@ -947,9 +961,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void dc_attention
     if (set) return;
 #pragma unroll
     for (uint32_t i = 1; i < kSets; i++) sum += lds_sum[i][at];
-    AttentionArgs whole = a;
-    whole.n_slots = 1;
-    store_result<T, D>(whole, row, head, 0, 4 * at, sum, top, total);
+    store_whole<T>(a, row, head, 4 * at, sum, top, total);
 }
 
 // Which kernel works through a part: that for at most 16 rows or 32 rows, or that for many.
@@ -1013,7 +1025,7 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     // Of the kernel for few rows: items are workgroups uncut.
     auto cut_few = [&](uint64_t items, uint64_t tokens) {
         constexpr uint64_t tile = 32, least = 4;
-        const uint64_t n_tiles = (tokens + tile - 1) / tile, most = std::max<uint64_t>(1, std::min<uint64_t>((n_tiles + least - 1) / least, kMostSlots / 2));
+        const uint64_t n_tiles = (tokens + tile - 1) / tile, most = std::max<uint64_t>(1, std::min<uint64_t>((n_tiles + least - 1) / least, kMostSplits));
         uint64_t n = 1;
         // As few workgroups as give every compute unit the same number, to a tenth: a long run of keys is read faster by one workgroup
         // (256 of 8 heads' and 32 sequences' runs of 8000 tokens: 161 us, 512 halves of them 168, 1024 quarters 176), but an uneven number
@@ -1031,8 +1043,8 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
         const double most = std::max(1.0, ceil(tokens / tile)), mean = std::max(1.0, (tokens + fewer_tokens) / 2 / tile);
         uint64_t best = 1;
         double least = 1e30;
-        for (uint64_t n = 1; n <= std::min<uint64_t>((uint64_t)most, kMostSlots / 2); n += n < 8 ? 1 : n / 4) {
-            const double join = n > 1 || joined_anyway ? 4 + all_rows * cache->n_kv_heads * n * (8e-6 * d) / 2 : 0;
+        for (uint64_t n = 1; n <= std::min<uint64_t>((uint64_t)most, kMostSplits); n += n < 8 ? 1 : n / 4) {
+            const double join = n > 1 || joined_anyway ? 4 + all_rows * cache->n_kv_heads * n * (8e-6 * d) / (joined_anyway ? 2 : 4) : 0;
             const double time = std::max(ceil(most / n) * std::max(step, ceil(items * n / 256.0) / rate), items * mean / (256 * rate)) + join;
             if (time < least) least = time, best = n;
         }
@@ -1044,18 +1056,18 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
         return items * n < 1u << 24 ? Part{(uint32_t)(items * n), (uint32_t)n, (uint32_t)chunk, first_slot} : Part{};
     };
     const uint64_t tile_many = d == 256 ? 32 : 64;
+    // what a row, or some rows together, can see
+    auto seen = [&](uint64_t tokens, uint64_t rows) { return t->window ? std::min(tokens, (uint64_t)t->window + rows + t->sinks + 64) : tokens; };
     if (prefix_len && !a.whole) {
-        const uint64_t tokens = prefix_len;
+        const uint64_t tokens = seen(prefix_len, batch->max_new);
         if (prefix_kind == kTile) {
             const uint64_t items = cache->n_kv_heads * ((all_rows + kTileRows - 1) / kTileRows);
             a.prefix = part(items, tokens, tile_many, cut_many(items, tokens, tokens, true), 0);
         } else {
-            a.prefix = part(cache->n_kv_heads, tokens, 32, cut_few(cache->n_kv_heads, t->window ? std::min<uint64_t>(tokens, (uint64_t)t->window + t->sinks + 64) : tokens), 0);
+            a.prefix = part(cache->n_kv_heads, tokens, 32, cut_few(cache->n_kv_heads, tokens), 0);
         }
         if (!a.prefix.blocks) return false;
     }
-    // what a row, or a workgroup's rows, can see
-    auto seen = [&](uint64_t tokens, uint64_t rows) { return t->window ? std::min(tokens, (uint64_t)t->window + rows + t->sinks + 64) : tokens; };
     if (own_kind == kTile) {
         const uint64_t longest = a.whole ? prefix_len + own_len : own_len, rows = kTileRows / group + 1;
         const uint64_t tokens = seen(longest, rows), fewer = seen(longest > batch->max_new ? longest - batch->max_new : 1, rows);
