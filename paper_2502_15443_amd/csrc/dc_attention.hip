@@ -876,12 +876,15 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
     const float total = both[0] + both[1];
     const float top = any || total != total ? -below[0] * a.scale : -INFINITY; // (also if it saw scores and none was a number)
     if (my_row >= n) return;
+    uint32_t row = my_row; // where the results go is worked out here, not kept in registers from the beginning
+    dcdev::anew(row);
+    const uint32_t packed = row_first + row / a.group, head = kv * a.group + row % a.group;
 #pragma unroll
     for (int dt = 0; dt < DT; dt++)
 #pragma unroll
         for (int b = 0; b < 4; b++) {
             const f32x4 v = {o[dt][4 * b], o[dt][4 * b + 1], o[dt][4 * b + 2], o[dt][4 * b + 3]};
-            store_result<T, D>(a, (uint32_t)my_packed, my_head, part.first_slot + split, 32 * dt + 8 * b + 4 * half, v, top, total);
+            store_result<T, D>(a, packed, head, part.first_slot + split, 32 * dt + 8 * b + 4 * half, v, top, total);
         }
 }
 
