@@ -7,6 +7,7 @@
 #include "dc_pages.h"
 
 #include <math.h>
+#include <stddef.h>
 
 #include <algorithm>
 #include <type_traits>
@@ -688,7 +689,7 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
     auto swizzle = [](uint32_t token) {
         return D == 64 ? (token >> 1 & 1u) << 2 | (token >> 2 & 3u) : (token & 3u) << 2 | (token >> 2 & 3u);
     };
-    const uint32_t lds_k = dcdev::lds_address(lds.k), lds_v = dcdev::lds_address(lds.v);
+    const uint32_t lds_k = dcdev::lds_address(&lds) + offsetof(TileLds<D>, k), lds_v = dcdev::lds_address(&lds) + offsetof(TileLds<D>, v);
     // where a lane puts what it brings, and where it reads its part of the first operands
     uint32_t put_at[kLoads], k_at[KS], v_at[DT][2];
 #pragma unroll
