@@ -1030,6 +1030,8 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     auto cut_few = [&](uint64_t items, uint64_t tokens) {
         constexpr uint64_t tile = 32, least = 4;
         const uint64_t n_tiles = (tokens + tile - 1) / tile, most = std::max<uint64_t>(1, std::min<uint64_t>((n_tiles + least - 1) / least, kMostSplits));
+        // Up to three tiles to a wavefront, parts gain less than it costs to join them (8 heads, 200 tokens: 6.9 us, in parts 8.5; 400: 9.0 and 8.7).
+        if (!prefix_len && n_tiles <= 12) return (uint64_t)1;
         uint64_t n = 1;
         // As few workgroups as give every compute unit the same number, to a tenth: a long run of keys is read faster by one workgroup
         // (256 of 8 heads' and 32 sequences' runs of 8000 tokens: 161 us, 512 halves of them 168, 1024 quarters 176), but an uneven number
