@@ -632,13 +632,19 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
     const uint64_t page_stride = (uint64_t)a.n_kv_heads << a.batch.page_shift;
     const uint64_t head_at = (uint64_t)kv << a.batch.page_shift;
     const uint32_t place_mask = (1u << a.batch.page_shift) - 1u;
-    // What there is to know of 16 tiles, 16 tiles ahead.  Lane l has the page of the tokens that wavefront l mod 4 brings of tile i + l / 4, counted
-    // from t_begin (-1: not there), and a bit in each of: their being there; the tile being partial, which is to say that not all rows of the
-    // workgroup see all of it; this wavefront's rows seeing some of it; and not all of it.  A tile's step takes its own with a lane's
-    // value and shifts.  (Scalar loads would do for the pages, but the LDS's data are waited for by the same counter, all of it.)
+    // What there is to know of 16 tiles, 16 tiles ahead: lane l has, of tile i + l / 4 counted from t_begin, where the tokens that wavefront l mod 4
+    // brings lie in the pools (in bytes; where there is no page, those of page 0, which are then taken for hidden), and the tile's
+    // flags.  A tile's step takes its own with three reads of a lane.  (Scalar loads would do for the pages, but the LDS's data are waited
+    // for by the same counter, all of it.)
+    enum : uint32_t {
+        kThere = 15,    // a bit for each wavefront's tokens: they are there
+        kPrefix = 16,   // of the prefix's table
+        kPartial = 32,  // not all rows of the workgroup see all of it
+        kSome = 64,     // this wavefront's rows see some of it,
+        kEdge = 128     // and not all of it
+    };
     struct Known {
-        int32_t page, at, place; // place: of the lane's wavefront's tokens in their page
-        uint64_t there, prefix, partial, some, edge;
+        uint32_t low, high, flags;
     };
     auto pages_from = [&](int32_t i) {
         const int32_t t = t_begin + i + (int32_t)(lane >> 2), j = first_token(t) + (int32_t)(lane & 3u) * kTokens;
@@ -648,42 +654,33 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
         return (uint32_t)e < a.batch.n_pages ? e : -1;
     };
     auto known_from = [&](int32_t i, int32_t page) {
-        Known k;
         const int32_t t = t_begin + i + (int32_t)(lane >> 2), j = first_token(t);
-        k.page = page;
-        k.at = j;
-        k.place = (int32_t)((uint32_t)(j + (int32_t)(lane & 3u) * kTokens - (t < prefix_tiles.count ? 0 : base)) & place_mask);
-        k.there = __ballot(page >= 0);
-        k.prefix = __ballot(t < prefix_tiles.count);
-        const bool whole = ((uint32_t)(k.there >> (lane & 60u)) & 15u) == 15u && (t >= prefix_tiles.count || j + kTile <= base);
-        k.partial = __ballot(!whole || j + kTile > all_first.high || j < all_last.low);
-        k.some = __ballot(j < last_sees.high && (j + kTile > first_sees.low || j < last_sees.sinks));
-        k.edge = __ballot(!whole || j + kTile > first_sees.high || (j < last_sees.low && j + kTile > first_sees.sinks));
-        return k;
+        const bool in_prefix = t < prefix_tiles.count;
+        const uint32_t place = (uint32_t)(j + (int32_t)(lane & 3u) * kTokens - (in_prefix ? 0 : base)) & place_mask;
+        const uint64_t at = (page_stride * (uint32_t)max(page, 0) + head_at + place) * kRowBytes;
+        const uint32_t there4 = (uint32_t)(__ballot(page >= 0) >> (lane & 60u)) & 15u;
+        const bool whole = there4 == 15u && (!in_prefix || j + kTile <= base);
+        const bool partial = !whole || j + kTile > all_first.high || j < all_last.low;
+        const bool some = t < t_end && j < last_sees.high && (j + kTile > first_sees.low || j < last_sees.sinks);
+        const bool edge = !whole || j + kTile > first_sees.high || (j < last_sees.low && j + kTile > first_sees.sinks);
+        return Known{(uint32_t)at, (uint32_t)(at >> 32), there4 | (in_prefix ? kPrefix : 0u) | (partial ? kPartial : 0u) | (some ? kSome : 0u) | (edge ? kEdge : 0u)};
     };
     int32_t pages_ahead = pages_from(0);
     Known known = known_from(0, pages_ahead);
     pages_ahead = pages_from(16);
-    // a tile as its step wants it
-    struct Tile {
-        int32_t j;
-        uint32_t there;
-        bool prefix, partial, some, edge;
-    };
+    auto flags_of = [&](int32_t i) { return (uint32_t)__builtin_amdgcn_readlane((int)known.flags, 4 * (i & 15)); };
     // tokens from here on are not of the tile's table
-    auto end_of = [&](const Tile &tile) { return tile.prefix ? base : 0x7FFFFFFF; };
-    auto tile_of = [&](int32_t i) {
-        const int32_t l = 4 * (i & 15);
-        return Tile{__builtin_amdgcn_readlane(known.at, l), (uint32_t)(known.there >> l) & 15u, (known.prefix >> l & 1u) != 0, (known.partial >> l & 1u) != 0, (known.some >> l & 1u) != 0, (known.edge >> l & 1u) != 0};
-    };
+    auto end_of = [&](uint32_t flags) { return flags & kPrefix ? base : 0x7FFFFFFF; };
     u32x4 k_new[kLoads], v_new[kLoads];
+    const uint32_t lane_at = lane * 16;
     auto bring = [&](int32_t i) {
-        const int32_t l = 4 * (i & 15) + (int32_t)wave, page = __builtin_amdgcn_readlane(known.page, l);
-        const uint64_t at = (page_stride * (uint32_t)max(page, 0) + head_at + (uint32_t)__builtin_amdgcn_readlane(known.place, l)) * D + lane * 8;
+        const int32_t l = 4 * (i & 15) + (int32_t)wave;
+        const uint64_t at = (uint32_t)__builtin_amdgcn_readlane((int)known.low, l) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)known.high, l) << 32;
+        const uint8_t *k_at = static_cast<const uint8_t *>(a.k_pages) + at, *v_at = static_cast<const uint8_t *>(a.v_pages) + at;
 #pragma unroll
-        for (int i = 0; i < kLoads; i++) k_new[i] = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.k_pages) + at + i * 512);
+        for (int i = 0; i < kLoads; i++) k_new[i] = *reinterpret_cast<const u32x4 *>(k_at + lane_at + i * 1024);
 #pragma unroll
-        for (int i = 0; i < kLoads; i++) v_new[i] = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.v_pages) + at + i * 512);
+        for (int i = 0; i < kLoads; i++) v_new[i] = *reinterpret_cast<const u32x4 *>(v_at + lane_at + i * 1024);
     };
     // The 16-byte chunks of a token lie exchanged in the LDS, so that 16 tokens' same chunks are on different banks, and the same four of 4 tokens'.
     auto swizzle = [](uint32_t token) {
@@ -711,15 +708,15 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
         for (int i = 0; i < kLoads; i++) *(lds_u32x4 *)(uintptr_t)(lds_k + buffer * kBuffer + put_at[i]) = k_new[i];
     };
     // Of a partial tile a wavefront leaves in lds.odd whether one of the values of V that it brought is no number.
-    auto put_v = [&](const Tile &tile, uint32_t buffer) {
-        if (tile.partial) {
-            const bool is_there = (tile.there >> wave & 1u) != 0;
-            const int32_t j = tile.j + (int32_t)wave * kTokens;
+    auto put_v = [&](int32_t t, uint32_t flags, uint32_t buffer) {
+        if (flags & kPartial) {
+            const bool is_there = (flags >> wave & 1u) != 0;
+            const int32_t j = first_token(t) + (int32_t)wave * kTokens;
             u16x2 most = {};
 #pragma unroll
             for (int i = 0; i < kLoads; i++) {
                 const int32_t jj = j + i * (int32_t)kRowsALoad + (int32_t)(lane / kChunks);
-                const bool some = is_there & (jj < min(end_of(tile), all_last.high)) & ((jj >= all_first.low) | (jj < all_last.sinks));
+                const bool some = is_there & (jj < min(end_of(flags), all_last.high)) & ((jj >= all_first.low) | (jj < all_last.sinks));
                 v_new[i] = some ? v_new[i] : u32x4{};
                 most = largest(most, v_new[i]);
             }
@@ -744,25 +741,24 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
 
     // A step works on tile t, whose keys and values are in buffer B, while the next tile's go from registers into the other buffer and those
     // of the tile behind it are asked for.
-    Tile now = {}, next = {};
+    uint32_t flags = 0, flags_next = 0; // of tiles t and t + 1
     auto step = [&](auto B, int32_t t) {
         constexpr uint32_t buffer = decltype(B)::value;
         constexpr int kProducts = HT * KS, kGroups = 2 * HT, kAhead = 4;
-        const int32_t j = now.j;
         if (t + 1 < t_end) {
             put_k(buffer ^ 1u);
-            put_v(next, buffer ^ 1u);
+            put_v(t + 1, flags_next, buffer ^ 1u);
         }
         const int32_t i_after = t + 2 - t_begin;
         if ((i_after & 15) == 0) {
             known = known_from(i_after, pages_ahead);
             pages_ahead = pages_from(i_after + 16);
         }
-        const Tile after = tile_of(i_after);
+        const uint32_t flags_after = flags_of(i_after);
         if (t + 2 < t_end) bring(i_after);
 
         // a wavefront whose rows see nothing of the tile has nothing to do
-        if (now.some) {
+        if (flags & kSome) {
             // The operands come out of the LDS several products ahead of their use.
             f32x16 s[HT];
             TV x[kAhead];
@@ -781,24 +777,23 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
             }
             __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
 
-            if (now.edge) {
+            if (flags & kEdge) {
+                const int32_t j = first_token(t);
                 Seen here = seen;
-                here.high = min(here.high, end_of(now));
+                here.high = min(here.high, end_of(flags));
 #pragma unroll
                 for (int h = 0; h < HT; h++)
 #pragma unroll
                     for (int i = 0; i < 16; i++) {
                         const int token = 32 * h + 8 * (i / 4) + i % 4; // of the lower half; the upper half's is 4 further, brought by the same wavefront
-                        const bool sees = here.token(j + token + 4 * (int32_t)half) & ((now.there >> (token / kTokens) & 1u) != 0);
+                        const bool sees = here.token(j + token + 4 * (int32_t)half) & ((flags >> (token / kTokens) & 1u) != 0);
                         s[h][i] = sees ? s[h][i] : -INFINITY;
                     }
             }
-            float top = s[0][0];
+            float tops[4] = {s[0][0], s[0][1], s[0][2], s[0][3]}; // four chains of comparisons, not one of sixteen
 #pragma unroll
-            for (int h = 0; h < HT; h++)
-#pragma unroll
-                for (int i = 0; i < 16; i++) top = fmaxf(top, s[h][i]);
-            top = max_over_32(top);
+            for (int i = 4; i < 16 * HT; i++) tops[i % 4] = fmaxf(tops[i % 4], s[i / 16][i % 16]);
+            const float top = max_over_32(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
             // Scores come out of the products less a reference, with which the sums begin.  It moves, to the largest score so far, only when one
             // is so far above it that its weight would exceed 256: weights stay far inside the range of the type, and what has been added
             // up is scaled now and then, not for every tile.
@@ -832,17 +827,18 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
             }
             dcdev::in_register<false>(l); // the additions among the products, not behind them
             uint32_t odd_bits = 0;
-            if (now.partial) {
+            if (flags & kPartial) {
 #pragma unroll
                 for (int i = 0; i < 4; i++) odd_bits |= __builtin_amdgcn_readfirstlane(lds.odd[buffer][i]) << i;
             }
             if (odd_bits) {
 #pragma unroll 1
                 for (int i = 0; i < kTile; i++) {
+                    const int32_t j = first_token(t);
                     if (!(odd_bits >> (i / kTokens) & 1u)) continue;
-                    if (j + i >= end_of(now)) continue;
-                    const uint32_t place = (uint32_t)(j + i - (now.prefix ? 0 : base));
-                    const int32_t at = (now.prefix ? prefix_table : own_table)[place >> a.batch.page_shift]; // there, or nothing of it would be odd
+                    if (j + i >= end_of(flags)) continue;
+                    const uint32_t place = (uint32_t)(j + i - (flags & kPrefix ? 0 : base));
+                    const int32_t at = (flags & kPrefix ? prefix_table : own_table)[place >> a.batch.page_shift]; // there, or nothing of it would be odd
                     const T *src = static_cast<const T *>(a.v_pages) + (page_stride * (uint32_t)at + head_at + (place & place_mask)) * D + 4 * half;
                     const bool sees = seen.token(j + i);
 #pragma unroll
@@ -856,15 +852,15 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
                 }
             }
         }
-        now = next, next = after;
+        flags = flags_next, flags_next = flags_after;
         __syncthreads();
     };
 
     if (t_begin < t_end) {
-        now = tile_of(0), next = tile_of(1);
+        flags = flags_of(0), flags_next = flags_of(1);
         bring(0);
         put_k(0);
-        put_v(now, 0);
+        put_v(t_begin, flags, 0);
         if (t_begin + 1 < t_end) bring(1);
     }
     __syncthreads();
@@ -880,13 +876,25 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
     uint32_t row = my_row; // where the results go is worked out here, not kept in registers from the beginning
     dcdev::anew(row);
     const uint32_t packed = row_first + row / a.group, head = kv * a.group + row % a.group;
+    auto sums = [&](int dt, int b) { return f32x4{o[dt][4 * b], o[dt][4 * b + 1], o[dt][4 * b + 2], o[dt][4 * b + 3]}; };
+    if (a.n_slots == 1) {
+        typedef T T4 __attribute__((ext_vector_type(4)));
+        T *out = static_cast<T *>(a.out) + packed * a.out_row + head * a.out_head + 4 * half;
+        const float r = total == 0.0f ? 0.0f : 1.0f / total;
 #pragma unroll
-    for (int dt = 0; dt < DT; dt++)
+        for (int dt = 0; dt < DT; dt++)
 #pragma unroll
-        for (int b = 0; b < 4; b++) {
-            const f32x4 v = {o[dt][4 * b], o[dt][4 * b + 1], o[dt][4 * b + 2], o[dt][4 * b + 3]};
-            store_result<T, D>(a, packed, head, part.first_slot + split, 32 * dt + 8 * b + 4 * half, v, top, total);
-        }
+            for (int b = 0; b < 4; b++) *reinterpret_cast<T4 *>(out + 32 * dt + 8 * b) = __builtin_convertvector(sums(dt, b) * r, T4);
+        if (a.lse && half == 0) a.lse[(uint64_t)packed * a.n_heads + head] = total == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
+    } else {
+        const uint64_t i = ((uint64_t)packed * a.n_heads + head) * a.n_slots + part.first_slot + split;
+        float *out = a.partial + i * D + 4 * half;
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+            for (int b = 0; b < 4; b++) *reinterpret_cast<f32x4 *>(out + 32 * dt + 8 * b) = sums(dt, b);
+        if (half == 0) a.partial_ml[i] = f32x2{top, total};
+    }
 }
 
 template <int D> constexpr int workgroups_a_unit() { return D == 256 ? 1 : D == 64 ? 3 : 2; }
