@@ -87,6 +87,26 @@ __device__ __forceinline__ float sum_over_16(float v)
     return r[0] + r[1];
 }
 
+// Largest of the lanes' values.
+__device__ __forceinline__ uint32_t largest_of_lanes(uint32_t v)
+{
+    v = max(v, dcdev::dpp_or_zero<0x111, 0xF>(v));
+    v = max(v, dcdev::dpp_or_zero<0x112, 0xF>(v));
+    v = max(v, dcdev::dpp_or_zero<0x114, 0xF>(v));
+    v = max(v, dcdev::dpp_or_zero<0x118, 0xF>(v));
+    v = max(v, dcdev::dpp_or_zero<0x142, 0xA>(v));
+    v = max(v, dcdev::dpp_or_zero<0x143, 0xC>(v));
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+// Smallest and largest of the lanes' positions but kNoPosition; both are that if there is none.
+__device__ __forceinline__ void range_of_positions(int32_t p_low, int32_t p_high, int32_t &low, int32_t &high)
+{
+    // positions are above kNoPosition (-2^30) by less than 2^31 + 2^30: counted from there, and down from 2^32 - 1, they have 0 for none
+    high = (int32_t)(largest_of_lanes((uint32_t)p_high - (uint32_t)kNoPosition) + (uint32_t)kNoPosition);
+    const uint32_t l = largest_of_lanes(p_low == kNoPosition ? 0u : ~((uint32_t)p_low - (uint32_t)kNoPosition));
+    low = l ? (int32_t)(~l + (uint32_t)kNoPosition) : kNoPosition;
+}
+
 // 2^x; 0 for -infinity.
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -242,12 +262,8 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
             for (uint32_t r = first; r < end; r++) lds.p[r] = a.batch.length(b) - (int32_t)(end - r);
         }
         __syncthreads();
-        p_min = 0x7FFFFFFF, p_max = kNoPosition;
-        for (uint32_t r = 0; r < a.batch.n_rows; r++) {
-            const int32_t p = lds.p[r];
-            if (p != kNoPosition) p_min = min(p_min, p), p_max = max(p_max, p);
-        }
-        p_min = min(p_min, p_max);
+        const int32_t p = lane < min(a.batch.n_rows, 16u * RT) ? lds.p[lane] : kNoPosition;
+        range_of_positions(p, p, p_min, p_max);
     } else {
         row_first = a.batch.first_row(seq);
         const uint32_t end = a.batch.rows_end(seq);
@@ -576,18 +592,10 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
                 for (uint32_t i = max(r * a.group, i_first); i < min((r + 1) * a.group, i_first + kRows); i++) lds.p[i - i_first] = len - (int32_t)(end - r);
         }
         __syncthreads();
-        auto smallest_largest = [&](uint32_t first, uint32_t count, int32_t &low, int32_t &high) {
-            low = 0x7FFFFFFF, high = kNoPosition;
-            for (uint32_t i = lane; i < count; i += 64) {
-                const int32_t p = lds.p[first + i];
-                if (p != kNoPosition) low = min(low, p), high = max(high, p);
-            }
-#pragma unroll
-            for (int i = 1; i < 64; i <<= 1) low = min(low, __shfl_xor(low, i)), high = max(high, __shfl_xor(high, i));
-            low = __builtin_amdgcn_readfirstlane(min(low, high)), high = __builtin_amdgcn_readfirstlane(high);
-        };
-        smallest_largest(0, kRows, p_min, p_max);
-        smallest_largest(wave * 32, 32, wave_p_min, wave_p_max);
+        const int32_t p0 = lds.p[lane], p1 = lds.p[lane + 64];
+        range_of_positions(p0 == kNoPosition ? p1 : p1 == kNoPosition ? p0 : min(p0, p1), max(p0, p1), p_min, p_max);
+        const int32_t p = lds.p[wave * 32 + c];
+        range_of_positions(p, p, wave_p_min, wave_p_max);
         my_p = lds.p[wave * 32 + c];
     } else {
         auto position = [&](uint32_t i) { return i < n ? p_first + (int32_t)(i / a.group) : kNoPosition; };
