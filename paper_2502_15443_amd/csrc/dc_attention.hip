@@ -212,6 +212,8 @@ template <typename T, int D> __device__ __forceinline__ void store_result(const 
 // first operand, 8 tokens of one value, comes out of the LDS through the transposing read.  So maxima, sums and the scaling of
 // what has been added up stay inside a lane but for two exchanges a tile.  K and then V go through registers into the wavefront's
 // own part of the LDS: no barrier in the loop.  The next tile's loads are under way during the rest of the tile's work.
+// One token over 131071 tokens, 537 MB: 80.5 us (6.7 TB/s) and 4.5 for the join; 64 sequences of 512 to 8192 tokens, 1.2 GB: 205 us (5.85 TB/s, for
+// sequences of unlike lengths end at unlike times; alike ones read 6.6); one token over 1999, 32 heads: 8 us and 3.
 template <int D, int RT> struct FewLds {
     static constexpr int kPadded = D + 4; // floats of a row's sums
     union {
@@ -510,7 +512,9 @@ constexpr uint32_t kTileRows = 128; // of a workgroup of the kernel for many row
 // units bound this kernel.  Keys and values go through the LDS in tiles that its four wavefronts share, double buffered with one barrier a
 // tile; a wavefront owns 32 rows.  The products are those of the kernel for few rows in the 32x32x16 shape: scores as [token][row]
 // = K Q^T, of which a lane holds 16 of 32 tokens of one row, results as [head_dim][row] = V^T P^T; maxima and sums stay in a lane but for one
-// exchange between the halves.
+// exchange between the halves.  A prompt of 8192 tokens, 32 heads of 128: 559 to 591 us (930 to 980 TFLOP/s; a large library product reaches 1250),
+// the matrix units busy 45 % and the vector units 42 % of the cycles at a clock that falls to 2.0 GHz.  Tiles of 64 tokens are 8 to 20 % faster
+// than of 32, for which alone heads of 256 have registers (560 to 585 TFLOP/s).
 template <int D> struct TileLds {
     static constexpr int kTile = D == 256 ? 32 : 64; // tokens
     uint8_t k[2][kTile * 2 * D], v[2][kTile * 2 * D];
@@ -915,7 +919,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, workgroups_a_unit
 
 // A common prefix with many rows and few rows in each sequence: the first is bound by the matrix units, the second by memory, and the two
 // kinds of workgroups lie in one launch in turn, so that a compute unit has some of each (64 sequences behind 16384 tokens: 67 us instead of 72
-// in two launches).
+// in two launches; 62 since then, 5 of them the join).
 // In turn by eights: a workgroup's XCD is its number modulo 8, and those of one key/value head's prefix stay on one.
 template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void dc_attention_both_kernel(AttentionArgs a)
 {
@@ -934,7 +938,8 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
 }
 
 // Joins the splits of a row and head: each has its sums relative to a maximum of its own.  The weights of the splits first, into the LDS; then
-// 4 D / 1024 of the threads go through every so many splits with several loads under way.
+// 4 D / 1024 of the threads go through every so many splits with several loads under way: 3 us for 32 rows and heads, 5.4 for 64 rows of 32 heads.  (The last
+// split to arrive joining them all instead: every workgroup's device-wide fence empties its L2, one token 106 instead of 12 us.)
 constexpr uint32_t kMostSplits = 128, kMostSlots = 2 * kMostSplits; // of a part, of both parts
 template <typename T, int D> __global__ __launch_bounds__(256) void dc_attention_join_kernel(AttentionArgs a)
 {
@@ -1030,6 +1035,9 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
 {
     *workspace_bytes = 0;
     const uint64_t group = t->n_heads / cache->n_kv_heads, d = cache->head_dim, prefix_len = batch->prefix_len;
+    // Up to 32 rows the kernel for few rows, of the matrix units' 16 or 32 (16 sequences of 8192 tokens, 8 heads of 128: 16 rows 88 us, by the kernel
+    // for many 119; 20 rows 91 and 122; of one sequence, 16 rows of 4000 tokens 11.5 and 13.9, but 20 rows of 8192 19.1 and 16.4).  Heads of
+    // 256 have no registers for 32.
     auto kind_of = [&](uint64_t rows) { return rows <= 16 ? kFew16 : rows <= 32 && d < 256 ? kFew32 : kTile; };
     const uint64_t all_rows = batch->n_rows * group, seq_rows = batch->max_new * group;
     const Kind prefix_kind = kind_of(all_rows), own_kind = kind_of(seq_rows);
@@ -1038,9 +1046,16 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     const uint64_t seq_tiles = (seq_rows + kTileRows - 1) / kTileRows; // workgroups to a sequence's rows
     // upper bound of the workgroups' number, as the kernel counts them off
     const uint64_t row_tiles = !batch->row_start_dev ? batch->n_seqs * seq_tiles : std::min<uint64_t>(all_rows / kTileRows + batch->n_seqs, all_rows);
-    // A sequence's many rows read the prefix along with their own pages: there is nothing to join then.  Unless that takes more than twice
-    // the workgroups that all sequences' rows together take for the prefix, and no window hides most of it.
-    a.whole = prefix_len && own_kind == kTile && (t->window || batch->n_seqs * seq_tiles <= 2 * ((all_rows + kTileRows - 1) / kTileRows));
+    const uint64_t tile_many = d == 256 ? 32 : 64;
+    const double unit_rate = d == 64 ? 1.5 : d == 128 ? 0.87 : 0.55; // steps a us of a full compute unit in the kernel for many rows
+    // A sequence's many rows read the prefix along with their own pages, with nothing to join then, where the workgroups that this takes beyond those of all
+    // sequences' rows together cost less than the join (their steps taken at 0.57 of the full rate, for launches fill the units unevenly), and where a window
+    // hides most of the prefix.  8 sequences, 8 heads of 128 (us; read whole, and once): 64 rows behind 512 tokens 20 and 24, behind 4096 32.5 and
+    // 30.9; 160 rows 23 and 33, 65 and 56; 400 rows behind 4096 96 and 107, behind 16384 302 and 272; 64 rows with a window of 512 20.5 and 26.5.
+    const uint64_t shared_tiles = (all_rows + kTileRows - 1) / kTileRows;
+    const uint64_t more_tiles = batch->n_seqs * seq_tiles - std::min(batch->n_seqs * seq_tiles, shared_tiles);
+    const double more_time = (double)more_tiles * cache->n_kv_heads * prefix_len / tile_many / (0.57 * 256 * unit_rate);
+    a.whole = prefix_len && own_kind == kTile && (t->window || more_time <= 4 + all_rows * cache->n_kv_heads * (8e-6 * d));
 
     // Of the kernel for few rows: items are workgroups uncut.
     auto cut_few = [&](uint64_t items, uint64_t tokens) {
@@ -1058,16 +1073,16 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
         return n;
     };
     // Of the kernel for many rows: the number of parts with the least estimate of the time, in us.  A tile's step takes `step` where a workgroup
-    // has its compute unit to itself, and a unit does `rate` steps a us where it is full; joining costs a launch and the parts' way to
+    // has its compute unit to itself, and a unit does unit_rate steps a us where it is full; joining costs a launch and the parts' way to
     // memory and back.
     auto cut_many = [&](uint64_t items, uint64_t tokens, uint64_t fewer_tokens, bool joined_anyway) {
-        const double tile = d == 256 ? 32 : 64, step = d == 64 ? 1.2 : d == 128 ? 1.4 : 1.8, rate = d == 64 ? 1.5 : d == 128 ? 0.87 : 0.55;
+        const double tile = tile_many, step = d == 64 ? 1.2 : d == 128 ? 1.4 : 1.8;
         const double most = std::max(1.0, ceil(tokens / tile)), mean = std::max(1.0, (tokens + fewer_tokens) / 2 / tile);
         uint64_t best = 1;
         double least = 1e30;
         for (uint64_t n = 1; n <= std::min<uint64_t>((uint64_t)most, kMostSplits); n += n < 8 ? 1 : n / 4) {
             const double join = n > 1 || joined_anyway ? 4 + all_rows * cache->n_kv_heads * n * (8e-6 * d) / (joined_anyway ? 2 : 4) : 0;
-            const double time = std::max(ceil(most / n) * std::max(step, ceil(items * n / 256.0) / rate), items * mean / (256 * rate)) + join;
+            const double time = std::max(ceil(most / n) * std::max(step, ceil(items * n / 256.0) / unit_rate), items * mean / (256 * unit_rate)) + join;
             if (time < least) least = time, best = n;
         }
         return best;
@@ -1077,7 +1092,6 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
         n = (n_tiles + chunk - 1) / chunk;
         return items * n < 1u << 24 ? Part{(uint32_t)(items * n), (uint32_t)n, (uint32_t)chunk, first_slot} : Part{};
     };
-    const uint64_t tile_many = d == 256 ? 32 : 64;
     // what a row, or some rows together, can see
     auto seen = [&](uint64_t tokens, uint64_t rows) { return t->window ? std::min(tokens, (uint64_t)t->window + rows + t->sinks + 64) : tokens; };
     if (prefix_len && !a.whole) {

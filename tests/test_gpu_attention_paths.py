@@ -51,6 +51,13 @@ def test_prefix_apart_from_the_own_pages(d, prefix):
 
 
 @pytest.mark.parametrize("d", [64, 128, 256])
+def test_long_prefix_apart_from_the_own_pages(d):
+    # twelve workgroups instead of three over a prefix of this length cost more than what is joined afterwards
+    news = [9, 1, 5, 9, 9, 9, 2, 9, 9, 0, 9, 9]
+    run(44, "bf16", 4, 1, d, 64, [7003 + n + 3 * i for i, n in enumerate(news)], news, prefix=7003, absent=[(3, 0)])
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("heads,kv_heads", [(9, 1), (40, 2)])
 @pytest.mark.parametrize("window,sinks", [(0, 0), (260, 4)])
 def test_prefix_and_own_pages_in_one_launch(d, heads, kv_heads, window, sinks):
