@@ -590,7 +590,8 @@ typedef struct {
  * A row that sees nothing (or only s_j = -inf) has out = 0 and lse = -inf.  What is not seen has no influence, NaN and infinities
  * included: tokens beyond a sequence's length, behind its window, or on pages that are not there may hold anything.
  * Scores, sums and results are held in fp32; exp(s_j - reference) is rounded to the cache's type for the product with the values.
- * A common prefix (prefix_len > 0) is read once for all sequences' rows together.
+ * A common prefix (prefix_len > 0) is read once for all sequences' rows together, or where that takes longer by each sequence's rows
+ * along with its own pages.
  *   workspace_dev   at least dc_attention_paged_workspace() bytes, 16-byte aligned (NULL if that is 0); its contents before the
  *                   call do not matter, and it may be reused once the call's work on the stream is done
  * Errors: DC_E_ARG, DC_E_CAP (workspace too small), DC_E_HIP.

@@ -514,7 +514,7 @@ constexpr uint32_t kTileRows = 128; // of a workgroup of the kernel for many row
 // = K Q^T, of which a lane holds 16 of 32 tokens of one row, results as [head_dim][row] = V^T P^T; maxima and sums stay in a lane but for one
 // exchange between the halves.  A prompt of 8192 tokens, 32 heads of 128: 559 to 591 us (930 to 980 TFLOP/s; a large library product reaches 1250),
 // the matrix units busy 45 % and the vector units 42 % of the cycles at a clock that falls to 2.0 GHz.  Tiles of 64 tokens are 8 to 20 % faster
-// than of 32, for which alone heads of 256 have registers (560 to 585 TFLOP/s).
+// than of 32, for which alone heads of 256 have registers (560 to 600 TFLOP/s).
 template <int D> struct TileLds {
     static constexpr int kTile = D == 256 ? 32 : 64; // tokens
     uint8_t k[2][kTile * 2 * D], v[2][kTile * 2 * D];
@@ -892,11 +892,11 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
     if (a.n_slots == 1) {
         typedef T T4 __attribute__((ext_vector_type(4)));
         T *out = static_cast<T *>(a.out) + packed * a.out_row + head * a.out_head + 4 * half;
-        const float r = total == 0.0f ? 0.0f : 1.0f / total;
+        const float r = 1.0f / total;
 #pragma unroll
         for (int dt = 0; dt < DT; dt++)
 #pragma unroll
-            for (int b = 0; b < 4; b++) *reinterpret_cast<T4 *>(out + 32 * dt + 8 * b) = __builtin_convertvector(sums(dt, b) * r, T4);
+            for (int b = 0; b < 4; b++) *reinterpret_cast<T4 *>(out + 32 * dt + 8 * b) = __builtin_convertvector(total == 0.0f ? f32x4{} : sums(dt, b) * r, T4);
         if (a.lse && half == 0) a.lse[(uint64_t)packed * a.n_heads + head] = total == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
     } else {
         const uint64_t i = ((uint64_t)packed * a.n_heads + head) * a.n_slots + part.first_slot + split;

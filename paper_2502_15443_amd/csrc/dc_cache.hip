@@ -109,9 +109,10 @@ template <typename X, typename T, int D, int WAVES> void launch_w(const AppendAr
 template <typename X, typename T, int D> void launch_d(const AppendArgs &a, bool neighbours, hipStream_t stream)
 {
     const uint32_t slots = a.n_heads + 2 * a.n_kv_heads, slots_a_block = kThreads / (D / 16), rows = a.batch.n_rows;
-    // Few rows: a row's heads are asked for all at once (128 to 512 rows: 3.1 to 4.1 instead of 4.1 to 4.7 us; 2048 rows of 48 heads 10.5 instead of 10.1).  Many: the cosines and sines stay in registers for all of a row's heads, of which a workgroup
-    // takes a row, or if they are not enough for its threads four (rows of 2 x 5 to 20 heads of 64: 4.0 instead of 5.3 us for 3000, 5.1 instead of
-    // 6.3 for 3500; 8192 rows of 48 heads of 128: 33 instead of 31.4).
+    // Few rows: a row's heads are asked for all at once (128 to 512 rows: 3.1 to 4.1 instead of 4.1 to 4.7 us; 2048 rows of 48 heads 10.5 instead
+    // of 10.1).  Many: the cosines and sines stay in registers for all of a row's heads, of which a workgroup takes a row, or if they are not
+    // enough for its threads four (rows of 2 x 5 to 20 heads of 64: 4.0 instead of 5.3 us for 3000, 5.1 instead of 6.3 for 3500; 8192 rows of 48
+    // heads of 128: 33 instead of 31.4).
     if (rows < 512) {
         const dim3 grid(rows, (slots + slots_a_block - 1) / slots_a_block);
         launch_w<X, T, D, 0>(a, neighbours, grid, stream);

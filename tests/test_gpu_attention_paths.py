@@ -111,3 +111,19 @@ def test_rows_whose_scores_are_no_numbers_or_infinite():
         got, got_lse = attend(p, 1, q, 0.5)
         assert np.isnan(got[:news]).all() and np.isnan(got_lse[:news]).all()
         assert (got[news:] == 0).all() and np.isneginf(got_lse[news:]).all()
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("news,length", [(1, 4), (1, 700), (40, 43), (40, 1500)])
+def test_rows_whose_scores_are_all_minus_infinity_beside_infinite_values(d, news, length):
+    """Such rows count as seeing nothing, whatever the values are."""
+    p = paged(45, "f16", 1, d, 16, [length, length], [news, news])
+    q = torch.ones((2 * news, 1, d), dtype=torch.float16)
+    for b in (0, 1):
+        for j in range(length):
+            page, at = oa.place_of(p["batch"], b, j, 16, p["n_pages"])
+            p["k"][page, 0, at, 7] = float("-inf")
+            if b == 0:
+                p["v"][page, 0, at, j % d] = float("inf")
+    got, got_lse = attend(p, 1, q, 0.1)
+    assert (got == 0).all() and np.isneginf(got_lse).all()
