@@ -47,16 +47,22 @@ struct AttentionArgs {
     Part prefix, own;
 };
 
+// kLiftFew, kLiftMany: by how many powers of two a row's reference lies below the largest score that it was taken from.  bf16 reaches as far
+// down as fp32; f16 loses bits below 2^-14 and everything below 2^-25, which over a long context adds up to more than its unit (131071 keys:
+// 0.4 %).  Its largest value is 2^16: in the kernel for few rows the largest weight is 2^15; in the one for many, whose reference lags
+// behind the largest score, 2^7 to 2^15.  The sums are fp32 and have room for both.
 template <typename T> struct Mfma;
 template <> struct Mfma<__bf16> {
     __device__ static __forceinline__ f32x4 m16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     __device__ static __forceinline__ f32x16 m32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     static constexpr uint32_t kExponent = 0x7F80u;
+    static constexpr float kLiftFew = 0.0f, kLiftMany = 0.0f;
 };
 template <> struct Mfma<_Float16> {
     __device__ static __forceinline__ f32x4 m16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
     __device__ static __forceinline__ f32x16 m32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
     static constexpr uint32_t kExponent = 0x7C00u;
+    static constexpr float kLiftFew = 15.0f, kLiftMany = 7.0f;
 };
 
 // Maximum and sum over the lanes with the same number modulo 16 (32).
@@ -421,13 +427,13 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
             float top = fmaxf(fmaxf(fmaxf(s[rt][0][0], s[rt][0][1]), fmaxf(s[rt][0][2], s[rt][0][3])),
                               fmaxf(fmaxf(s[rt][1][0], s[rt][1][1]), fmaxf(s[rt][1][2], s[rt][1][3])));
             top = fmaxf(m[rt], max_over_16(top));
-            const float ref = top == -INFINITY ? 0.0f : top * a.scale;
-            const float fade = exp2_of(m[rt] * a.scale - ref);
+            const float ref = top == -INFINITY ? 0.0f : top;
+            const float fade = exp2_of((m[rt] - ref) * a.scale);
             m[rt] = top;
             typedef float f32x8 __attribute__((ext_vector_type(8)));
             f32x8 e;
 #pragma unroll
-            for (int i = 0; i < 8; i++) e[i] = exp2_of(__builtin_fmaf(s[rt][i / 4][i % 4], a.scale, -ref));
+            for (int i = 0; i < 8; i++) e[i] = exp2_of(__builtin_fmaf(s[rt][i / 4][i % 4] - ref, a.scale, Mfma<T>::kLiftFew));
             l[rt] = l[rt] * fade + (((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
             w[rt] = __builtin_convertvector(e, TV);
 #pragma unroll
@@ -464,7 +470,7 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) {
         l[rt] = sum_over_16(l[rt]);
-        m[rt] *= a.scale;
+        m[rt] = m[rt] * a.scale - Mfma<T>::kLiftFew; // what the weights are relative to
         if (l[rt] != l[rt] && m[rt] == -INFINITY) m[rt] = 0.0f; // saw scores, none of them a number
         if (g == 0) lds.m[wave][rt * 16 + c] = m[rt], lds.l[wave][rt * 16 + c] = l[rt];
     }
@@ -807,8 +813,8 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
             for (int i = 4; i < 16 * HT; i++) tops[i % 4] = fmaxf(tops[i % 4], s[i / 16][i % 16]);
             const float top = max_over_32(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
             // Scores come out of the products less a reference, with which the sums begin.  It moves, to the largest score so far, only when one
-            // is so far above it that its weight would exceed 256: weights stay far inside the range of the type, and what has been added
-            // up is scaled now and then, not for every tile.
+            // is so far above it that its weight would exceed 2^(kLiftMany + 8): weights stay inside the range of the type, and what has been
+            // added up is scaled now and then, not for every tile.
             if (__any(top * a.scale > 8.0f || (!any && top != -INFINITY))) {
                 const float rise = any ? fmaxf(top, 0.0f) : top == -INFINITY ? 0.0f : top;
                 const float fade = any ? exp2_of(-rise * a.scale) : 0.0f;
@@ -826,9 +832,10 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
 #pragma unroll
             for (int u = 0; u < kGroups; u++) {
                 typedef float f32x8 __attribute__((ext_vector_type(8)));
+                auto lifted = [&](float x) { return Mfma<T>::kLiftMany == 0.0f ? x * a.scale : __builtin_fmaf(x, a.scale, Mfma<T>::kLiftMany); };
                 f32x8 e;
 #pragma unroll
-                for (int i = 0; i < 8; i++) e[i] = exp2_of(s[u / 2][8 * (u % 2) + i] * a.scale);
+                for (int i = 0; i < 8; i++) e[i] = exp2_of(lifted(s[u / 2][8 * (u % 2) + i]));
                 l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
                 w[u] = __builtin_convertvector(e, TV);
             }
@@ -883,7 +890,8 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
 
     const f32x2 both = swapped32(l);
     const float total = both[0] + both[1];
-    const float top = any || total != total ? -below[0] * a.scale : -INFINITY; // (also if it saw scores and none was a number)
+    // what the weights are relative to (also if the row saw scores and none was a number)
+    const float top = any || total != total ? -below[0] * a.scale - Mfma<T>::kLiftMany : -INFINITY;
     if (my_row >= n) return;
     uint32_t row = my_row; // where the results go is worked out here, not kept in registers from the beginning
     dcdev::anew(row);
