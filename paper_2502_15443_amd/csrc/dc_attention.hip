@@ -777,54 +777,60 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
 
         // a wavefront whose rows see nothing of the tile has nothing to do
         if (flags & kSome) {
-            // The operands come out of the LDS several products ahead of their use.
             f32x16 s[HT];
             TV x[kAhead];
+            auto scores = [&](const f32x16 &from) {
+                // The operands come out of the LDS several products ahead of their use.
 #pragma unroll
-            for (int i = 0; i < kAhead; i++) x[i] = k_operand(i, buffer);
+                for (int i = 0; i < kAhead; i++) x[i] = k_operand(i, buffer);
 #pragma unroll
-            for (int i = 0; i < kProducts; i++) {
-                s[i / KS] = Mfma<T>::m32(x[i % kAhead], q[i % KS], i % KS ? s[i / KS] : below);
-                if (i + kAhead < kProducts) x[i % kAhead] = k_operand(i + kAhead, buffer);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+                for (int i = 0; i < kProducts; i++) {
+                    s[i / KS] = Mfma<T>::m32(x[i % kAhead], q[i % KS], i % KS ? s[i / KS] : from);
+                    if (i + kAhead < kProducts) x[i % kAhead] = k_operand(i + kAhead, buffer);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
 #pragma unroll
-            for (int i = 0; i < kProducts - kAhead; i++) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+                for (int i = 0; i < kProducts - kAhead; i++) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
 
-            if (flags & kEdge) {
-                const int32_t j = first_token(t);
-                Seen here = seen;
-                here.high = min(here.high, end_of(flags));
+                if (flags & kEdge) {
+                    const int32_t j = first_token(t);
+                    Seen here = seen;
+                    here.high = min(here.high, end_of(flags));
 #pragma unroll
-                for (int h = 0; h < HT; h++)
+                    for (int h = 0; h < HT; h++)
 #pragma unroll
-                    for (int i = 0; i < 16; i++) {
-                        const int token = 32 * h + 8 * (i / 4) + i % 4; // of the lower half; the upper half's is 4 further, brought by the same wavefront
-                        const bool sees = here.token(j + token + 4 * (int32_t)half) & ((flags >> (token / kTokens) & 1u) != 0);
-                        s[h][i] = sees ? s[h][i] : -INFINITY;
-                    }
-            }
-            float tops[4] = {s[0][0], s[0][1], s[0][2], s[0][3]}; // four chains of comparisons, not one of sixteen
+                        for (int i = 0; i < 16; i++) {
+                            const int token = 32 * h + 8 * (i / 4) + i % 4; // of the lower half; the upper half's is 4 further, brought by the same wavefront
+                            const bool sees = here.token(j + token + 4 * (int32_t)half) & ((flags >> (token / kTokens) & 1u) != 0);
+                            s[h][i] = sees ? s[h][i] : -INFINITY;
+                        }
+                }
+                float tops[4] = {s[0][0], s[0][1], s[0][2], s[0][3]}; // four chains of comparisons, not one of sixteen
 #pragma unroll
-            for (int i = 4; i < 16 * HT; i++) tops[i % 4] = fmaxf(tops[i % 4], s[i / 16][i % 16]);
-            const float top = max_over_32(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+                for (int i = 4; i < 16 * HT; i++) tops[i % 4] = fmaxf(tops[i % 4], s[i / 16][i % 16]);
+                return max_over_32(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+            };
             // Scores come out of the products less a reference, with which the sums begin.  It moves, to the largest score so far, only when one
             // is so far above it that its weight would exceed 2^(kLiftMany + 8): weights stay inside the range of the type, and what has been
-            // added up is scaled now and then, not for every tile.
+            // added up is scaled now and then, not for every tile.  Then the products are made once more from 0: a sum that began with a reference far
+            // below has lost the score's last bits, or all of them (64 keys with scores of -1e9 before ordinary ones).
+            float top = scores(below);
             if (__any(top * a.scale > 8.0f || (!any && top != -INFINITY))) {
-                const float rise = any ? fmaxf(top, 0.0f) : top == -INFINITY ? 0.0f : top;
-                const float fade = any ? exp2_of(-rise * a.scale) : 0.0f;
+                if (__any(any)) top = scores(f32x16{}); // else the reference was 0
+                const float old = -below[0];
+                const float next = any ? fmaxf(old, top) : top == -INFINITY ? 0.0f : top;
+                const float fade = any ? exp2_of((old - next) * a.scale) : 0.0f;
                 any = any || top != -INFINITY;
                 l *= fade;
 #pragma unroll
                 for (int dt = 0; dt < DT; dt++) o[dt] *= fade;
 #pragma unroll
-                for (int h = 0; h < HT; h++) s[h] -= rise;
-                below -= rise;
+                for (int h = 0; h < HT; h++) s[h] -= next;
+                below = f32x16{} - next;
             }
             TV w[kGroups];
 #pragma unroll
