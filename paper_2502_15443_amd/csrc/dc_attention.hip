@@ -964,8 +964,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void dc_attention
     const uint64_t first = ((uint64_t)row * a.n_heads + head) * a.n_slots;
     f32x2 ml = {-INFINITY, 0.0f};
     if (threadIdx.x < a.n_slots) ml = a.partial_ml[first + threadIdx.x];
-    const uint32_t seq = a.batch.sequence_of(row);
-    if (seq >= a.batch.n_seqs || row - a.batch.first_row(seq) >= a.max_new) return;
+    if (a.batch.sequence_of(row, a.max_new) >= a.batch.n_seqs) return;
     float top = max_over_16(ml[0]);
 #pragma unroll
     for (int k = 1; k < 16; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));

@@ -23,7 +23,7 @@ struct AppendArgs {
     const float *cos, *sin;
     const int32_t *position;
     uint64_t k_row, k_head, v_row, v_head, q_row, q_head, q_out_row, q_out_head;
-    uint32_t n_heads, n_kv_heads, rot_dim, n_positions;
+    uint32_t n_heads, n_kv_heads, rot_dim, n_positions, max_new;
 };
 
 template <typename V> __device__ __forceinline__ f32x8 widened(const void *p) { return __builtin_convertvector(*static_cast<const V *>(p), f32x8); }
@@ -37,7 +37,7 @@ template <typename X, typename T, int D, bool NEIGHBOURS, int WAVES> __global__ 
     constexpr uint32_t kUnits = D / 16;
     const uint32_t row = WAVES == 1 ? blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x;
     if (WAVES == 1 && row >= a.batch.n_rows) return;
-    const uint32_t seq = a.batch.sequence_of(row);
+    const uint32_t seq = a.batch.sequence_of(row, a.max_new);
     if (seq >= a.batch.n_seqs) return;
     const uint32_t end = a.batch.rows_end(seq);
     // row - end >= -n_rows and length >= 0: no overflow; negative for rows of a sequence that is shorter than its rows
@@ -169,6 +169,7 @@ extern "C" int dc_kv_append(const dc_kv_cache *cache, const dc_kv_batch *batch, 
     a.q_row = rows->q_row_stride, a.q_head = rows->q_head_stride;
     a.q_out_row = rows->q_out_row_stride, a.q_out_head = rows->q_out_head_stride;
     a.n_heads = rows->n_heads, a.n_kv_heads = cache->n_kv_heads, a.rot_dim = rows->rot_dim, a.n_positions = rows->n_positions;
+    a.max_new = batch->max_new;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const bool neighbours = rows->pairing == DC_ROPE_NEIGHBOURS;
     if (cache->type == DC_TYPE_BF16) launch_x<__bf16>(a, rows->type, d, neighbours, stream);

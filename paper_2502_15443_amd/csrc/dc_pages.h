@@ -45,14 +45,15 @@ struct Batch {
     {
         return (pos < prefix_len ? pos : pos - prefix_len) & ((1u << page_shift) - 1u);
     }
-    // The first sequence that a row belongs to (the same row in all lanes of the wavefront, which are all active); n_seqs if there
-    // is none.
-    __device__ __forceinline__ uint32_t sequence_of(uint32_t row) const
+    // The first sequence that has a row among its first max_new ones (the same row in all lanes of the wavefront, which are all active);
+    // n_seqs if there is none.
+    __device__ __forceinline__ uint32_t sequence_of(uint32_t row, uint32_t max_new) const
     {
         if (!row_start) return row;
         for (uint32_t b = 0; b < n_seqs; b += 64) {
             const uint32_t i = b + (threadIdx.x & 63u);
-            const uint64_t has = __ballot(i < n_seqs && clamped_row(row_start[i]) <= row && clamped_row(row_start[i + 1]) > row);
+            // (a row before the sequence's first is as if very far behind it)
+            const uint64_t has = __ballot(i < n_seqs && row - clamped_row(row_start[i]) < max_new && clamped_row(row_start[i + 1]) > row);
             if (has) return b + (uint32_t)__builtin_ctzll(has);
         }
         return n_seqs;
