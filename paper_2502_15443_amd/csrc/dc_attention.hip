@@ -1061,15 +1061,6 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     const uint64_t row_tiles = !batch->row_start_dev ? batch->n_seqs * seq_tiles : std::min<uint64_t>(all_rows / kTileRows + batch->n_seqs, all_rows);
     const uint64_t tile_many = d == 256 ? 32 : 64;
     const double unit_rate = d == 64 ? 1.5 : d == 128 ? 0.87 : 0.55; // steps a us of a full compute unit in the kernel for many rows
-    // A sequence's many rows read the prefix along with their own pages, with nothing to join then, where the workgroups that this takes beyond those of all
-    // sequences' rows together cost less than the join (their steps taken at 0.57 of the full rate, for launches fill the units unevenly), and where a window
-    // hides most of the prefix.  8 sequences, 8 heads of 128 (us; read whole, and once): 64 rows behind 512 tokens 20 and 24, behind 4096 32.5 and
-    // 30.9; 160 rows 23 and 33, 65 and 56; 400 rows behind 4096 96 and 107, behind 16384 302 and 272; 64 rows with a window of 512 20.5 and 26.5.
-    const uint64_t shared_tiles = (all_rows + kTileRows - 1) / kTileRows;
-    const uint64_t more_tiles = batch->n_seqs * seq_tiles - std::min(batch->n_seqs * seq_tiles, shared_tiles);
-    const double more_time = (double)more_tiles * cache->n_kv_heads * prefix_len / tile_many / (0.57 * 256 * unit_rate);
-    a.whole = prefix_len && own_kind == kTile && (t->window || more_time <= 4 + all_rows * cache->n_kv_heads * (8e-6 * d));
-
     // Of the kernel for few rows: items are workgroups uncut.
     auto cut_few = [&](uint64_t items, uint64_t tokens) {
         constexpr uint64_t tile = 32, least = 4;
@@ -1107,6 +1098,32 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     };
     // what a row, or some rows together, can see
     auto seen = [&](uint64_t tokens, uint64_t rows) { return t->window ? std::min(tokens, (uint64_t)t->window + rows + t->sinks + 64) : tokens; };
+    // a sequence's many rows, over their own pages or over the prefix along with them
+    auto many_part = [&](bool along) {
+        const uint64_t longest = along ? prefix_len + own_len : own_len, rows = kTileRows / group + 1;
+        const uint64_t tokens = seen(longest, rows), fewer = seen(longest > batch->max_new ? longest - batch->max_new : 1, rows);
+        const uint64_t filled = std::max<uint64_t>(1, all_rows / kTileRows); // of the workgroups counted off, about
+        return part(cache->n_kv_heads * row_tiles, tokens, tile_many, cut_many(cache->n_kv_heads * filled, tokens, fewer, a.prefix.blocks != 0), a.prefix.n_splits);
+    };
+    // A sequence's many rows read the prefix along with their own pages where that is estimated to cost less than to read it once for all sequences' rows
+    // together and to join the two.  It costs the steps of the workgroups that it takes beyond those of all rows together, of the prefix only what
+    // the middle one of the longest sequence's rows sees through the window; and it saves the join, or part of it where what it takes is itself
+    // cut and joined.  The two constants beside the measured rates (0.8; 0.4) are fitted to both ways' times at 60 sizes: the slower way is taken
+    // at 5 of them, by 12 % at most.  Heads of 128, 8 of keys and values (us; read along, and once): 8 sequences of 64 rows behind 512 tokens 19 and
+    // 23, behind 4096 32.5 and 30.8; of 160 rows 23 and 33, 65 and 56; of 400 behind 4096 97 and 106, behind 16384 297 and 270; 64 sequences of
+    // 36 rows behind 512 40 and 66, behind 16384 500 and 208, there with a window of 12000 371 and 163, of 1500 54 and 68.
+    if (prefix_len && own_kind == kTile) {
+        const Part along = many_part(true);
+        const uint64_t shared_tiles = (all_rows + kTileRows - 1) / kTileRows;
+        const uint64_t more_tiles = batch->n_seqs * seq_tiles - std::min(batch->n_seqs * seq_tiles, shared_tiles);
+        const int64_t behind = (int64_t)own_len - (int64_t)(batch->max_new + 1) / 2;
+        const uint64_t prefix_seen = t->window ? std::min<uint64_t>(prefix_len, std::max<int64_t>((int64_t)t->window - behind, 0) + t->sinks) : prefix_len;
+        const double more_time = 0.8 * more_tiles * cache->n_kv_heads * prefix_seen / tile_many / (256 * unit_rate);
+        const double parts_time = all_rows * cache->n_kv_heads * (8e-6 * d);
+        const double join_time = 4 + parts_time - (along.n_splits > 1 ? 0.4 * (4 + parts_time * along.n_splits / 4) : 0.0);
+        a.whole = along.blocks && more_time <= join_time;
+        if (a.whole) a.own = along;
+    }
     if (prefix_len && !a.whole) {
         const uint64_t tokens = seen(prefix_len, batch->max_new);
         if (prefix_kind == kTile) {
@@ -1118,10 +1135,7 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
         if (!a.prefix.blocks) return false;
     }
     if (own_kind == kTile) {
-        const uint64_t longest = a.whole ? prefix_len + own_len : own_len, rows = kTileRows / group + 1;
-        const uint64_t tokens = seen(longest, rows), fewer = seen(longest > batch->max_new ? longest - batch->max_new : 1, rows);
-        const uint64_t filled = std::max<uint64_t>(1, all_rows / kTileRows); // of the workgroups counted off, about
-        a.own = part(cache->n_kv_heads * row_tiles, tokens, tile_many, cut_many(cache->n_kv_heads * filled, tokens, fewer, a.prefix.blocks != 0), a.prefix.n_splits);
+        if (!a.whole) a.own = many_part(false);
     } else {
         const uint64_t tokens = seen(own_len, batch->max_new), items = (uint64_t)cache->n_kv_heads * batch->n_seqs;
         a.own = part(items, tokens, 32, cut_few(items, tokens), a.prefix.n_splits);
