@@ -816,20 +816,24 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
             };
             // Scores come out of the products less a reference, with which the sums begin.  It moves, to the largest score so far, only when one
             // is so far above it that its weight would exceed 2^(kLiftMany + 8): weights stay inside the range of the type, and what has been
-            // added up is scaled now and then, not for every tile.  Then the products are made once more from 0: a sum that began with a reference far
-            // below has lost the score's last bits, or all of them (64 keys with scores of -1e9 before ordinary ones).
+            // added up is scaled now and then, not for every tile.  Where it moves by more than 16 powers of two the products are made once more from
+            // 0: a sum that began with a reference far below has lost the score's last bits, or all of them (64 keys with scores of -1e9
+            // before ordinary ones).
             float top = scores(below);
             if (__any(top * a.scale > 8.0f || (!any && top != -INFINITY))) {
-                if (__any(any)) top = scores(f32x16{}); // else the reference was 0
-                const float old = -below[0];
-                const float next = any ? fmaxf(old, top) : top == -INFINITY ? 0.0f : top;
+                const float old = -below[0]; // 0 if no score has been seen
+                const bool again = __any(any && top * a.scale > 16.0f);
+                if (again) top = scores(f32x16{});
+                // by how much the scores go down, which are relative to the old reference or to 0
+                const float shift = any ? fmaxf(top, again ? old : 0.0f) : top == -INFINITY ? 0.0f : top;
+                const float next = again ? shift : old + shift;
                 const float fade = any ? exp2_of((old - next) * a.scale) : 0.0f;
                 any = any || top != -INFINITY;
                 l *= fade;
 #pragma unroll
                 for (int dt = 0; dt < DT; dt++) o[dt] *= fade;
 #pragma unroll
-                for (int h = 0; h < HT; h++) s[h] -= next;
+                for (int h = 0; h < HT; h++) s[h] -= shift;
                 below = f32x16{} - next;
             }
             TV w[kGroups];
