@@ -26,13 +26,16 @@ struct AppendArgs {
     uint32_t n_heads, n_kv_heads, rot_dim, n_positions, max_new;
 };
 
-template <typename V> __device__ __forceinline__ f32x8 widened(const void *p) { return __builtin_convertvector(*static_cast<const V *>(p), f32x8); }
+template <typename X> __device__ __forceinline__ f32x8 widened(const X *p)
+{
+    return __builtin_convertvector(*reinterpret_cast<const typename Vec8<X>::type *>(p), f32x8);
+}
+__device__ __forceinline__ f32x8 widened(const float *p) { return *reinterpret_cast<const f32x8_at16 *>(p); }
 
 // X: type of the rows, T: type of the cache, D: head_dim, NEIGHBOURS: which values are a pair; WAVES: wavefronts that go
 // through all of a row's heads; 0: a workgroup takes as many of a row's heads as it has threads for.
 template <typename X, typename T, int D, bool NEIGHBOURS, int WAVES> __global__ __launch_bounds__(kThreads) void dc_kv_append_kernel(AppendArgs a)
 {
-    typedef typename Vec8<X>::type XV;
     typedef typename Vec8<T>::type TV;
     constexpr uint32_t kUnits = D / 16;
     const uint32_t row = WAVES == 1 ? blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x;
@@ -53,8 +56,8 @@ template <typename X, typename T, int D, bool NEIGHBOURS, int WAVES> __global__ 
         if ((uint32_t)at >= a.n_positions) return;
         if (turns) {
             const uint64_t o = (uint64_t)(uint32_t)at * (a.rot_dim / 2) + 8 * unit;
-            c = *reinterpret_cast<const f32x8 *>(a.cos + o);
-            s = *reinterpret_cast<const f32x8 *>(a.sin + o);
+            c = *reinterpret_cast<const f32x8_at16 *>(a.cos + o);
+            s = *reinterpret_cast<const f32x8_at16 *>(a.sin + o);
         }
     }
     // where the thread's two groups of 8 values begin
@@ -77,7 +80,7 @@ template <typename X, typename T, int D, bool NEIGHBOURS, int WAVES> __global__ 
                                    a.batch.place_in_page((uint32_t)pos)) * D;
         T *dst = is_q ? static_cast<T *>(a.q_out) + row * a.q_out_row + head * a.q_out_head
                       : (is_k ? static_cast<T *>(a.k_pages) : static_cast<T *>(a.v_pages)) + in_pages;
-        f32x8 x = widened<XV>(src + first), y = widened<XV>(src + second);
+        f32x8 x = widened(src + first), y = widened(src + second);
         if (turns && (is_q || is_k)) {
             if (NEIGHBOURS) {
                 f32x8 u, w;

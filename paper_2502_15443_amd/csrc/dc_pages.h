@@ -13,6 +13,7 @@ namespace dcpages {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef f32x8 f32x8_at16 __attribute__((aligned(16))); // in memory: addresses are multiples of 16 bytes, not of the vector's 32
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -20,7 +21,6 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 template <typename T> struct Vec8;
 template <> struct Vec8<__bf16> { typedef bf16x8 type; };
 template <> struct Vec8<_Float16> { typedef f16x8 type; };
-template <> struct Vec8<float> { typedef f32x8 type; };
 
 // The batch as kernels take it.  Whatever the device arrays hold, first_row / rows_end lie in [0, n_rows], length in [0, capacity]
 // and a page that is used in [0, n_pages).
