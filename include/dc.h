@@ -539,7 +539,7 @@ typedef struct {
     uint32_t n_rows;       /* rows in the row buffers; below 2^24 */
     uint32_t max_new;      /* no sequence has more rows than this (more are left alone), 1 .. n_rows */
     uint32_t max_len;      /* about the largest length: work is split by it; results do not depend on it beyond rounding */
-    uint32_t pages_stride; /* entries of a sequence's row of pages_dev; prefix_len + pages_stride * page_tokens < 2^31 */
+    uint32_t pages_stride; /* entries of a sequence's row of pages_dev; prefix_len + pages_stride * page_tokens <= 2^31 - 2^16 */
     uint32_t prefix_len;   /* 0: no common prefix */
     const int32_t *len_dev;          /* n_seqs */
     const int32_t *pages_dev;        /* n_seqs * pages_stride */

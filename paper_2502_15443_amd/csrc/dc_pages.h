@@ -77,7 +77,8 @@ inline bool batch_ok(const dc_kv_cache *c, const dc_kv_batch *b)
         return false;
     if (!b->row_start_dev && (b->n_rows != b->n_seqs || b->max_new != 1)) return false;
     if ((b->prefix_len != 0) != (b->prefix_pages_dev != nullptr)) return false;
-    return (uint64_t)b->prefix_len + (uint64_t)b->pages_stride * c->page_tokens < 0x80000000ull;
+    // kernels reckon with positions some tiles beyond the last one, in 32 bits
+    return (uint64_t)b->prefix_len + (uint64_t)b->pages_stride * c->page_tokens <= 0x7FFF0000ull;
 }
 
 // A row stride and a head stride of rows that are read; of rows that are written, which must not lie over one another.
