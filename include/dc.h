@@ -577,7 +577,7 @@ typedef struct {
     uint32_t n_heads; /* query heads, a multiple of n_kv_heads: query head h reads key/value head h / (n_heads / n_kv_heads) */
     uint32_t window;  /* 0: a row sees all positions j <= p; else p - window < j <= p */
     uint32_t sinks;   /* the first positions j < sinks (j <= p) are seen whatever the window */
-    float scale;      /* finite */
+    float scale;      /* at most 2^127, with either sign */
     const void *q_dev; /* type of the cache; 16-byte aligned, strides as in dc_kv_rows */
     void *out_dev;     /* type of the cache, likewise; not q_dev */
     float *lse_dev;    /* fp32 [n_rows][n_heads], may be NULL */

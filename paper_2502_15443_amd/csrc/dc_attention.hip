@@ -1016,7 +1016,8 @@ bool attention_ok(const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_a
 {
     if (!cache_ok(cache) || !batch_ok(cache, batch) || !t) return false;
     if ((uint64_t)batch->n_rows * t->n_heads >= 0x80000000ull) return false;
-    if (t->n_heads < 1 || t->n_heads > 65535 || t->n_heads % cache->n_kv_heads || !isfinite(t->scale)) return false;
+    if (t->n_heads < 1 || t->n_heads > 65535 || t->n_heads % cache->n_kv_heads) return false;
+    if (!(fabsf(t->scale) <= 0x1p127f)) return false; // scale log2(e) is a number
     return t->q_dev && t->out_dev && t->q_dev != t->out_dev && aligned16(t->q_dev) && aligned16(t->out_dev) && ((uintptr_t)t->lse_dev & 3u) == 0 &&
            strides_ok(t->q_row_stride, t->q_head_stride) &&
            strides_apart(t->out_row_stride, t->out_head_stride, batch->n_rows, t->n_heads, cache->head_dim);
