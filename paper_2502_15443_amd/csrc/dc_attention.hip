@@ -41,8 +41,8 @@ struct AttentionArgs {
     f32x2 *partial_ml; // [row][head][slot]: that maximum (of scores in powers of two) and the sum of the weights
     uint64_t q_row, q_head, out_row, out_head;
     uint32_t n_heads, n_kv_heads, group, window, sinks, max_new, n_slots;
-    float scale;       // not negative; with `negate` of queries that are taken with the other sign
-    bool negate, zero; // scale 0: queries are taken as zeros and scale is 1
+    float scale;       // above 0; with `negate` of queries that are taken with the other sign
+    bool negate;
     bool whole;        // the prefix is read with the sequences' own pages, not as a part of its own
     Part prefix, own;
 };
@@ -301,7 +301,7 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
 #pragma unroll
         for (int s = 0; s < KS; s++) {
             u32x4 x = {};
-            if (is && !a.zero) x = *reinterpret_cast<const u32x4 *>(src + 32 * s);
+            if (is) x = *reinterpret_cast<const u32x4 *>(src + 32 * s);
             if (a.negate) x ^= 0x80008000u;
             q[rt][s] = __builtin_bit_cast(TV, x);
         }
@@ -639,7 +639,7 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
 #pragma unroll
     for (int i = 0; i < KS; i++) {
         u32x4 x = {};
-        if (my_row < n && !a.zero) x = *reinterpret_cast<const u32x4 *>(q_src + 16 * i);
+        if (my_row < n) x = *reinterpret_cast<const u32x4 *>(q_src + 16 * i);
         if (a.negate) x ^= 0x80008000u;
         q[i] = __builtin_bit_cast(TV, x);
     }
@@ -1173,8 +1173,9 @@ extern "C" int dc_attention_paged(const dc_kv_cache *cache, const dc_kv_batch *b
     a.out_row = attention->out_row_stride, a.out_head = attention->out_head_stride;
     a.n_heads = attention->n_heads, a.n_kv_heads = cache->n_kv_heads, a.group = a.n_heads / a.n_kv_heads;
     a.window = attention->window, a.sinks = attention->sinks, a.max_new = batch->max_new;
-    a.negate = attention->scale < 0.0f, a.zero = attention->scale == 0.0f;
-    a.scale = a.zero ? 1.0f : fabsf(attention->scale) * kLog2e;
+    a.negate = attention->scale < 0.0f;
+    // Never 0, which would turn the -infinity of hidden tokens into NaN: the smallest number that there is leaves of any score less than 2^-21.
+    a.scale = std::max(fabsf(attention->scale) * kLog2e, 0x1p-149f);
     uint64_t needed = 0;
     Plan plan;
     if (!make_plan(a, plan, cache, batch, attention, &needed) || (needed && !workspace_dev)) return DC_E_ARG;

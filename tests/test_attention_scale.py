@@ -54,3 +54,28 @@ def test_scales_at_the_ends(type, news, scale):
         # weights 1 and one rounding; a mean of n values in fp32
         assert (np.abs(got[row, 0] - want) <= UNIT[type] * np.abs(want) + 2 * n * 2.0 ** -24 * np.abs(values[:n]).max()).all()
         assert abs(got_lse[row, 0] - lse) <= 8 * 2.0 ** -24 * abs(lse) + 2.0 ** -20
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 256])
+@pytest.mark.parametrize("news,heads", [(5, 2), (140, 1)])  # of each kernel
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_queries_that_are_no_numbers_with_a_scale_of_zero(type, d, news, heads, value):
+    """0 times a score that is no number is none; rows of numbers take the mean of their values."""
+    torch = pytest.importorskip("torch")
+    import numpy as np
+
+    import oracle.attention as oa
+    from tests.attention_cases import check_attend, f64, paged
+    from tests.test_gpu_attention import attend, queries
+
+    print(f"case scale 0 {type} d={d} news={news} {value}", flush=True)
+    p = paged(96, type, 1, d, 16, [200], [news])
+    q = queries(p, heads, type)
+    out, lse, size = oa.attend(f64(p["k"]), f64(p["v"]), p["batch"], f64(q), 0.0)
+    q[2, 0, 5] = value
+    got, got_lse = attend(p, heads, q, 0.0)
+    assert np.isnan(got[2, 0]).all() and np.isnan(got_lse[2, 0])
+    got[2, 0], got_lse[2, 0] = out[2, 0], lse[2, 0]
+    check_attend(type, d, got, got_lse, out, lse, size)
