@@ -1,5 +1,5 @@
 """dc_kv_append and each kernel of dc_attention_paged on pages beyond 2^32 bytes and 2^31 elements of the pools, every result compared; and a
-common prefix some of whose pages are not there."""
+common prefix some of whose pages are not there, or inside which sequences end."""
 import numpy as np
 import pytest
 
@@ -91,3 +91,16 @@ def test_prefix_pages_that_are_not_there(heads, kv_heads, news, gone):
     got, got_lse = attend(p, heads, q, 0.125)
     want = oa.attend(f64(p["k"]), f64(p["v"]), p["batch"], f64(q), 0.125)
     check_attend("bf16", 64, got, got_lse, *want)
+
+
+@pytest.mark.parametrize("heads,kv_heads,d,news", [(4, 2, 64, [1, 3, 1]), (9, 1, 128, [2, 1] * 10), (4, 1, 64, [60, 40, 33]), (2, 1, 256, [70, 64, 5])])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (30, 2)])
+def test_sequences_that_end_inside_the_prefix(heads, kv_heads, d, news, window, sinks):
+    print(f"case ends inside the prefix heads={heads}/{kv_heads} d={d} news={news} window={window}", flush=True)
+    prefix = 150
+    lens = [[140, 150, 75, 170][i % 4] for i in range(len(news))]
+    p = paged(104, "bf16", kv_heads, d, 16, lens, news, prefix)
+    q = queries(p, heads, "bf16")
+    got, got_lse = attend(p, heads, q, 0.125, window, sinks)
+    want = oa.attend(f64(p["k"]), f64(p["v"]), p["batch"], f64(q), 0.125, window, sinks)
+    check_attend("bf16", d, got, got_lse, *want)
