@@ -518,9 +518,10 @@ constexpr uint32_t kTileRows = 128; // of a workgroup of the kernel for many row
 // units bound this kernel.  Keys and values go through the LDS in tiles that its four wavefronts share, double buffered with one barrier a
 // tile; a wavefront owns 32 rows.  The products are those of the kernel for few rows in the 32x32x16 shape: scores as [token][row]
 // = K Q^T, of which a lane holds 16 of 32 tokens of one row, results as [head_dim][row] = V^T P^T; maxima and sums stay in a lane but for one
-// exchange between the halves.  A prompt of 8192 tokens, 32 heads of 128: 559 to 591 us (930 to 980 TFLOP/s; a large library product reaches 1250),
-// the matrix units busy 45 % and the vector units 42 % of the cycles at a clock that falls to 2.0 GHz.  Tiles of 64 tokens are 8 to 20 % faster
-// than of 32, for which alone heads of 256 have registers (560 to 600 TFLOP/s).
+// exchange between the halves.  A prompt of 8192 tokens, 32 heads of 128: 580 to 600 us for as long as it runs (915 to 945 TFLOP/s; a large library
+// product reaches 1250; the first 40 launches after an idle time up to 770 us, while the clock settles), the matrix units busy 45 % and the
+// vector units 43 % of the cycles at a clock that falls to 2.0 GHz.  Tiles of 64 tokens are 8 to 20 % faster than of 32, for which
+// alone heads of 256 have registers (590 to 600 TFLOP/s).
 template <int D> struct TileLds {
     static constexpr int kTile = D == 256 ? 32 : 64; // tokens
     uint8_t k[2][kTile * 2 * D], v[2][kTile * 2 * D];

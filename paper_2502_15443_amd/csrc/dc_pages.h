@@ -22,8 +22,8 @@ template <typename T> struct Vec8;
 template <> struct Vec8<__bf16> { typedef bf16x8 type; };
 template <> struct Vec8<_Float16> { typedef f16x8 type; };
 
-// The batch as kernels take it.  Whatever the device arrays hold, first_row / rows_end lie in [0, n_rows], length in [0, capacity]
-// and a page that is used in [0, n_pages).
+// The batch as kernels take it.  Whatever the device arrays hold, first_row / rows_end lie in [0, n_rows], a length is not negative (callers
+// look up no position at or beyond the capacity) and a page that is used lies in [0, n_pages).
 struct Batch {
     const int32_t *len, *pages, *row_start, *prefix_pages;
     uint32_t n_seqs, n_rows, pages_stride, prefix_len, n_pages, page_shift;

@@ -25,6 +25,21 @@ def test_positions_beyond_the_limit_are_refused(page, prefix):
     dc.attention_paged_workspace(cache, batch, a)
 
 
+@pytest.mark.parametrize("rows,seqs,heads,kv_heads,good", [(2 ** 23, 1, 255, 1, True), (2 ** 23, 1, 256, 1, False), (65535, 65535, 256, 256, True),
+                                                           (65535, 65535, 257, 257, False)])
+def test_batches_that_are_too_large_are_refused(rows, seqs, heads, kv_heads, good):
+    cache = dc.KVCache(ADDR, ADDR, 10, kv_heads, 64, 16, dc.TYPE_BF16)
+    batch = dc.KVBatch(seqs, rows, rows // seqs, 100, ADDR, ADDR, 7, row_start_dev=ADDR)
+    a = dc.Attention(heads, ADDR, 2 * ADDR, None, 0.1, q_strides=(heads * 64, 64), out_strides=(heads * 64, 64))
+    if good:
+        dc.attention_paged_workspace(cache, batch, a)
+        return
+    for call in (lambda: dc.attention_paged_workspace(cache, batch, a), lambda: dc.attention_paged(cache, batch, a, ADDR, 1 << 40)):
+        with pytest.raises(dc.DCError) as e:
+            call()
+        assert e.value.code == -1
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("d", [64, 256])
 @pytest.mark.parametrize("news,window,sinks", [(1, 100, 0), (20, 300, 5), (200, 64, 0), (150, 1, 20)])
