@@ -590,7 +590,8 @@ typedef struct {
  * A row that sees nothing (or only s_j = -inf) has out = 0 and lse = -inf.  What is not seen has no influence, NaN and infinities
  * included: tokens beyond a sequence's length, behind its window, or on pages that are not there may hold anything.
  * Scores, sums and results are held in fp32; exp(s_j - reference) is rounded to the cache's type for the product with the values (f16: to at least
- * 2^-32 of the row's largest, so that many small ones are not lost beside a large one).
+ * 2^-32 of the row's largest, so that many small ones are not lost beside a large one).  The sum of exp(s_j - max s) |v_j| has to stay below 2^120
+ * (bf16 values near the type's largest).
  * A common prefix (prefix_len > 0) is read once for all sequences' rows together, or where that takes longer by each sequence's rows
  * along with its own pages.
  *   workspace_dev   at least dc_attention_paged_workspace() bytes, 16-byte aligned (NULL if that is 0); its contents before the

@@ -519,8 +519,8 @@ constexpr uint32_t kTileRows = 128; // of a workgroup of the kernel for many row
 // tile; a wavefront owns 32 rows.  The products are those of the kernel for few rows in the 32x32x16 shape: scores as [token][row]
 // = K Q^T, of which a lane holds 16 of 32 tokens of one row, results as [head_dim][row] = V^T P^T; maxima and sums stay in a lane but for one
 // exchange between the halves.  A prompt of 8192 tokens, 32 heads of 128: 580 to 600 us for as long as it runs (915 to 945 TFLOP/s; a large library
-// product reaches 1250; the first 40 launches after an idle time up to 770 us, while the clock settles), the matrix units busy 45 % and the
-// vector units 43 % of the cycles at a clock that falls to 2.0 GHz.  Tiles of 64 tokens are 8 to 20 % faster than of 32, for which
+// product reaches 1250; the first 40 launches after an idle time up to 770 us, while the clock settles), the matrix units busy 44 % and the
+// vector units 42 % of the cycles at a clock that falls to 2.0 GHz.  Tiles of 64 tokens are 8 to 20 % faster than of 32, for which
 // alone heads of 256 have registers (590 to 600 TFLOP/s).
 template <int D> struct TileLds {
     static constexpr int kTile = D == 256 ? 32 : 64; // tokens
@@ -1067,6 +1067,7 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     const uint64_t row_tiles = !batch->row_start_dev ? batch->n_seqs * seq_tiles : std::min<uint64_t>(all_rows / kTileRows + batch->n_seqs, all_rows);
     const uint64_t tile_many = d == 256 ? 32 : 64;
     const double unit_rate = d == 64 ? 1.5 : d == 128 ? 0.87 : 0.55; // steps a us of a full compute unit in the kernel for many rows
+
     // Of the kernel for few rows: items are workgroups uncut.
     auto cut_few = [&](uint64_t items, uint64_t tokens) {
         constexpr uint64_t tile = 32, least = 4;
@@ -1114,8 +1115,8 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     // A sequence's many rows read the prefix along with their own pages where that is estimated to cost less than to read it once for all sequences' rows
     // together and to join the two.  It costs the steps of the workgroups that it takes beyond those of all rows together, of the prefix only what
     // the middle one of the longest sequence's rows sees through the window; and it saves the join, or part of it where what it takes is itself
-    // cut and joined.  The two constants beside the measured rates (0.8; 0.4) are fitted to both ways' times at 60 sizes: the slower way is taken
-    // at 5 of them, by 12 % at most.  Heads of 128, 8 of keys and values (us; read along, and once): 8 sequences of 64 rows behind 512 tokens 19 and
+    // cut and joined.  The two constants beside the measured rates (0.8; 0.4) are fitted to both ways' times at 64 sizes: the slower way is taken
+    // at 3 of them, by 12, 1.3 and 0.6 %.  Heads of 128, 8 of keys and values (us; read along, and once): 8 sequences of 64 rows behind 512 tokens 19 and
     // 23, behind 4096 32.5 and 30.8; of 160 rows 23 and 33, 65 and 56; of 400 behind 4096 97 and 106, behind 16384 297 and 270; 64 sequences of
     // 36 rows behind 512 40 and 66, behind 16384 500 and 208, there with a window of 12000 371 and 163, of 1500 54 and 68.
     if (prefix_len && own_kind == kTile) {
