@@ -431,7 +431,7 @@ def plain_tables(st, c):
     starts = torch.cat([st["starts"][:1] * 0, st["new"].clamp(min=0).cumsum(0)]).clamp(max=st["rows"])
     lens = held + starts[1:] - starts[:-1]
     at = P + torch.arange(S, device="cuda") * page  # first position of each entry
-    wanted = at < lens[:, None]
+    wanted = at < (held + st["new"].clamp(min=0))[:, None]
     if c["window"]:
         wanted &= (at + page - 1 > held[:, None] - c["window"]) | (at < c["sinks"])
     before = st["pages_in"]
