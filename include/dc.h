@@ -495,7 +495,7 @@ int dc_gemv_i8(const int8_t *q_dev, const float *row_scale_dev, uint32_t rows, u
                const uint16_t *x_bf16_dev, float *y_f32_dev, uint16_t *y_bf16_dev, void *hip_stream);
 
 /*
- * What a decoder layer does between its products: keys and values in pages, and the attention that reads them
+ * What a decoder layer does between its products: keys and values in pages, the tables of those pages, and the attention that reads them
  * ------------------------------------------------------------------------------------------------------------
  * A layer whose weights stay compressed is run as query/key/value products (dc_decompress_gemv_layer), dc_kv_append,
  * dc_attention_paged, output product, and the feed-forward products.  The two calls here work for one new token a
@@ -503,6 +503,9 @@ int dc_gemv_i8(const int8_t *q_dev, const float *row_scale_dev, uint32_t rows, u
  *
  * Cache.  k_dev and v_dev are pools of n_pages pages; a page holds page_tokens tokens of every key/value head:
  * element [page][head][token][i], i < head_dim, type bf16 or f16.  16-byte aligned; offsets are 64-bit.
+ * A cache of DC_TYPE_I8 holds whole numbers of 8 bits: the value that element [page][head][token][i] stands for is that number times
+ * scale [page][head][token / scale_tokens], of keys in k_scale_dev, of values in v_scale_dev.  Half the room and half the reading of 16 bits.
+ * Scales are numbers above 0 (one that is not, or is NaN, counts as 2^-126).  What calls write as "type of the cache" is rows_type then.
  *
  * Batch.  Sequence b has len_dev[b] tokens, the new ones included; its new tokens are its last ones and their rows
  * (queries, keys, values, results) stand one after the other: rows row_start_dev[b] .. row_start_dev[b+1]-1.
@@ -519,19 +522,25 @@ int dc_gemv_i8(const int8_t *q_dev, const float *row_scale_dev, uint32_t rows, u
 #define DC_TYPE_BF16 0
 #define DC_TYPE_F16 1
 #define DC_TYPE_F32 2 /* rows given to dc_kv_append only */
+#define DC_TYPE_I8 3  /* a cache only: whole numbers of 8 bits, times a scale for each block of tokens of a head */
 
 /* which values of a head turn as a pair, i < rot_dim / 2 */
 #define DC_ROPE_HALVES 0     /* i and i + rot_dim / 2 */
 #define DC_ROPE_NEIGHBOURS 1 /* 2 i and 2 i + 1 */
 
 typedef struct {
-    uint32_t type;        /* DC_TYPE_BF16 or DC_TYPE_F16 */
+    uint32_t type;        /* DC_TYPE_BF16, DC_TYPE_F16 or DC_TYPE_I8 */
     uint32_t n_kv_heads;  /* 1 .. 65535 */
     uint32_t head_dim;    /* 64, 128 or 256 */
     uint32_t page_tokens; /* 16, 32, 64, 128 or 256 */
     uint32_t n_pages;     /* 1 .. 2^31 - 1 */
     void *k_dev;
     void *v_dev;
+    /* of a cache of DC_TYPE_I8; not read for the other types */
+    uint32_t rows_type;    /* DC_TYPE_BF16 or DC_TYPE_F16: turned queries, and the attention's queries and results */
+    uint32_t scale_tokens; /* tokens of a block: 16, 32, 64, 128 or 256, at most page_tokens */
+    float *k_scale_dev;    /* [n_pages][n_kv_heads][page_tokens / scale_tokens] */
+    float *v_scale_dev;
 } dc_kv_cache;
 
 typedef struct {
@@ -569,6 +578,12 @@ typedef struct {
  * rounded.  Queries go to q_out_dev, keys and values into the pages.  A row whose cosines lie outside the table (rot_dim > 0) is
  * left out as a whole, one whose page is not there is not put into the cache.  Positions below prefix_len belong to the prefix
  * and are written there.  Two rows of one call must not share a place in the cache.  One launch.
+ * Into a cache of DC_TYPE_I8, block by block: with A the largest magnitude among the finite values that the call puts into the block (keys as they
+ * are turned, in fp32, each product and each sum rounded), s is the smallest power of two with A <= 127 s, 2^-126 at least; where the block's first
+ * token is not the call's, s is at least the block's scale so far.  A new value x is held as the whole number nearest to x / s (ties to
+ * even), an infinity as 127 with its sign, NaN as 0; if s has grown, the numbers that the block's earlier tokens hold become the nearest ones to what
+ * they stood for.  So a block's scale does not depend on how its tokens were divided into calls.  Earlier tokens are those between the block's first
+ * and the sequence's first new one; tokens behind the new ones are left as they are.  Sequences of one call must not share a block that the call writes.
  * Errors: DC_E_ARG, DC_E_HIP.
  */
 int dc_kv_append(const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_kv_rows *rows, void *hip_stream);
@@ -590,7 +605,8 @@ typedef struct {
  * A row that sees nothing (or only s_j = -inf) has out = 0 and lse = -inf.  What is not seen has no influence, NaN and infinities
  * included: tokens beyond a sequence's length, behind its window, or on pages that are not there may hold anything.
  * Scores, sums and results are held in fp32; exp(s_j - reference) is rounded to the cache's type for the product with the values (f16: to at least
- * 2^-32 of the row's largest, so that many small ones are not lost beside a large one).  The sum of exp(s_j - max s) |v_j| has to stay below 2^120
+ * 2^-32 of the row's largest, so that many small ones are not lost beside a large one).  Over a cache of DC_TYPE_I8 queries and keys enter their product
+ * as they are, and exp(s_j - reference) times the value's scale is rounded to bf16.  The sum of exp(s_j - max s) |v_j| has to stay below 2^120
  * (bf16 values near the type's largest).
  * A common prefix (prefix_len > 0) is read once for all sequences' rows together, or where that takes longer by each sequence's rows
  * along with its own pages.
@@ -603,6 +619,59 @@ int dc_attention_paged_workspace(const dc_kv_cache *cache, const dc_kv_batch *ba
                                  uint64_t *workspace_bytes);
 int dc_attention_paged(const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_attention *attention, void *workspace_dev,
                        uint64_t workspace_bytes, void *hip_stream);
+
+/*
+ * A step's tables: which pages sequences hold, and where their new tokens go
+ * --------------------------------------------------------------------------
+ * A program that serves many sequences knows before a step how many tokens each one holds and how many it gets.  This call makes the arrays
+ * that a dc_kv_batch points to from that, on the device, so that steps can follow one another (and be recorded) without the host.
+ *
+ * Sequence b holds h = held_dev[b] tokens (at least 0) and gets n = new_dev[b]; new_dev[b] < 0: it is over, h = n = 0.  Its entry i covers the
+ * page_tokens positions from f = prefix_len + i * page_tokens on, and is wanted if f < h + n and, with a window, a row from position h on can see
+ * one of them: f + page_tokens - 1 > h - window, or f < sinks.
+ *   - a page that is there (an entry in [0, n_pages)) and wanted stays;
+ *   - one that is there and not wanted goes back to the free pages;
+ *   - one that is not there is taken from the free pages if it is wanted and f >= h: pages that only tokens held before would be on stay away;
+ *   - all other entries become -1.
+ * Free pages are a queue: a ring of n_pages page numbers, queue_in_dev[1] of them from place queue_in_dev[0] on.  Pages are taken from its front in
+ * the order of sequences and entries, and go back to its end in that order; what goes back in a call is not taken in it.  Where none is left entries stay
+ * -1, and queue_dev[2] counts them: the program gives such a sequence's tokens again once there are pages, or ends a sequence.
+ * A program begins with every page in the ring and every entry -1, and holds no page twice; a common prefix's pages are in neither.
+ *
+ * Results: len_dev[b] = h + n (which has to stay below 2^31) and row_start_dev as in dc_kv_batch, rows one after the other.  If the rows are more than n_rows, those
+ * beyond are cut: row starts are at most n_rows, and len_dev[b] counts the rows that there are.  For each row slot_dev (place in the
+ * cache, page * page_tokens + token in the page; -1 if there is none), position_dev, seq_dev; -1 in all three for rows of no sequence.
+ * The order is always the same: equal inputs give equal results.
+ */
+typedef struct {
+    uint32_t n_seqs;       /* 1 .. 65535 */
+    uint32_t n_rows;       /* of the row arrays; 1 .. 2^24 - 1 */
+    uint32_t page_tokens;  /* as in dc_kv_cache */
+    uint32_t pages_stride; /* as in dc_kv_batch; n_seqs * pages_stride < 2^31 */
+    uint32_t n_pages;      /* 1 .. 2^31 - 1 */
+    uint32_t prefix_len;   /* as in dc_kv_batch */
+    uint32_t window, sinks; /* as in dc_attention */
+    const int32_t *held_dev, *new_dev; /* n_seqs */
+    const int32_t *pages_in_dev;       /* n_seqs * pages_stride */
+    const int32_t *prefix_pages_dev;   /* as in dc_kv_batch */
+    const int32_t *queue_in_dev;       /* 2: first place in the ring, number of free pages (taken modulo n_pages, and as at most n_pages) */
+    int32_t *free_dev;                 /* n_pages: the ring, changed where pages go back */
+    int32_t *len_dev;                  /* n_seqs; may be held_dev */
+    int32_t *row_start_dev;            /* n_seqs + 1 */
+    int32_t *pages_dev;                /* n_seqs * pages_stride; may be pages_in_dev */
+    int32_t *queue_dev;                /* 3: first place, number of free pages, pages that were missing; may begin with queue_in_dev */
+    int64_t *slot_dev;                 /* n_rows each; may be NULL */
+    int32_t *position_dev, *seq_dev;
+} dc_kv_requests;
+
+/*
+ *   workspace_dev   at least dc_kv_tables_workspace() bytes, 16-byte aligned; its contents before the call do not matter, and it may be
+ *                   reused once the call's work on the stream is done
+ * Arrays are aligned to their elements.  Whatever they hold, the kernels read and write only inside their stated sizes.
+ * Errors: DC_E_ARG, DC_E_CAP (workspace too small), DC_E_HIP.
+ */
+int dc_kv_tables_workspace(const dc_kv_requests *requests, uint64_t *workspace_bytes);
+int dc_kv_tables(const dc_kv_requests *requests, void *workspace_dev, uint64_t workspace_bytes, void *hip_stream);
 
 /*
  * Plain device copy kernel (reads n bytes, writes n bytes, 16-byte aligned): the denominator for

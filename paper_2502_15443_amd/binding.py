@@ -21,7 +21,7 @@ FORMAT_ID = 5  # DC_FORMAT_ID of include/dc.h
 CHUNK_RAW = 0x80000000
 STATIC_SCRATCH_BYTES = 16 << 20
 TRACE_DECODED, TRACE_COPIED, TRACE_SKIPPED = 0, 1, 2
-TYPE_BF16, TYPE_F16, TYPE_F32 = 0, 1, 2
+TYPE_BF16, TYPE_F16, TYPE_F32, TYPE_I8 = 0, 1, 2, 3
 ROPE_HALVES, ROPE_NEIGHBOURS = 0, 1
 CHUNK_DTYPE = np.dtype([("off", "<u8"), ("comp_bytes", "<u4"), ("raw_bytes_flags", "<u4")])
 
@@ -93,13 +93,17 @@ def _strides(t, given) -> Tuple[int, int]:
 
 
 class KVCache(C.Structure):
-    """Keys and values in pages (dc_kv_cache).  Made once beside the buffers, which it keeps alive."""
+    """Keys and values in pages (dc_kv_cache).  Made once beside the buffers, which it keeps alive.  Of TYPE_I8: int8 pools, fp32 scales
+    [pages, kv_heads, page_tokens // scale_tokens], and the type of queries and results."""
     _fields_ = [("type", C.c_uint32), ("n_kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("page_tokens", C.c_uint32),
-                ("n_pages", C.c_uint32), ("k_dev", C.c_void_p), ("v_dev", C.c_void_p)]
+                ("n_pages", C.c_uint32), ("k_dev", C.c_void_p), ("v_dev", C.c_void_p), ("rows_type", C.c_uint32),
+                ("scale_tokens", C.c_uint32), ("k_scale_dev", C.c_void_p), ("v_scale_dev", C.c_void_p)]
 
-    def __init__(self, k_dev, v_dev, n_pages: int, n_kv_heads: int, head_dim: int, page_tokens: int, type: int = TYPE_BF16):
-        super().__init__(type, n_kv_heads, head_dim, page_tokens, n_pages, _dev(k_dev) or None, _dev(v_dev) or None)
-        self._buffers = (k_dev, v_dev)
+    def __init__(self, k_dev, v_dev, n_pages: int, n_kv_heads: int, head_dim: int, page_tokens: int, type: int = TYPE_BF16, *,
+                 rows_type: int = TYPE_BF16, scale_tokens: int = 0, k_scale_dev=None, v_scale_dev=None):
+        super().__init__(type, n_kv_heads, head_dim, page_tokens, n_pages, _dev(k_dev) or None, _dev(v_dev) or None, rows_type, scale_tokens,
+                         _dev(k_scale_dev) or None, _dev(v_scale_dev) or None)
+        self._buffers = (k_dev, v_dev, k_scale_dev, v_scale_dev)
 
 
 class KVBatch(C.Structure):
@@ -146,6 +150,24 @@ class Attention(C.Structure):
         super().__init__(n_heads, window, sinks, float(scale), _dev(q_dev) or None, _dev(out_dev) or None, _dev(lse_dev) or None,
                          *_strides(q_dev, q_strides), *_strides(out_dev, out_strides))
         self._buffers = (q_dev, out_dev, lse_dev)
+
+
+class KVRequests(C.Structure):
+    """A step's requests and the tables that dc_kv_tables makes of them (dc_kv_requests).  The device arrays may be rewritten between calls."""
+    _fields_ = [("n_seqs", C.c_uint32), ("n_rows", C.c_uint32), ("page_tokens", C.c_uint32), ("pages_stride", C.c_uint32),
+                ("n_pages", C.c_uint32), ("prefix_len", C.c_uint32), ("window", C.c_uint32), ("sinks", C.c_uint32),
+                ("held_dev", C.c_void_p), ("new_dev", C.c_void_p), ("pages_in_dev", C.c_void_p), ("prefix_pages_dev", C.c_void_p),
+                ("queue_in_dev", C.c_void_p), ("free_dev", C.c_void_p), ("len_dev", C.c_void_p), ("row_start_dev", C.c_void_p),
+                ("pages_dev", C.c_void_p), ("queue_dev", C.c_void_p), ("slot_dev", C.c_void_p), ("position_dev", C.c_void_p),
+                ("seq_dev", C.c_void_p)]
+
+    def __init__(self, n_seqs: int, n_rows: int, page_tokens: int, pages_stride: int, n_pages: int, *, held_dev, new_dev, pages_in_dev, queue_in_dev,
+                 free_dev, len_dev, row_start_dev, pages_dev, queue_dev, slot_dev=None, position_dev=None, seq_dev=None, window: int = 0,
+                 sinks: int = 0, prefix_len: int = 0, prefix_pages_dev=None):
+        arrays = (held_dev, new_dev, pages_in_dev, prefix_pages_dev, queue_in_dev, free_dev, len_dev, row_start_dev, pages_dev, queue_dev, slot_dev,
+                  position_dev, seq_dev)
+        super().__init__(n_seqs, n_rows, page_tokens, pages_stride, n_pages, prefix_len, window, sinks, *(_dev(a) or None for a in arrays))
+        self._buffers = arrays
 
 
 def lib_path() -> str:
@@ -229,6 +251,11 @@ def _load():
     L.dc_kv_append.argtypes = [pc, pb, pr, vp]
     L.dc_attention_paged_workspace.restype = i32
     L.dc_attention_paged_workspace.argtypes = [pc, pb, pa, pu64]
+    pq = C.POINTER(KVRequests)
+    L.dc_kv_tables_workspace.restype = i32
+    L.dc_kv_tables_workspace.argtypes = [pq, pu64]
+    L.dc_kv_tables.restype = i32
+    L.dc_kv_tables.argtypes = [pq, vp, u64, vp]
     L.dc_attention_paged.restype = i32
     L.dc_attention_paged.argtypes = [pc, pb, pa, vp, u64, vp]
     L.dc_device_copy.restype = i32
@@ -492,6 +519,17 @@ def attention_paged(cache: KVCache, batch: KVBatch, attention: Attention, worksp
                     stream: int = 0) -> None:
     """dc_attention_paged: attention of the batch's new tokens over the cache."""
     _check(_L.dc_attention_paged(cache, batch, attention, _dev(workspace_dev), workspace_bytes, stream), "dc_attention_paged")
+
+
+def kv_tables_workspace(requests: KVRequests) -> int:
+    n = C.c_uint64(0)
+    _check(_L.dc_kv_tables_workspace(requests, C.byref(n)), "dc_kv_tables_workspace")
+    return int(n.value)
+
+
+def kv_tables(requests: KVRequests, workspace_dev, workspace_bytes: int, stream: int = 0) -> None:
+    """dc_kv_tables: a step's lengths, first rows, tables of pages and places of rows from the tokens that sequences hold and get."""
+    _check(_L.dc_kv_tables(requests, _dev(workspace_dev), workspace_bytes, stream), "dc_kv_tables")
 
 
 def device_copy(src_dev, dst_dev, nbytes: int, stream: int = 0) -> None:

@@ -14,9 +14,11 @@ ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libdc_mi355x.so")
 SOURCES = [os.path.join(PKG, "csrc", "dc_host.cpp"), os.path.join(PKG, "csrc", "dc_decode.hip"),
            os.path.join(PKG, "csrc", "dc_encode.hip"), os.path.join(PKG, "csrc", "dc_probe.hip"),
-           os.path.join(PKG, "csrc", "dc_cache.hip"), os.path.join(PKG, "csrc", "dc_attention.hip")]
+           os.path.join(PKG, "csrc", "dc_cache.hip"), os.path.join(PKG, "csrc", "dc_attention.hip"),
+           os.path.join(PKG, "csrc", "dc_cache_i8.hip"), os.path.join(PKG, "csrc", "dc_attention_i8.hip"),
+           os.path.join(PKG, "csrc", "dc_tables.hip")]
 HEADERS = [os.path.join(ROOT, "include", "dc.h"), os.path.join(PKG, "csrc", "dc_device.h"),
-           os.path.join(PKG, "csrc", "dc_pages.h")]
+           os.path.join(PKG, "csrc", "dc_pages.h"), os.path.join(PKG, "csrc", "dc_attention.h"), os.path.join(PKG, "csrc", "dc_cache.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Packed fp32 VALU forms (v_pk_add_f32, v_pk_mul_f32, v_pk_fma_f32) are kept out of the device code.  The switch

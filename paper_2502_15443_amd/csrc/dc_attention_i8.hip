@@ -1,0 +1,744 @@
+// Attention of new tokens over a paged cache of keys and values held in 8 bits: whole numbers times a scale for each block of tokens of a head.
+//
+// For a row with query q: s_j = scale ks_j (q . k_j), out = sum_j exp(s_j - m) vs_j v_j / sum_j exp(s_j - m) with the running maximum m, where k_j and
+// v_j are the whole numbers and ks_j, vs_j their blocks' scales.  The numbers are exact in bf16 and f16: products are the matrix units' 16-bit ones, on
+// which a key's scale is put after the sum and a value's scale on the weight before it.  A hidden token's numbers are numbers, whatever the cache holds:
+// a weight of 0 keeps it out.
+#include "dc_attention.h"
+
+#include <algorithm>
+
+using namespace dcattn;
+
+namespace {
+
+// 16 whole numbers of 8 bits as T: 8 in each.
+template <typename T> struct Sixteen {
+    u32x4 low, high;
+    __device__ __forceinline__ explicit Sixteen(u32x4 x)
+    {
+        typedef typename Vec8<T>::type TV;
+        f32x8 f[2];
+#pragma unroll
+        for (int i = 0; i < 16; i++) f[i / 8][i % 8] = (float)(int8_t)(x[i / 4] >> (8 * (i % 4)));
+        low = __builtin_bit_cast(u32x4, __builtin_convertvector(f[0], TV)), high = __builtin_bit_cast(u32x4, __builtin_convertvector(f[1], TV));
+    }
+};
+
+// A scale that is read: a number above 0.
+__device__ __forceinline__ float sound_scale(float s) { return fminf(fmaxf(s, 0x1p-126f), 0x1p127f); }
+
+// ---- few rows -------------------------------------------------------------------------------------------------------------
+//
+// At most 16 RT rows (new tokens times the query heads that share a key/value head) read the keys: memory bounds this kernel.  A
+// wavefront takes tiles of 32 tokens.  Scores come as a matrix [token][row] = K Q^T, of which a lane holds 4 tokens of one row in each half of
+// the tile; that is the second operand of [head_dim][row] = V^T P^T if the product's 32 tokens are numbered that way.  K and then V go through
+// registers into the wavefront's own part of the LDS: no barrier in the loop.  The next tile's loads are under way during the rest of the tile's work.
+template <int D, int RT> struct FewLds {
+    static constexpr int kPadded = D + 4; // floats of a row's sums
+    union {
+        uint8_t tokens[4][32 * 2 * D]; // of each wavefront: a tile's keys in 8 bits, then its values in bf16
+        float sums[4][16][kPadded];
+    };
+    float m[4][16 * RT], l[4][16 * RT];
+    int32_t p[16 * RT];
+};
+
+template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(const AttentionArgs &a, FewLds<D, RT> &lds, bool common, uint32_t item)
+{
+    typedef typename Vec8<T>::type TV;
+    constexpr int kTile = 32, KS = D / 32, DT = D / 16;
+    constexpr int kRowBytes = 2 * D, kChunks = D / 16, kRowsALoad = 64 / kChunks, kLoads = kTile / kRowsALoad; // rows: of values; chunks: of 16 bytes
+
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15u, g = lane >> 4;
+    const Part &part = common ? a.prefix : a.own;
+    const uint32_t kv = item % a.n_kv_heads;
+    item /= a.n_kv_heads;
+    const uint32_t seq = common ? 0 : item % a.batch.n_seqs, split = common ? item : item / a.batch.n_seqs;
+    const int32_t *table = common ? a.batch.prefix_pages : a.batch.pages + (uint64_t)seq * a.batch.pages_stride;
+    const uint32_t table_entries = common ? (a.batch.prefix_len + (1u << a.batch.page_shift) - 1) >> a.batch.page_shift : a.batch.pages_stride;
+    // entries of a tile's two halves
+    auto entries_at = [&](uint32_t j, int32_t (&entry)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const uint32_t i = (j + 16 * h) >> a.batch.page_shift;
+            entry[h] = i < table_entries ? table[i] : -1;
+        }
+    };
+    // Without a window it is known at once where a wavefront's first tile is: its pages are asked for together with the sequence's length.
+    int32_t first_entry[2] = {-1, -1};
+    const uint64_t first_tile = (uint64_t)split * part.chunk + wave;
+    if (!a.window && first_tile < 1u << 26) entries_at((uint32_t)first_tile * kTile, first_entry);
+
+    // rows of this workgroup: row_first + i / group of head kv * group + i % group for i < n
+    uint32_t row_first = 0, n;
+    int32_t p_first = 0, there, base = 0, p_min, p_max;
+    if (common) {
+        n = a.batch.n_rows * a.group;
+        there = (int32_t)a.batch.prefix_len;
+        // positions of the rows, sequence by sequence
+        if (threadIdx.x < 16 * RT) lds.p[threadIdx.x] = kNoPosition;
+        __syncthreads();
+        for (uint32_t b = threadIdx.x; b < a.batch.n_seqs; b += 256) {
+            const uint32_t first = a.batch.first_row(b), end = a.batch.rows_end(b);
+            for (uint32_t r = first; r < end; r++) lds.p[r] = a.batch.length(b) - (int32_t)(end - r);
+        }
+        __syncthreads();
+        const int32_t p = lane < min(a.batch.n_rows, 16u * RT) ? lds.p[lane] : kNoPosition;
+        range_of_positions(p, p, p_min, p_max);
+    } else {
+        row_first = a.batch.first_row(seq);
+        const uint32_t end = a.batch.rows_end(seq);
+        const int32_t len = a.batch.length(seq);
+        if (end <= row_first) return;
+        const uint32_t rows = min(end - row_first, a.max_new);
+        n = rows * a.group;
+        base = (int32_t)a.batch.prefix_len;
+        there = min(max(len - base, 0), (int32_t)(a.batch.pages_stride << a.batch.page_shift));
+        p_first = len - (int32_t)(end - row_first);
+        p_min = p_first - base, p_max = p_first + (int32_t)rows - 1 - base;
+    }
+    const Tiles<kTile> tiles(p_min, p_max, there, a.window, (int64_t)a.sinks - base);
+    const int32_t t_begin = (int32_t)min((uint64_t)split * part.chunk, (uint64_t)tiles.count);
+    const int32_t t_end = split + 1 == part.n_splits ? tiles.count : (int32_t)min((uint64_t)t_begin + part.chunk, (uint64_t)tiles.count);
+
+    // queries, and what the lane's rows see
+    TV q[RT][KS];
+    Seen seen[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) {
+        const uint32_t r = rt * 16 + c;
+        const bool is = r < n;
+        const uint32_t i = r / a.group, head = kv * a.group + r % a.group;
+        seen[rt] = Seen(!is ? kNoPosition : common ? lds.p[i] : p_first + (int32_t)i - base, there, a.window, (int64_t)a.sinks - base);
+        // of 64 neighbouring values the lane has 16, for two products: as it has of a key's
+        const T *src = static_cast<const T *>(a.q) + (uint64_t)(row_first + i) * a.q_row + head * a.q_head + 16 * g;
+#pragma unroll
+        for (int s = 0; s < KS; s++) {
+            u32x4 x = {};
+            if (is) x = *reinterpret_cast<const u32x4 *>(src + 64 * (s / 2) + 8 * (s % 2));
+            if (a.negate) x ^= 0x80008000u;
+            q[rt][s] = __builtin_bit_cast(TV, x);
+        }
+    }
+
+    f32x4 o[RT][DT];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) {
+        m[rt] = -INFINITY, l[rt] = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++) o[rt][dt] = f32x4{};
+    }
+
+    const uint64_t page_stride = (uint64_t)a.n_kv_heads << a.batch.page_shift;
+    const uint64_t head_at = (uint64_t)kv << a.batch.page_shift;
+    const uint32_t place_mask = (1u << a.batch.page_shift) - 1u;
+    // page of each half of a tile, -1 where there is none
+    auto pages_from = [&](const int32_t (&entry)[2], int32_t (&page)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) page[h] = __builtin_amdgcn_readfirstlane((uint32_t)entry[h] < a.batch.n_pages ? entry[h] : -1);
+    };
+    auto pages_of = [&](int32_t tile, int32_t (&page)[2]) {
+        int32_t entry[2];
+        entries_at((uint32_t)tiles.first_token(tile), entry);
+        pages_from(entry, page);
+    };
+    // first value of a half's tokens; where there is no page, of page 0, whose tokens are then taken for hidden
+    auto half_at = [&](int32_t j, int32_t page) {
+        return (page_stride * (uint32_t)max(page, 0) + head_at + ((uint32_t)j & place_mask)) * D;
+    };
+    // scales of a tile's halves; a half is inside a block
+    auto scales_of = [&](int32_t j, const int32_t (&page)[2], float (&ks)[2], float (&vs)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const uint64_t at = (((uint64_t)(uint32_t)max(page[h], 0) * a.n_kv_heads + kv) << (a.batch.page_shift - a.block_shift)) +
+                                (((uint32_t)(j + 16 * h) & place_mask) >> a.block_shift);
+            ks[h] = sound_scale(a.k_scales[at]), vs[h] = sound_scale(a.v_scales[at]);
+        }
+    };
+    u32x4 k[kLoads], v[kLoads];
+    // A tile's keys or values in the order of memory, whole tokens side by side; nothing else will ask for them.
+    auto load = [&](u32x4 (&to)[kLoads], const void *pages, int32_t j, const int32_t (&page)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const uint8_t *src = static_cast<const uint8_t *>(pages) + half_at(j + 16 * h, page[h]) + lane * 16;
+#pragma unroll
+            for (int i = 0; i < kLoads / 2; i++) to[h * (kLoads / 2) + i] = dcdev::load16_stream(src + i * 1024);
+        }
+    };
+    // Tokens lie in the LDS with their 16-byte chunks exchanged so that 8 tokens' same chunks, and pairs of chunks, are on different banks.
+    auto swizzle = [](uint32_t row) { return D == 64 ? ((row >> 1) & 3u) << 1 : (row & 7u) << 1; };
+    const uint32_t my_lds = dcdev::lds_address(lds.tokens[wave]);
+    // Keys in 8 bits: 16 tokens' same chunks are on different banks.
+    auto key_swizzle = [](uint32_t row) { return D == 64 ? row >> 2 & 3u : D == 128 ? row >> 1 & 7u : row & 15u; };
+    auto put_keys = [&](const u32x4 (&from)[kLoads]) {
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const uint32_t row = i * kRowsALoad + lane / kChunks, chunk = lane % kChunks;
+            *(lds_u32x4 *)(uintptr_t)(my_lds + row * D + ((chunk ^ key_swizzle(row)) << 4)) = from[i];
+        }
+        __builtin_amdgcn_wave_barrier();
+    };
+    auto put_values = [&](const u32x4 (&from)[kLoads]) {
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const uint32_t row = i * kRowsALoad + lane / kChunks, chunk = 2 * (lane % kChunks);
+            const Sixteen<__bf16> x(from[i]);
+            *(lds_u32x4 *)(uintptr_t)(my_lds + row * kRowBytes + ((chunk ^ swizzle(row)) << 4)) = x.low;
+            *(lds_u32x4 *)(uintptr_t)(my_lds + row * kRowBytes + (((chunk + 1) ^ swizzle(row)) << 4)) = x.high;
+        }
+        __builtin_amdgcn_wave_barrier();
+    };
+
+    int32_t page[2], next_page[2];
+    float ks[2], vs[2], next_ks[2], next_vs[2];
+    int32_t t = t_begin + (int32_t)wave;
+    if (t < t_end) {
+        if (a.window) pages_of(t, page);
+        else pages_from(first_entry, page);
+        const int32_t j = tiles.first_token(t);
+        load(k, a.k_pages, j, page);
+        load(v, a.v_pages, j, page);
+        scales_of(j, page, ks, vs);
+        pages_of(min(t + 4, t_end - 1), next_page);
+    }
+    for (; t < t_end; t += 4) {
+        const int32_t j = tiles.first_token(t);
+        const bool more = t + 4 < t_end;
+        const int32_t next_j = tiles.first_token(min(t + 4, t_end - 1));
+
+        put_keys(k);
+        if (more) {
+            load(k, a.k_pages, next_j, next_page);
+            scales_of(next_j, next_page, next_ks, next_vs);
+        }
+        f32x4 s[RT][2];
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+#pragma unroll
+            for (int rt = 0; rt < RT; rt++) s[rt][h] = f32x4{};
+#pragma unroll
+            for (int i = 0; i < KS / 2; i++) {
+                const uint32_t row = 16 * h + c, chunk = 4 * i + g;
+                const Sixteen<T> x(*(const lds_u32x4 *)(uintptr_t)(my_lds + row * D + ((chunk ^ key_swizzle(row)) << 4)));
+#pragma unroll
+                for (int rt = 0; rt < RT; rt++) {
+                    s[rt][h] = Mfma<T>::m16(__builtin_bit_cast(TV, x.low), q[rt][2 * i], s[rt][h]);
+                    s[rt][h] = Mfma<T>::m16(__builtin_bit_cast(TV, x.high), q[rt][2 * i + 1], s[rt][h]);
+                }
+            }
+#pragma unroll
+            for (int rt = 0; rt < RT; rt++) s[rt][h] *= ks[h];
+        }
+        __builtin_amdgcn_wave_barrier();
+
+        // tokens that not all rows see
+        const bool edge = page[0] < 0 || page[1] < 0 || j + kTile > p_min + 1 || j + kTile > tiles.high || (j < tiles.low && j + kTile > tiles.sinks) ||
+                          (a.window && j + kTile > tiles.sinks && (int64_t)j <= (int64_t)p_max - a.window);
+        put_values(v);
+        if (more) load(v, a.v_pages, next_j, next_page);
+
+        bf16x8 w[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; rt++) {
+            if (edge) {
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const bool sees = seen[rt].token(j + 16 * h + 4 * (int32_t)g + i) & (page[h] >= 0);
+                        s[rt][h][i] = sees ? s[rt][h][i] : -INFINITY;
+                    }
+            }
+            float top = fmaxf(fmaxf(fmaxf(s[rt][0][0], s[rt][0][1]), fmaxf(s[rt][0][2], s[rt][0][3])),
+                              fmaxf(fmaxf(s[rt][1][0], s[rt][1][1]), fmaxf(s[rt][1][2], s[rt][1][3])));
+            top = fmaxf(m[rt], max_over_16(top));
+            const float ref = top == -INFINITY ? 0.0f : top;
+            const float fade = exp2_of((m[rt] - ref) * a.scale);
+            m[rt] = top;
+            f32x8 e;
+#pragma unroll
+            for (int i = 0; i < 8; i++) e[i] = exp2_of((s[rt][i / 4][i % 4] - ref) * a.scale);
+            l[rt] = l[rt] * fade + (((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
+#pragma unroll
+            for (int i = 0; i < 8; i++) e[i] *= vs[i / 4];
+            w[rt] = __builtin_convertvector(e, bf16x8);
+#pragma unroll
+            for (int dt = 0; dt < DT; dt++) o[rt][dt] *= fade;
+        }
+        const uint32_t i4 = c >> 2, half8 = (c & 1u) << 3;
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++) {
+            const uint32_t row = 4 * g + i4, chunk = 2 * dt + ((c & 3u) >> 1);
+            const uint32_t at = my_lds + row * kRowBytes + ((chunk ^ swizzle(row)) << 4) + half8;
+            const u32x2 lo = lds_column4(at), hi = lds_column4(at + 16 * kRowBytes);
+            const u32x4 x = {lo[0], lo[1], hi[0], hi[1]};
+#pragma unroll
+            for (int rt = 0; rt < RT; rt++) o[rt][dt] = Mfma<__bf16>::m16(__builtin_bit_cast(bf16x8, x), w[rt], o[rt][dt]);
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int h = 0; h < 2; h++) page[h] = next_page[h], ks[h] = next_ks[h], vs[h] = next_vs[h];
+        if (more) pages_of(min(t + 8, t_end - 1), next_page);
+    }
+
+    // the wavefronts' sums, brought to one maximum and added up in their order
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) {
+        l[rt] = sum_over_16(l[rt]);
+        m[rt] *= a.scale; // what the weights are relative to
+        if (l[rt] != l[rt] && m[rt] == -INFINITY) m[rt] = 0.0f; // saw scores, none of them a number
+        if (g == 0) lds.m[wave][rt * 16 + c] = m[rt], lds.l[wave][rt * 16 + c] = l[rt];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) {
+        const uint32_t r = rt * 16 + c;
+        const float top = fmaxf(fmaxf(lds.m[0][r], lds.m[1][r]), fmaxf(lds.m[2][r], lds.m[3][r]));
+        const float f = m[rt] == -INFINITY ? 0.0f : exp2_of(m[rt] - top);
+        if (rt) __syncthreads();
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++)
+            *reinterpret_cast<f32x4 *>(&lds.sums[wave][c][16 * dt + 4 * g]) = m[rt] == -INFINITY ? f32x4{} : o[rt][dt] * f;
+        __syncthreads();
+        constexpr uint32_t kQuads = D / 4;
+        for (uint32_t i = threadIdx.x; i < 16 * kQuads; i += 256) {
+            const uint32_t col = i / kQuads, at = i % kQuads * 4, rr = rt * 16 + col;
+            if (rr >= n) continue;
+            const float big = fmaxf(fmaxf(lds.m[0][rr], lds.m[1][rr]), fmaxf(lds.m[2][rr], lds.m[3][rr]));
+            f32x4 sum = {};
+            float total = 0.0f;
+#pragma unroll
+            for (int w4 = 0; w4 < 4; w4++) {
+                sum += *reinterpret_cast<const f32x4 *>(&lds.sums[w4][col][at]);
+                if (lds.m[w4][rr] != -INFINITY) total += lds.l[w4][rr] * exp2_of(lds.m[w4][rr] - big);
+            }
+            store_result<T, D>(a, row_first + rr / a.group, kv * a.group + rr % a.group, part.first_slot + split, at, sum, big, total);
+        }
+    }
+}
+
+// ---- many rows ------------------------------------------------------------------------------------------------------------
+//
+// A workgroup owns 128 rows of one key/value head (prompts, or the rows of many sequences behind a common prefix): the matrix
+// units bound this kernel.  Keys and values go through the LDS in tiles that its four wavefronts share, made 16 bits wide on their way, double buffered
+// with one barrier a tile; a wavefront owns 32 rows.  Scores as [token][row] = K Q^T, results as [head_dim][row] = V^T P^T in the 32x32x16 shape; maxima and
+// sums stay in a lane but for one exchange between the halves.
+template <int D> struct TileLds {
+    static constexpr int kTile = D == 256 ? 32 : 64; // tokens
+    uint8_t k[2][kTile * 2 * D], v[2][kTile * 2 * D];
+    int32_t p[kTileRows];
+    f32x2 scale[2][4]; // of the tokens that each wavefront brings: of keys in units of the scores' powers of two, of values
+};
+
+template <typename T, int D> __device__ __forceinline__ void many_rows(const AttentionArgs &a, TileLds<D> &lds, bool common, uint32_t block)
+{
+    typedef typename Vec8<T>::type TV;
+    constexpr int kTile = TileLds<D>::kTile, KS = D / 16, DT = D / 32, HT = kTile / 32; // HT: 32-token products of a tile
+    constexpr uint32_t kRows = kTileRows, kRowBytes = 2 * D, kChunks = D / 16, kRowsALoad = 64 / kChunks; // rows: in the LDS; chunks: of 16 bytes in the cache
+    constexpr int kTokens = kTile / 4, kLoads = kTokens / (int)kRowsALoad; // tokens that a wavefront brings, in so many loads
+    constexpr uint32_t kBuffer = kTile * kRowBytes;
+
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31u, half = lane >> 5;
+    const Part &part = common ? a.prefix : a.own;
+    uint32_t item = part.blocks - 1 - block; // the last rows, which see most, first
+    const uint32_t kv = a.n_kv_heads - 1 - item % a.n_kv_heads;
+    item /= a.n_kv_heads;
+    const uint32_t split = part.n_splits - 1 - item % part.n_splits;
+    uint32_t tile = item / part.n_splits;
+
+    // rows of this workgroup: i_first <= i < n of the sequence's (the batch's) rows, row_first + i / group of head kv * group + i % group
+    uint32_t row_first = 0, n = 0, seq = 0;
+    int32_t there = (int32_t)a.batch.prefix_len; // positions below it are, or may be, in the cache
+    int32_t p_first = 0;                         // of the sequence's first row
+    if (common) {
+        n = a.batch.n_rows * a.group;
+    } else {
+        // a lane to a sequence: how many workgroups it has, and so whose this one is
+        bool found = false;
+        uint32_t end = 0;
+        int32_t len = 0;
+        if (a.batch.row_start) {
+            for (uint32_t b = 0; b < a.batch.n_seqs && !found; b += 64) {
+                const uint32_t s = min(b + lane, a.batch.n_seqs - 1), first_s = a.batch.first_row(s), end_s = a.batch.rows_end(s);
+                const int32_t len_s = a.batch.length(s);
+                const uint32_t tiles = b + lane < a.batch.n_seqs && end_s > first_s ? (min(end_s - first_s, a.max_new) * a.group + kRows - 1) / kRows : 0;
+                const uint32_t upto = dcdev::lanes_prefix_sum<false>(tiles);
+                const uint64_t beyond = __ballot(upto > tile);
+                if (beyond) {
+                    const int l = __builtin_ctzll(beyond);
+                    seq = b + (uint32_t)l;
+                    tile -= (uint32_t)__builtin_amdgcn_readlane((int)(upto - tiles), l);
+                    row_first = (uint32_t)__builtin_amdgcn_readlane((int)first_s, l);
+                    end = (uint32_t)__builtin_amdgcn_readlane((int)end_s, l);
+                    len = __builtin_amdgcn_readlane(len_s, l);
+                    found = true;
+                } else {
+                    tile -= (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+                }
+            }
+        } else {
+            const uint32_t tiles = (a.group + kRows - 1) / kRows;
+            seq = tile / tiles, tile %= tiles;
+            found = seq < a.batch.n_seqs;
+            if (found) row_first = seq, end = seq + 1, len = a.batch.length(seq);
+        }
+        if (!found) return;
+        seq = __builtin_amdgcn_readfirstlane(seq), tile = __builtin_amdgcn_readfirstlane(tile);
+        n = min(end - row_first, a.max_new) * a.group;
+        p_first = len - (int32_t)(end - row_first);
+        there = max(there, min(len, a.batch.capacity()));
+    }
+    const uint32_t i_first = tile * kRows;
+
+    // positions of the rows: of a sequence they follow from one another; of the batch they are gathered, sequence by sequence
+    int32_t p_min, p_max, wave_p_min, wave_p_max, my_p;
+    const uint32_t my_row = i_first + wave * 32 + c;
+    if (common) {
+        for (uint32_t i = threadIdx.x; i < kRows; i += 256) lds.p[i] = kNoPosition;
+        __syncthreads();
+        const uint32_t r_low = i_first / a.group, r_high = min((i_first + kRows - 1) / a.group + 1, a.batch.n_rows);
+        for (uint32_t b = threadIdx.x; b < a.batch.n_seqs; b += 256) {
+            const uint32_t first = a.batch.first_row(b), end = a.batch.rows_end(b);
+            const int32_t len = first < end ? a.batch.length(b) : 0;
+            for (uint32_t r = max(first, r_low); r < min(end, r_high); r++)
+                for (uint32_t i = max(r * a.group, i_first); i < min((r + 1) * a.group, i_first + kRows); i++) lds.p[i - i_first] = len - (int32_t)(end - r);
+        }
+        __syncthreads();
+        const int32_t p0 = lds.p[lane], p1 = lds.p[lane + 64];
+        range_of_positions(p0 == kNoPosition ? p1 : p1 == kNoPosition ? p0 : min(p0, p1), max(p0, p1), p_min, p_max);
+        const int32_t p = lds.p[wave * 32 + c];
+        range_of_positions(p, p, wave_p_min, wave_p_max);
+        my_p = lds.p[wave * 32 + c];
+    } else {
+        auto position = [&](uint32_t i) { return i < n ? p_first + (int32_t)(i / a.group) : kNoPosition; };
+        const uint32_t wave_first = i_first + wave * 32;
+        p_min = position(i_first), p_max = position(min(i_first + kRows, n) - 1);
+        wave_p_min = position(wave_first), wave_p_max = wave_first < n ? position(min(wave_first + 32, n) - 1) : kNoPosition;
+        my_p = position(my_row);
+    }
+    // The tiles of the common prefix, if it is this launch's to read here, and behind them those of the sequence's own pages, whose first token
+    // is at `base`.  Positions count from the sequence's first token, but in the two tables of pages.
+    const int32_t base = (int32_t)a.batch.prefix_len;
+    auto beyond = [&](int32_t p) { return (int32_t)max((int64_t)p - base, (int64_t)-1); };
+    const Tiles<kTile> prefix_tiles(p_min, p_max, common || a.whole ? base : 0, a.window, a.sinks);
+    const Tiles<kTile> own_tiles(beyond(p_min), beyond(p_max), common ? 0 : there - base, a.window, (int64_t)a.sinks - base);
+    const int32_t count = prefix_tiles.count + own_tiles.count;
+    const int32_t t_begin = (int32_t)min((uint64_t)split * part.chunk, (uint64_t)count);
+    const int32_t t_end = split + 1 == part.n_splits ? count : (int32_t)min((uint64_t)t_begin + part.chunk, (uint64_t)count);
+    auto first_token = [&](int32_t t) { return t < prefix_tiles.count ? prefix_tiles.first_token(t) : base + own_tiles.first_token(t - prefix_tiles.count); };
+    const Seen all_last(p_max, there, a.window, a.sinks); // of the workgroup's rows
+    const Seen first_sees(wave_p_min, there, a.window, a.sinks), last_sees(wave_p_max, there, a.window, a.sinks); // of the wavefront's
+
+    const uint32_t my_head = kv * a.group + my_row % a.group;
+    const uint64_t my_packed = row_first + my_row / a.group;
+    const Seen seen(my_p, there, a.window, a.sinks);
+    TV q[KS];
+    f32x16 o[DT];
+    float ref = 0.0f; // what the weights are relative to, in powers of two
+    bool any = false; // a score has been seen
+    float l = 0.0f;
+    const T *q_src = static_cast<const T *>(a.q) + my_packed * a.q_row + my_head * a.q_head + 8 * half;
+#pragma unroll
+    for (int i = 0; i < KS; i++) {
+        u32x4 x = {};
+        if (my_row < n) x = *reinterpret_cast<const u32x4 *>(q_src + 16 * i);
+        if (a.negate) x ^= 0x80008000u;
+        q[i] = __builtin_bit_cast(TV, x);
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; dt++) o[dt] = f32x16{};
+
+    const int32_t *prefix_table = a.batch.prefix_pages, *own_table = a.batch.pages + (uint64_t)seq * a.batch.pages_stride;
+    const uint64_t page_stride = (uint64_t)a.n_kv_heads << a.batch.page_shift;
+    const uint64_t head_at = (uint64_t)kv << a.batch.page_shift;
+    const uint32_t place_mask = (1u << a.batch.page_shift) - 1u;
+    // What there is to know of 16 tiles, 16 tiles ahead: lane l has, of tile i + l / 4 counted from t_begin, where the tokens that wavefront l mod 4
+    // brings lie in the pools (in bytes; where there is no page, those of page 0, which are then taken for hidden), and the tile's
+    // flags.  A tile's step takes its own with three reads of a lane.  (Scalar loads would do for the pages, but the LDS's data are waited
+    // for by the same counter, all of it.)
+    enum : uint32_t {
+        kThere = 15,    // a bit for each wavefront's tokens: they are there
+        kPrefix = 16,   // of the prefix's table
+        kSome = 64,     // this wavefront's rows see some of it,
+        kEdge = 128     // and not all of it
+    };
+    struct Known {
+        uint32_t low, high, flags;
+        float ks, vs;
+    };
+    auto pages_from = [&](int32_t i) {
+        const int32_t t = t_begin + i + (int32_t)(lane >> 2), j = first_token(t) + (int32_t)(lane & 3u) * kTokens;
+        const bool in_prefix = t < prefix_tiles.count;
+        int32_t e = -1;
+        if (t < t_end && j < (in_prefix ? base : all_last.high)) e = in_prefix ? prefix_table[(uint32_t)j >> a.batch.page_shift] : own_table[(uint32_t)(j - base) >> a.batch.page_shift];
+        return (uint32_t)e < a.batch.n_pages ? e : -1;
+    };
+    auto known_from = [&](int32_t i, int32_t page) {
+        const int32_t t = t_begin + i + (int32_t)(lane >> 2), j = first_token(t);
+        const bool in_prefix = t < prefix_tiles.count;
+        const uint32_t place = (uint32_t)(j + (int32_t)(lane & 3u) * kTokens - (in_prefix ? 0 : base)) & place_mask;
+        const uint64_t token = page_stride * (uint32_t)max(page, 0) + head_at + place, at = token * D;
+        const uint32_t there4 = (uint32_t)(__ballot(page >= 0) >> (lane & 60u)) & 15u;
+        const bool whole = there4 == 15u && (!in_prefix || j + kTile <= base);
+        const bool some = t < t_end && j < last_sees.high && (j + kTile > first_sees.low || j < last_sees.sinks);
+        const bool edge = !whole || j + kTile > first_sees.high || (j < last_sees.low && j + kTile > first_sees.sinks);
+        return Known{(uint32_t)at, (uint32_t)(at >> 32), there4 | (in_prefix ? kPrefix : 0u) | (some ? kSome : 0u) | (edge ? kEdge : 0u),
+                     a.k_scales[token >> a.block_shift], a.v_scales[token >> a.block_shift]};
+    };
+    int32_t pages_ahead = pages_from(0);
+    Known known = known_from(0, pages_ahead);
+    pages_ahead = pages_from(16);
+    auto flags_of = [&](int32_t i) { return (uint32_t)__builtin_amdgcn_readlane((int)known.flags, 4 * (i & 15)); };
+    // tokens from here on are not of the tile's table
+    auto end_of = [&](uint32_t flags) { return flags & kPrefix ? base : 0x7FFFFFFF; };
+    u32x4 k_new[kLoads], v_new[kLoads];
+    const uint32_t lane_at = lane * 16;
+    auto bring = [&](int32_t i) {
+        const int32_t l = 4 * (i & 15) + (int32_t)wave;
+        const uint64_t at = (uint32_t)__builtin_amdgcn_readlane((int)known.low, l) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)known.high, l) << 32;
+        const uint8_t *k_at = static_cast<const uint8_t *>(a.k_pages) + at, *v_at = static_cast<const uint8_t *>(a.v_pages) + at;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) k_new[i] = *reinterpret_cast<const u32x4 *>(k_at + lane_at + i * 1024);
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) v_new[i] = *reinterpret_cast<const u32x4 *>(v_at + lane_at + i * 1024);
+    };
+    // Keys and values lie in the LDS in 16 bits, of which a chunk of the cache gives two chunks.  The 16-byte chunks of a token lie exchanged in the LDS, so that 16 tokens' same chunks are on different banks, and the same four of 4 tokens'.
+    auto swizzle = [](uint32_t token) {
+        return D == 64 ? (token >> 1 & 1u) << 2 | (token >> 2 & 3u) : (token & 3u) << 2 | (token >> 2 & 3u);
+    };
+    const uint32_t lds_k = dcdev::lds_address(&lds) + offsetof(TileLds<D>, k), lds_v = dcdev::lds_address(&lds) + offsetof(TileLds<D>, v);
+    // where a lane puts what it brings, and where it reads its part of the first operands
+    uint32_t put_at[kLoads][2], k_at[KS], v_at[DT][2];
+#pragma unroll
+    for (int i = 0; i < kLoads; i++)
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const uint32_t token = wave * kTokens + i * kRowsALoad + lane / kChunks, chunk = 2 * (lane % kChunks) + h;
+            put_at[i][h] = token * kRowBytes + ((chunk ^ swizzle(token)) << 4);
+        }
+#pragma unroll
+    for (int i = 0; i < KS; i++) k_at[i] = c * kRowBytes + (((2 * i + half) ^ swizzle(c)) << 4);
+#pragma unroll
+    for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const uint32_t i16 = lane & 15u, token = 4 * half + (i16 >> 2) + 8 * h, chunk = 4 * dt + 2 * (lane >> 4 & 1u) + (i16 >> 1 & 1u);
+            v_at[dt][h] = token * kRowBytes + ((chunk ^ swizzle(token)) << 4) + (i16 & 1u) * 8;
+        }
+    auto put = [&](int32_t i, uint32_t buffer) {
+        const int32_t l = 4 * (i & 15) + (int32_t)wave;
+        const float ks = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(known.ks), l));
+        const float vs = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(known.vs), l));
+        if (lane == 0) lds.scale[buffer][wave] = f32x2{fminf(fmaxf(sound_scale(ks) * a.scale, 0x1p-149f), 0x1p127f), sound_scale(vs)};
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const Sixteen<T> k(k_new[i]);
+            const Sixteen<__bf16> v(v_new[i]);
+            *(lds_u32x4 *)(uintptr_t)(lds_k + buffer * kBuffer + put_at[i][0]) = k.low;
+            *(lds_u32x4 *)(uintptr_t)(lds_k + buffer * kBuffer + put_at[i][1]) = k.high;
+            *(lds_u32x4 *)(uintptr_t)(lds_v + buffer * kBuffer + put_at[i][0]) = v.low;
+            *(lds_u32x4 *)(uintptr_t)(lds_v + buffer * kBuffer + put_at[i][1]) = v.high;
+        }
+    };
+    auto k_operand = [&](int i, uint32_t buffer) {
+        return __builtin_bit_cast(TV, *(const lds_u32x4 *)(uintptr_t)(lds_k + buffer * kBuffer + 32 * (i / KS) * kRowBytes + k_at[i % KS]));
+    };
+    auto v_operand = [&](int i, uint32_t buffer) {
+        const u32x2 lo = lds_column4(lds_v + buffer * kBuffer + 16 * (i / DT) * kRowBytes + v_at[i % DT][0]);
+        const u32x2 hi = lds_column4(lds_v + buffer * kBuffer + 16 * (i / DT) * kRowBytes + v_at[i % DT][1]);
+        return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+    };
+
+    // A step works on tile t, whose keys and values are in buffer B, while the next tile's go from registers into the other buffer and those
+    // of the tile behind it are asked for.
+    uint32_t flags = 0, flags_next = 0; // of tiles t and t + 1
+    auto step = [&](auto B, int32_t t) {
+        constexpr uint32_t buffer = decltype(B)::value;
+        constexpr int kProducts = HT * KS, kGroups = 2 * HT, kAhead = 4;
+        if (t + 1 < t_end) {
+            put(t + 1 - t_begin, buffer ^ 1u);
+        }
+        const int32_t i_after = t + 2 - t_begin;
+        if ((i_after & 15) == 0) {
+            known = known_from(i_after, pages_ahead);
+            pages_ahead = pages_from(i_after + 16);
+        }
+        const uint32_t flags_after = flags_of(i_after);
+        if (t + 2 < t_end) bring(i_after);
+
+        // a wavefront whose rows see nothing of the tile has nothing to do
+        if (flags & kSome) {
+            f32x16 s[HT];
+            f32x2 scale[2 * HT]; // of 16 tokens each
+#pragma unroll
+            for (int i = 0; i < 2 * HT; i++) scale[i] = lds.scale[buffer][i * (16 / kTokens)];
+            TV x[kAhead];
+            // The operands come out of the LDS several products ahead of their use.
+#pragma unroll
+            for (int i = 0; i < kAhead; i++) x[i] = k_operand(i, buffer);
+#pragma unroll
+            for (int i = 0; i < kProducts; i++) {
+                s[i / KS] = Mfma<T>::m32(x[i % kAhead], q[i % KS], i % KS ? s[i / KS] : f32x16{});
+                if (i + kAhead < kProducts) x[i % kAhead] = k_operand(i + kAhead, buffer);
+            }
+            if (flags & kEdge) {
+                const int32_t j = first_token(t);
+                Seen here = seen;
+                here.high = min(here.high, end_of(flags));
+#pragma unroll
+                for (int h = 0; h < HT; h++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) {
+                        const int token = 32 * h + 8 * (i / 4) + i % 4; // of the lower half; the upper half's is 4 further, brought by the same wavefront
+                        const bool sees = here.token(j + token + 4 * (int32_t)half) & ((flags >> (token / kTokens) & 1u) != 0);
+                        s[h][i] = sees ? s[h][i] : -INFINITY;
+                    }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < 2 * HT; u++) {
+                float tops[2] = {s[u / 2][8 * (u % 2)], s[u / 2][8 * (u % 2) + 1]};
+#pragma unroll
+                for (int i = 2; i < 8; i++) tops[i % 2] = fmaxf(tops[i % 2], s[u / 2][8 * (u % 2) + i]);
+                top = fmaxf(top, fmaxf(tops[0], tops[1]) * scale[u][0]);
+            }
+            top = max_over_32(top);
+            // The reference moves, to the largest score so far, only when one is so far above it that its weight would exceed 2^8: what has been
+            // added up is scaled now and then, not for every tile.
+            if (__any(top - ref > 8.0f || (!any && top != -INFINITY))) {
+                const float next = any ? fmaxf(ref, top) : top == -INFINITY ? 0.0f : top;
+                const float fade = any ? exp2_of(ref - next) : 0.0f;
+                any = any || top != -INFINITY;
+                l *= fade;
+#pragma unroll
+                for (int dt = 0; dt < DT; dt++) o[dt] *= fade;
+                ref = next;
+            }
+            bf16x8 w[kGroups], y[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; i++) y[i] = v_operand(i, buffer);
+#pragma unroll
+            for (int u = 0; u < kGroups; u++) {
+                f32x8 e;
+#pragma unroll
+                for (int i = 0; i < 8; i++) e[i] = exp2_of(__builtin_fmaf(s[u / 2][8 * (u % 2) + i], scale[u][0], -ref));
+                l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+                w[u] = __builtin_convertvector(e * scale[u][1], bf16x8);
+            }
+#pragma unroll
+            for (int i = 0; i < kGroups * DT; i++) {
+                o[i % DT] = Mfma<__bf16>::m32(y[i % kAhead], w[i / DT], o[i % DT]);
+                if (i + kAhead < kGroups * DT) y[i % kAhead] = v_operand(i + kAhead, buffer);
+            }
+        }
+        flags = flags_next, flags_next = flags_after;
+        __syncthreads();
+    };
+
+    if (t_begin < t_end) {
+        flags = flags_of(0), flags_next = flags_of(1);
+        bring(0);
+        put(0, 0);
+        if (t_begin + 1 < t_end) bring(1);
+    }
+    __syncthreads();
+    for (int32_t t = t_begin; t < t_end; t += 2) {
+        step(std::integral_constant<uint32_t, 0>{}, t);
+        if (t + 1 < t_end) step(std::integral_constant<uint32_t, 1>{}, t + 1);
+    }
+
+    const f32x2 both = swapped32(l);
+    const float total = both[0] + both[1];
+    // what the weights are relative to (also if the row saw scores and none was a number)
+    const float top = any || total != total ? ref : -INFINITY;
+    if (my_row >= n) return;
+    uint32_t row = my_row; // where the results go is worked out here, not kept in registers from the beginning
+    dcdev::anew(row);
+    const uint32_t packed = row_first + row / a.group, head = kv * a.group + row % a.group;
+    auto sums = [&](int dt, int b) { return f32x4{o[dt][4 * b], o[dt][4 * b + 1], o[dt][4 * b + 2], o[dt][4 * b + 3]}; };
+    if (a.n_slots == 1) {
+        typedef T T4 __attribute__((ext_vector_type(4)));
+        T *out = static_cast<T *>(a.out) + packed * a.out_row + head * a.out_head + 4 * half;
+        const float r = 1.0f / total;
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+            for (int b = 0; b < 4; b++) *reinterpret_cast<T4 *>(out + 32 * dt + 8 * b) = __builtin_convertvector(total == 0.0f ? f32x4{} : sums(dt, b) * r, T4);
+        if (a.lse && half == 0) a.lse[(uint64_t)packed * a.n_heads + head] = total == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
+    } else {
+        const uint64_t i = ((uint64_t)packed * a.n_heads + head) * a.n_slots + part.first_slot + split;
+        float *out = a.partial + i * D + 4 * half;
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+            for (int b = 0; b < 4; b++) *reinterpret_cast<f32x4 *>(out + 32 * dt + 8 * b) = sums(dt, b);
+        if (half == 0) a.partial_ml[i] = f32x2{top, total};
+    }
+}
+
+template <int D> constexpr int workgroups_a_unit() { return D == 256 ? 1 : D == 64 ? 3 : 2; }
+
+template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void dc_attention_i8_few_kernel(AttentionArgs a)
+{
+    __shared__ __align__(16) FewLds<D, RT> lds;
+    const bool common = blockIdx.x < a.prefix.blocks;
+    few_rows<T, D, RT>(a, lds, common, common ? blockIdx.x : blockIdx.x - a.prefix.blocks);
+}
+
+template <typename T, int D> __global__ __launch_bounds__(256, workgroups_a_unit<D>()) void dc_attention_i8_tile_kernel(AttentionArgs a)
+{
+    __shared__ __align__(16) TileLds<D> lds;
+    const bool common = blockIdx.x < a.prefix.blocks;
+    many_rows<T, D>(a, lds, common, common ? blockIdx.x : blockIdx.x - a.prefix.blocks);
+}
+
+// A common prefix with many rows and few rows in each sequence, the two kinds of workgroups in turn by eights (a workgroup's XCD is its number modulo 8,
+// and those of one key/value head's prefix stay on one).
+template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void dc_attention_i8_both_kernel(AttentionArgs a)
+{
+    __shared__ __align__(16) union {
+        FewLds<D, RT> few;
+        TileLds<D> many;
+    } lds;
+    const uint32_t eight = blockIdx.x >> 3, prefix_eights = (a.prefix.blocks + 7) / 8, own_eights = (a.own.blocks + 7) / 8, less = min(prefix_eights, own_eights);
+    const bool common = eight < 2 * less ? (eight & 1u) == 0 : prefix_eights > own_eights;
+    const uint32_t block = (eight < 2 * less ? eight / 2 : eight - less) * 8 + (blockIdx.x & 7u);
+    if (common) {
+        if (block < a.prefix.blocks) many_rows<T, D>(a, lds.many, true, block);
+    } else {
+        if (block < a.own.blocks) few_rows<T, D, RT>(a, lds.few, false, block);
+    }
+}
+
+template <typename T, int D> void launch(const AttentionArgs &a, const Plan &plan, hipStream_t stream)
+{
+    const dim3 threads(256);
+    if (a.prefix.blocks && plan.prefix_kind == kTile && plan.own_kind != kTile) {
+        const dim3 grid(8 * ((a.prefix.blocks + 7) / 8 + (a.own.blocks + 7) / 8));
+        if (plan.own_kind == kFew16) hipLaunchKernelGGL((dc_attention_i8_both_kernel<T, D, 1>), grid, threads, 0, stream, a);
+        else if constexpr (D < 256) hipLaunchKernelGGL((dc_attention_i8_both_kernel<T, D, 2>), grid, threads, 0, stream, a);
+    } else { // a sequence's rows are never more than the batch's: both parts are of the kind of their rows together, or the prefix is alone
+        const Kind kind = a.prefix.blocks ? std::max(plan.prefix_kind, plan.own_kind) : plan.own_kind;
+        const dim3 grid(a.prefix.blocks + a.own.blocks);
+        if (kind == kFew16) hipLaunchKernelGGL((dc_attention_i8_few_kernel<T, D, 1>), grid, threads, 0, stream, a);
+        else if (kind == kTile) hipLaunchKernelGGL((dc_attention_i8_tile_kernel<T, D>), grid, threads, 0, stream, a);
+        else if constexpr (D < 256) hipLaunchKernelGGL((dc_attention_i8_few_kernel<T, D, 2>), grid, threads, 0, stream, a);
+    }
+}
+
+template <typename T> void launch_d(const AttentionArgs &a, const Plan &plan, uint32_t head_dim, hipStream_t stream)
+{
+    if (head_dim == 64) launch<T, 64>(a, plan, stream);
+    else if (head_dim == 128) launch<T, 128>(a, plan, stream);
+    else launch<T, 256>(a, plan, stream);
+}
+
+} // namespace
+
+void dcattn::launch_i8(const AttentionArgs &a, const Plan &plan, uint32_t rows_type, uint32_t head_dim, hipStream_t stream)
+{
+    if (rows_type == DC_TYPE_BF16) launch_d<__bf16>(a, plan, head_dim, stream);
+    else launch_d<_Float16>(a, plan, head_dim, stream);
+}

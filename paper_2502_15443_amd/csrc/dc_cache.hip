@@ -7,30 +7,11 @@
 // 16-byte accesses each way, no exchange between lanes, and queries may be turned in place.  Results are stored past the caches'
 // keeping: 2048 fp32 rows of 96 heads of 128 take 24.0 instead of 27.0 us (6.3 TB/s), 8192 rows of 120 in 16 bits 98 instead of 101 (5.2).
 // (Loads that way gain only where the rows are more than the caches hold, and lose up to a fifth below.)
-#include "dc_device.h"
-#include "dc_pages.h"
+#include "dc_cache.h"
 
-using namespace dcpages;
+using namespace dccache;
 
 namespace {
-
-constexpr uint32_t kThreads = 256;
-
-struct AppendArgs {
-    Batch batch;
-    const void *k, *v, *q;
-    void *k_pages, *v_pages, *q_out;
-    const float *cos, *sin;
-    const int32_t *position;
-    uint64_t k_row, k_head, v_row, v_head, q_row, q_head, q_out_row, q_out_head;
-    uint32_t n_heads, n_kv_heads, rot_dim, n_positions, max_new;
-};
-
-template <typename X> __device__ __forceinline__ f32x8 widened(const X *p)
-{
-    return __builtin_convertvector(*reinterpret_cast<const typename Vec8<X>::type *>(p), f32x8);
-}
-__device__ __forceinline__ f32x8 widened(const float *p) { return *reinterpret_cast<const f32x8_at16 *>(p); }
 
 // X: type of the rows, T: type of the cache, D: head_dim, NEIGHBOURS: which values are a pair; WAVES: wavefronts that go
 // through all of a row's heads; 0: a workgroup takes as many of a row's heads as it has threads for.
@@ -156,7 +137,7 @@ extern "C" int dc_kv_append(const dc_kv_cache *cache, const dc_kv_batch *batch, 
             !strides_ok(rows->q_row_stride, rows->q_head_stride) ||
             !strides_apart(rows->q_out_row_stride, rows->q_out_head_stride, batch->n_rows, rows->n_heads, d))
             return DC_E_ARG;
-        if (rows->q_dev == rows->q_out_dev && (rows->type != cache->type || rows->q_row_stride != rows->q_out_row_stride ||
+        if (rows->q_dev == rows->q_out_dev && (rows->type != rows_type_of(cache) || rows->q_row_stride != rows->q_out_row_stride ||
                                                rows->q_head_stride != rows->q_out_head_stride))
             return DC_E_ARG;
     }
@@ -175,7 +156,10 @@ extern "C" int dc_kv_append(const dc_kv_cache *cache, const dc_kv_batch *batch, 
     a.max_new = batch->max_new;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const bool neighbours = rows->pairing == DC_ROPE_NEIGHBOURS;
-    if (cache->type == DC_TYPE_BF16) launch_x<__bf16>(a, rows->type, d, neighbours, stream);
+    if (cache->type == DC_TYPE_I8) {
+        a.k_scales = cache->k_scale_dev, a.v_scales = cache->v_scale_dev, a.block_shift = shift_of(cache->scale_tokens);
+        launch_i8(a, rows->type, cache->rows_type, d, neighbours, stream);
+    } else if (cache->type == DC_TYPE_BF16) launch_x<__bf16>(a, rows->type, d, neighbours, stream);
     else launch_x<_Float16>(a, rows->type, d, neighbours, stream);
     return dc_launch_status();
 }

@@ -62,13 +62,21 @@ struct Batch {
 
 inline bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 
+inline bool page_tokens_ok(uint32_t n) { return n >= 16 && n <= 256 && (n & (n - 1)) == 0; }
+
 inline bool cache_ok(const dc_kv_cache *c)
 {
-    return c && (c->type == DC_TYPE_BF16 || c->type == DC_TYPE_F16) && c->n_kv_heads >= 1 && c->n_kv_heads <= 65535 &&
-           (c->head_dim == 64 || c->head_dim == 128 || c->head_dim == 256) && c->page_tokens >= 16 && c->page_tokens <= 256 &&
-           (c->page_tokens & (c->page_tokens - 1)) == 0 && c->n_pages >= 1 && c->n_pages <= 0x7FFFFFFFu && c->k_dev && c->v_dev &&
-           aligned16(c->k_dev) && aligned16(c->v_dev);
+    if (!c || (c->type != DC_TYPE_BF16 && c->type != DC_TYPE_F16 && c->type != DC_TYPE_I8) || c->n_kv_heads < 1 || c->n_kv_heads > 65535 ||
+        (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) || !page_tokens_ok(c->page_tokens) || c->n_pages < 1 ||
+        c->n_pages > 0x7FFFFFFFu || !c->k_dev || !c->v_dev || !aligned16(c->k_dev) || !aligned16(c->v_dev))
+        return false;
+    return c->type != DC_TYPE_I8 || ((c->rows_type == DC_TYPE_BF16 || c->rows_type == DC_TYPE_F16) && page_tokens_ok(c->scale_tokens) &&
+                                     c->scale_tokens <= c->page_tokens && c->k_scale_dev && c->v_scale_dev &&
+                                     ((uintptr_t)c->k_scale_dev & 3u) == 0 && ((uintptr_t)c->v_scale_dev & 3u) == 0);
 }
+
+// Type of turned queries and of the attention's queries and results.
+inline uint32_t rows_type_of(const dc_kv_cache *c) { return c->type == DC_TYPE_I8 ? c->rows_type : c->type; }
 
 inline bool batch_ok(const dc_kv_cache *c, const dc_kv_batch *b)
 {
