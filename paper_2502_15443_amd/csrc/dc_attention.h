@@ -191,6 +191,9 @@ struct Plan {
     Kind prefix_kind, own_kind;
 };
 
+// Tokens of a tile of the kernel for few rows over a cache of 8 bits: 64, or with 32 rows, which leave fewer registers, 32.
+constexpr int few_tile(int row_tiles) { return row_tiles == 1 ? 64 : 32; }
+
 // The kernels over a cache of 8 bits; joining, where results are in parts, is the caller's.
 void launch_i8(const AttentionArgs &a, const Plan &plan, uint32_t rows_type, uint32_t head_dim, hipStream_t stream);
 

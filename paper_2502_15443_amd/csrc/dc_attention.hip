@@ -894,12 +894,14 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     // upper bound of the workgroups' number, as the kernel counts them off
     const uint64_t row_tiles = !batch->row_start_dev ? batch->n_seqs * seq_tiles : std::min<uint64_t>(all_rows / kTileRows + batch->n_seqs, all_rows);
     const uint64_t tile_many = d == 256 ? 32 : 64;
+    const Kind few_kind = prefix_len && prefix_kind != kTile ? prefix_kind : own_kind; // of the kernel for few rows, if one runs
+    const uint64_t tile_few = cache->type == DC_TYPE_I8 ? few_tile(few_kind == kFew16 ? 1 : 2) : 32;
     const double unit_rate = d == 64 ? 1.5 : d == 128 ? 0.87 : 0.55; // steps a us of a full compute unit in the kernel for many rows
 
     // Of the kernel for few rows: items are workgroups uncut.
     auto cut_few = [&](uint64_t items, uint64_t tokens) {
-        constexpr uint64_t tile = 32, least = 4;
-        const uint64_t n_tiles = (tokens + tile - 1) / tile, most = std::max<uint64_t>(1, std::min<uint64_t>((n_tiles + least - 1) / least, kMostSplits));
+        constexpr uint64_t least = 4;
+        const uint64_t n_tiles = (tokens + tile_few - 1) / tile_few, most = std::max<uint64_t>(1, std::min<uint64_t>((n_tiles + least - 1) / least, kMostSplits));
         // Up to three tiles to a wavefront, parts gain less than it costs to join them (8 heads, 200 tokens: 6.9 us, in parts 8.5; 400: 9.0 and 8.7).
         if (!prefix_len && n_tiles <= 12) return (uint64_t)1;
         uint64_t n = 1;
@@ -965,7 +967,7 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
             const uint64_t items = cache->n_kv_heads * ((all_rows + kTileRows - 1) / kTileRows);
             a.prefix = part(items, tokens, tile_many, cut_many(items, tokens, tokens, true), 0);
         } else {
-            a.prefix = part(cache->n_kv_heads, tokens, 32, cut_few(cache->n_kv_heads, tokens), 0);
+            a.prefix = part(cache->n_kv_heads, tokens, tile_few, cut_few(cache->n_kv_heads, tokens), 0);
         }
         if (!a.prefix.blocks) return false;
     }
@@ -973,7 +975,7 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
         if (!a.whole) a.own = many_part(false);
     } else {
         const uint64_t tokens = seen(own_len, batch->max_new), items = (uint64_t)cache->n_kv_heads * batch->n_seqs;
-        a.own = part(items, tokens, 32, cut_few(items, tokens), a.prefix.n_splits);
+        a.own = part(items, tokens, tile_few, cut_few(items, tokens), a.prefix.n_splits);
     }
     if (!a.own.blocks || (uint64_t)a.own.blocks + a.prefix.blocks >= 1u << 24) return false;
     a.n_slots = a.prefix.n_splits + a.own.n_splits;

@@ -1,9 +1,9 @@
 // Attention of new tokens over a paged cache of keys and values held in 8 bits: whole numbers times a scale for each block of tokens of a head.
 //
 // For a row with query q: s_j = scale ks_j (q . k_j), out = sum_j exp(s_j - m) vs_j v_j / sum_j exp(s_j - m) with the running maximum m, where k_j and
-// v_j are the whole numbers and ks_j, vs_j their blocks' scales.  The numbers are exact in bf16 and f16: products are the matrix units' 16-bit ones, on
-// which a key's scale is put after the sum and a value's scale on the weight before it.  A hidden token's numbers are numbers, whatever the cache holds:
-// a weight of 0 keeps it out.
+// v_j are the whole numbers and ks_j, vs_j their blocks' scales.  The numbers are exact in f16: products are the matrix units' f16 ones, also of bf16 queries;
+// a key's scale is put on the sum, a value's scale on the weight before its product.  A hidden token's numbers are numbers, whatever the cache holds: a weight of
+// 0 keeps it out.
 #include "dc_attention.h"
 
 #include <algorithm>
@@ -12,32 +12,107 @@ using namespace dcattn;
 
 namespace {
 
-// 16 whole numbers of 8 bits as T: 8 in each.
-template <typename T> struct Sixteen {
-    u32x4 low, high;
-    __device__ __forceinline__ explicit Sixteen(u32x4 x)
-    {
-        typedef typename Vec8<T>::type TV;
-        f32x8 f[2];
-#pragma unroll
-        for (int i = 0; i < 16; i++) f[i / 8][i % 8] = (float)(int8_t)(x[i / 4] >> (8 * (i % 4)));
-        low = __builtin_bit_cast(u32x4, __builtin_convertvector(f[0], TV)), high = __builtin_bit_cast(u32x4, __builtin_convertvector(f[1], TV));
-    }
-};
+// 4 whole numbers of 8 bits in f16: with its sign bit turned a byte is 128 more, as the low byte of an f16 between 1024 and 2048 it is exact, and less 1152 it is
+// the number.  5 operations; conversions byte by byte take 6.
+__device__ __forceinline__ u32x2 four_f16(uint32_t x)
+{
+    const uint32_t more = x ^ 0x80808080u;
+    const f16x2 less = {(_Float16)1152.0f, (_Float16)1152.0f};
+    const f16x2 low = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, more, 0x04010400u)) - less;
+    const f16x2 high = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, more, 0x04030402u)) - less;
+    return u32x2{__builtin_bit_cast(uint32_t, low), __builtin_bit_cast(uint32_t, high)};
+}
+__device__ __forceinline__ u32x4 eight_f16(uint32_t x, uint32_t y)
+{
+    const u32x2 a = four_f16(x), b = four_f16(y);
+    return u32x4{a[0], a[1], b[0], b[1]};
+}
+
+// Of 8 rows of 16 values of 8 bits that the 16 lanes name (half a row each), lane i gets column i.
+__device__ __forceinline__ u32x2 lds_column8(uint32_t addr)
+{
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2 *)(uintptr_t)addr));
+}
 
 // A scale that is read: a number above 0.
 __device__ __forceinline__ float sound_scale(float s) { return fminf(fmaxf(s, 0x1p-126f), 0x1p127f); }
 
+// Queries as f16.  Those of bf16 are brought to a largest one of 2^14 to 2^15 by a power of two, of which the score gets the reciprocal: the 8 bits of
+// all that are above 2^-29 times the largest stay as they are, and those below are off by 2^-40 of it at most, far less than the sum's own roundings.
+// `most`: largest of the row's values, as bits without sign.
+template <typename T> struct Queries;
+template <> struct Queries<_Float16> {
+    float back = 1.0f;
+    __device__ __forceinline__ explicit Queries(uint32_t) {}
+    __device__ __forceinline__ f16x8 operator()(u32x4 x) const { return __builtin_bit_cast(f16x8, x); }
+};
+template <> struct Queries<__bf16> {
+    float by, back;
+    __device__ __forceinline__ explicit Queries(uint32_t most)
+    {
+        const uint32_t e = min(268u - (most >> 7), 253u); // 2^(e - 127): reciprocals are numbers too
+        by = __uint_as_float(e << 23), back = __uint_as_float((254u - e) << 23);
+    }
+    __device__ __forceinline__ f16x8 operator()(u32x4 x) const
+    {
+        return __builtin_convertvector(__builtin_convertvector(__builtin_bit_cast(bf16x8, x), f32x8) * by, f16x8);
+    }
+};
+// Largest of 16-bit values without their signs.
+__device__ __forceinline__ uint32_t largest(uint32_t m, const u32x4 &x)
+{
+    u16x2 v = {(uint16_t)m, 0};
+#pragma unroll
+    for (int i = 0; i < 4; i++) v = __builtin_elementwise_max(v, __builtin_bit_cast(u16x2, x[i] & 0x7FFF7FFFu));
+    return max((uint32_t)v[0], (uint32_t)v[1]);
+}
+
+// Largest over the lanes with the same number modulo 16 (32).
+__device__ __forceinline__ uint32_t largest_over_32(uint32_t v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return max(r[0], r[1]);
+}
+__device__ __forceinline__ uint32_t largest_over_16(uint32_t v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return largest_over_32(max(r[0], r[1]));
+}
+
+// Weights go into the product with the values as f16, times the value's scale over the largest scale so far (as a power of two, at least 2^-100) and
+// times 2^kLift: f16 loses bits below 2^-14 and everything below 2^-25, and its largest value is 2^16.  In the kernel for few rows a weight is at most
+// 1, in the one for many 2^8.
+constexpr int kLiftFew = 15, kLiftMany = 7;
+struct ValueScale {
+    uint32_t ref; // bits of the largest scale so far, rounded up to a power of two
+    __device__ __forceinline__ ValueScale() : ref(27u << 23) {}
+    __device__ __forceinline__ float value() const { return __uint_as_float(ref); }
+    // by what weights are multiplied
+    template <int LIFT> __device__ __forceinline__ float by() const { return __uint_as_float(((254u + LIFT) << 23) - ref); }
+    // takes another scale in; true if the reference has grown, and by what sums are multiplied then
+    __device__ __forceinline__ bool grows(uint32_t scale_bits, float &fade)
+    {
+        const uint32_t up = (scale_bits + 0x7FFFFFu) & 0x7F800000u;
+        if (up <= ref) return false;
+        fade = __uint_as_float((uint32_t)max((int32_t)((127u << 23) + ref - up), 0));
+        ref = up;
+        return true;
+    }
+};
+
 // ---- few rows -------------------------------------------------------------------------------------------------------------
 //
 // At most 16 RT rows (new tokens times the query heads that share a key/value head) read the keys: memory bounds this kernel.  A
-// wavefront takes tiles of 32 tokens.  Scores come as a matrix [token][row] = K Q^T, of which a lane holds 4 tokens of one row in each half of
-// the tile; that is the second operand of [head_dim][row] = V^T P^T if the product's 32 tokens are numbered that way.  K and then V go through
-// registers into the wavefront's own part of the LDS: no barrier in the loop.  The next tile's loads are under way during the rest of the tile's work.
+// wavefront takes tiles of 64 tokens.  Scores come as a matrix [token][row] = K Q^T, of which a lane holds 4 tokens of one row in each quarter of
+// the tile; two quarters are the second operand of [head_dim][row] = V^T P^T if the product's 32 tokens are numbered that way.  K and then V go through
+// registers into the wavefront's own part of the LDS, as bytes, and become f16 on their way to the products: of K a lane reads 16 neighbouring values of a
+// token, for two products; of V the transposing read gives it 8 tokens of one value.  No barrier in the loop; the next tile's loads are under way during the
+// rest of the tile's work.
 template <int D, int RT> struct FewLds {
     static constexpr int kPadded = D + 4; // floats of a row's sums
     union {
-        uint8_t tokens[4][32 * 2 * D]; // of each wavefront: a tile's keys in 8 bits, then its values in bf16
+        uint8_t tokens[4][few_tile(RT) * D]; // of each wavefront: a tile's keys, then its values
         float sums[4][16][kPadded];
     };
     float m[4][16 * RT], l[4][16 * RT];
@@ -46,9 +121,8 @@ template <int D, int RT> struct FewLds {
 
 template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(const AttentionArgs &a, FewLds<D, RT> &lds, bool common, uint32_t item)
 {
-    typedef typename Vec8<T>::type TV;
-    constexpr int kTile = 32, KS = D / 32, DT = D / 16;
-    constexpr int kRowBytes = 2 * D, kChunks = D / 16, kRowsALoad = 64 / kChunks, kLoads = kTile / kRowsALoad; // rows: of values; chunks: of 16 bytes
+    constexpr int kTile = few_tile(RT), kQuarters = kTile / 16, KS = D / 32, DT = D / 16;
+    constexpr int kChunks = D / 16, kTokensALoad = 64 / kChunks, kLoads = kTile / kTokensALoad; // chunks: of 16 bytes
 
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15u, g = lane >> 4;
     const Part &part = common ? a.prefix : a.own;
@@ -57,18 +131,15 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
     const uint32_t seq = common ? 0 : item % a.batch.n_seqs, split = common ? item : item / a.batch.n_seqs;
     const int32_t *table = common ? a.batch.prefix_pages : a.batch.pages + (uint64_t)seq * a.batch.pages_stride;
     const uint32_t table_entries = common ? (a.batch.prefix_len + (1u << a.batch.page_shift) - 1) >> a.batch.page_shift : a.batch.pages_stride;
-    // entries of a tile's two halves
-    auto entries_at = [&](uint32_t j, int32_t (&entry)[2]) {
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const uint32_t i = (j + 16 * h) >> a.batch.page_shift;
-            entry[h] = i < table_entries ? table[i] : -1;
-        }
+    // the table's entry of 16 tokens of a tile, in each lane that of the 16 with its number modulo kQuarters
+    auto entry_at = [&](uint32_t j) {
+        const uint32_t i = (j + 16 * (lane % kQuarters)) >> a.batch.page_shift;
+        return i < table_entries ? table[i] : -1;
     };
     // Without a window it is known at once where a wavefront's first tile is: its pages are asked for together with the sequence's length.
-    int32_t first_entry[2] = {-1, -1};
+    int32_t first_entry = -1;
     const uint64_t first_tile = (uint64_t)split * part.chunk + wave;
-    if (!a.window && first_tile < 1u << 26) entries_at((uint32_t)first_tile * kTile, first_entry);
+    if (!a.window && first_tile < 1u << 25) first_entry = entry_at((uint32_t)first_tile * kTile);
 
     // rows of this workgroup: row_first + i / group of head kv * group + i % group for i < n
     uint32_t row_first = 0, n;
@@ -103,7 +174,8 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
     const int32_t t_end = split + 1 == part.n_splits ? tiles.count : (int32_t)min((uint64_t)t_begin + part.chunk, (uint64_t)tiles.count);
 
     // queries, and what the lane's rows see
-    TV q[RT][KS];
+    f16x8 q[RT][KS];
+    float row_scale[RT]; // of the scores as they come out of the products, times their keys' scales: to powers of two
     Seen seen[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) {
@@ -113,13 +185,19 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
         seen[rt] = Seen(!is ? kNoPosition : common ? lds.p[i] : p_first + (int32_t)i - base, there, a.window, (int64_t)a.sinks - base);
         // of 64 neighbouring values the lane has 16, for two products: as it has of a key's
         const T *src = static_cast<const T *>(a.q) + (uint64_t)(row_first + i) * a.q_row + head * a.q_head + 16 * g;
+        u32x4 x[KS];
+        uint32_t most = 0;
 #pragma unroll
         for (int s = 0; s < KS; s++) {
-            u32x4 x = {};
-            if (is) x = *reinterpret_cast<const u32x4 *>(src + 64 * (s / 2) + 8 * (s % 2));
-            if (a.negate) x ^= 0x80008000u;
-            q[rt][s] = __builtin_bit_cast(TV, x);
+            x[s] = u32x4{};
+            if (is) x[s] = *reinterpret_cast<const u32x4 *>(src + 64 * (s / 2) + 8 * (s % 2));
+            if (a.negate) x[s] ^= 0x80008000u;
+            most = largest(most, x[s]);
         }
+        const Queries<T> as_f16(largest_over_16(most));
+        row_scale[rt] = fminf(fmaxf(a.scale * as_f16.back, 0x1p-149f), 0x1p127f);
+#pragma unroll
+        for (int s = 0; s < KS; s++) q[rt][s] = as_f16(x[s]);
     }
 
     f32x4 o[RT][DT];
@@ -131,163 +209,171 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
         for (int dt = 0; dt < DT; dt++) o[rt][dt] = f32x4{};
     }
 
-    const uint64_t page_stride = (uint64_t)a.n_kv_heads << a.batch.page_shift;
+    const uint64_t page_stride = (uint64_t)a.n_kv_heads << a.batch.page_shift; // in tokens of a head
     const uint64_t head_at = (uint64_t)kv << a.batch.page_shift;
     const uint32_t place_mask = (1u << a.batch.page_shift) - 1u;
-    // page of each half of a tile, -1 where there is none
-    auto pages_from = [&](const int32_t (&entry)[2], int32_t (&page)[2]) {
-#pragma unroll
-        for (int h = 0; h < 2; h++) page[h] = __builtin_amdgcn_readfirstlane((uint32_t)entry[h] < a.batch.n_pages ? entry[h] : -1);
+    auto page_from = [&](int32_t entry) { return (uint32_t)entry < a.batch.n_pages ? entry : -1; };
+    auto page_of = [&](int32_t page, int quarter) { return __builtin_amdgcn_readlane(page, quarter); };
+    // Scales of a tile: the first kQuarters lanes have those of the keys, the next ones those of the values; 16 tokens are inside a block.
+    const float *scales = lane & kQuarters ? a.v_scales : a.k_scales;
+    // Of tokens that no row sees they may be anything.
+    auto sound_of = [&](int32_t j, int32_t page, float scale) {
+        const int32_t first = j + 16 * (int32_t)(lane % kQuarters);
+        const bool some = (page >= 0) & (first < tiles.high) & ((first + 16 > tiles.low) | (first < tiles.sinks));
+        return some ? sound_scale(scale) : 0x1p-126f;
     };
-    auto pages_of = [&](int32_t tile, int32_t (&page)[2]) {
-        int32_t entry[2];
-        entries_at((uint32_t)tiles.first_token(tile), entry);
-        pages_from(entry, page);
-    };
-    // first value of a half's tokens; where there is no page, of page 0, whose tokens are then taken for hidden
-    auto half_at = [&](int32_t j, int32_t page) {
-        return (page_stride * (uint32_t)max(page, 0) + head_at + ((uint32_t)j & place_mask)) * D;
-    };
-    // scales of a tile's halves; a half is inside a block
-    auto scales_of = [&](int32_t j, const int32_t (&page)[2], float (&ks)[2], float (&vs)[2]) {
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const uint64_t at = (((uint64_t)(uint32_t)max(page[h], 0) * a.n_kv_heads + kv) << (a.batch.page_shift - a.block_shift)) +
-                                (((uint32_t)(j + 16 * h) & place_mask) >> a.block_shift);
-            ks[h] = sound_scale(a.k_scales[at]), vs[h] = sound_scale(a.v_scales[at]);
-        }
+    auto scale_of = [&](int32_t j, int32_t page) {
+        const uint64_t at = (((uint64_t)(uint32_t)max(page, 0) * a.n_kv_heads + kv) << (a.batch.page_shift - a.block_shift)) +
+                            ((((uint32_t)j + 16 * (lane % kQuarters)) & place_mask) >> a.block_shift);
+        return scales[at];
     };
     u32x4 k[kLoads], v[kLoads];
-    // A tile's keys or values in the order of memory, whole tokens side by side; nothing else will ask for them.
-    auto load = [&](u32x4 (&to)[kLoads], const void *pages, int32_t j, const int32_t (&page)[2]) {
+    // A tile's keys or values in the order of memory, whole tokens side by side; nothing else will ask for them.  Where there is no page, those of page 0, which
+    // are then taken for hidden.
+    auto load = [&](u32x4 (&to)[kLoads], const void *pages, int32_t j, int32_t page) {
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const uint8_t *src = static_cast<const uint8_t *>(pages) + half_at(j + 16 * h, page[h]) + lane * 16;
+        for (int h = 0; h < kQuarters; h++) {
+            const uint64_t first = page_stride * (uint32_t)max(page_of(page, h), 0) + head_at + ((uint32_t)(j + 16 * h) & place_mask);
+            const uint8_t *src = static_cast<const uint8_t *>(pages) + first * D + lane * 16;
 #pragma unroll
-            for (int i = 0; i < kLoads / 2; i++) to[h * (kLoads / 2) + i] = dcdev::load16_stream(src + i * 1024);
+            for (int i = 0; i < kLoads / kQuarters; i++) to[h * (kLoads / kQuarters) + i] = dcdev::load16_stream(src + i * 1024);
         }
     };
-    // Tokens lie in the LDS with their 16-byte chunks exchanged so that 8 tokens' same chunks, and pairs of chunks, are on different banks.
-    auto swizzle = [](uint32_t row) { return D == 64 ? ((row >> 1) & 3u) << 1 : (row & 7u) << 1; };
+    // Tokens lie in the LDS with their 16-byte chunks exchanged so that 16 tokens' same chunks are on different banks.
+    auto swizzle = [](uint32_t token) { return D == 64 ? token >> 2 & 3u : D == 128 ? token >> 1 & 7u : token & 15u; };
     const uint32_t my_lds = dcdev::lds_address(lds.tokens[wave]);
-    // Keys in 8 bits: 16 tokens' same chunks are on different banks.
-    auto key_swizzle = [](uint32_t row) { return D == 64 ? row >> 2 & 3u : D == 128 ? row >> 1 & 7u : row & 15u; };
-    auto put_keys = [&](const u32x4 (&from)[kLoads]) {
+    auto put = [&](const u32x4 (&from)[kLoads]) {
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
-            const uint32_t row = i * kRowsALoad + lane / kChunks, chunk = lane % kChunks;
-            *(lds_u32x4 *)(uintptr_t)(my_lds + row * D + ((chunk ^ key_swizzle(row)) << 4)) = from[i];
-        }
-        __builtin_amdgcn_wave_barrier();
-    };
-    auto put_values = [&](const u32x4 (&from)[kLoads]) {
-#pragma unroll
-        for (int i = 0; i < kLoads; i++) {
-            const uint32_t row = i * kRowsALoad + lane / kChunks, chunk = 2 * (lane % kChunks);
-            const Sixteen<__bf16> x(from[i]);
-            *(lds_u32x4 *)(uintptr_t)(my_lds + row * kRowBytes + ((chunk ^ swizzle(row)) << 4)) = x.low;
-            *(lds_u32x4 *)(uintptr_t)(my_lds + row * kRowBytes + (((chunk + 1) ^ swizzle(row)) << 4)) = x.high;
+            const uint32_t token = i * kTokensALoad + lane / kChunks, chunk = lane % kChunks;
+            *(lds_u32x4 *)(uintptr_t)(my_lds + token * D + ((chunk ^ swizzle(token)) << 4)) = from[i];
         }
         __builtin_amdgcn_wave_barrier();
     };
 
-    int32_t page[2], next_page[2];
-    float ks[2], vs[2], next_ks[2], next_vs[2];
+    // of this tile and the next one: pages of the quarters, scales; of the one behind it the table's entries
+    int32_t page = -1, next_page = -1, entry = -1;
+    float scale = 0.0f, next_scale = 0.0f;
+    ValueScale value_scale;
     int32_t t = t_begin + (int32_t)wave;
+    auto token_of = [&](int32_t t) { return tiles.first_token(min(t, t_end - 1)); };
     if (t < t_end) {
-        if (a.window) pages_of(t, page);
-        else pages_from(first_entry, page);
-        const int32_t j = tiles.first_token(t);
+        const int32_t j = token_of(t);
+        page = page_from(a.window ? entry_at((uint32_t)j) : first_entry);
+        next_page = page_from(entry_at((uint32_t)token_of(t + 4)));
+        scale = scale_of(j, page);
         load(k, a.k_pages, j, page);
         load(v, a.v_pages, j, page);
-        scales_of(j, page, ks, vs);
-        pages_of(min(t + 4, t_end - 1), next_page);
+        entry = entry_at((uint32_t)token_of(t + 8));
     }
     for (; t < t_end; t += 4) {
-        const int32_t j = tiles.first_token(t);
+        const int32_t j = token_of(t), next_j = token_of(t + 4);
         const bool more = t + 4 < t_end;
-        const int32_t next_j = tiles.first_token(min(t + 4, t_end - 1));
 
-        put_keys(k);
+        put(k);
         if (more) {
+            next_scale = scale_of(next_j, next_page);
             load(k, a.k_pages, next_j, next_page);
-            scales_of(next_j, next_page, next_ks, next_vs);
         }
-        f32x4 s[RT][2];
+        const float sound = sound_of(j, page, scale);
+        auto scale_in = [&](int lane) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(sound), lane)); };
+        f32x4 s[RT][kQuarters];
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
+        for (int h = 0; h < kQuarters; h++) {
 #pragma unroll
             for (int rt = 0; rt < RT; rt++) s[rt][h] = f32x4{};
 #pragma unroll
             for (int i = 0; i < KS / 2; i++) {
-                const uint32_t row = 16 * h + c, chunk = 4 * i + g;
-                const Sixteen<T> x(*(const lds_u32x4 *)(uintptr_t)(my_lds + row * D + ((chunk ^ key_swizzle(row)) << 4)));
+                const uint32_t token = 16 * h + c, chunk = 4 * i + g;
+                const u32x4 x = *(const lds_u32x4 *)(uintptr_t)(my_lds + token * D + ((chunk ^ swizzle(token)) << 4));
+                const f16x8 low = __builtin_bit_cast(f16x8, eight_f16(x[0], x[1])), high = __builtin_bit_cast(f16x8, eight_f16(x[2], x[3]));
 #pragma unroll
                 for (int rt = 0; rt < RT; rt++) {
-                    s[rt][h] = Mfma<T>::m16(__builtin_bit_cast(TV, x.low), q[rt][2 * i], s[rt][h]);
-                    s[rt][h] = Mfma<T>::m16(__builtin_bit_cast(TV, x.high), q[rt][2 * i + 1], s[rt][h]);
+                    s[rt][h] = Mfma<_Float16>::m16(low, q[rt][2 * i], s[rt][h]);
+                    s[rt][h] = Mfma<_Float16>::m16(high, q[rt][2 * i + 1], s[rt][h]);
                 }
             }
+            const float ks = scale_in(h);
 #pragma unroll
-            for (int rt = 0; rt < RT; rt++) s[rt][h] *= ks[h];
+            for (int rt = 0; rt < RT; rt++) s[rt][h] *= ks;
         }
         __builtin_amdgcn_wave_barrier();
-
-        // tokens that not all rows see
-        const bool edge = page[0] < 0 || page[1] < 0 || j + kTile > p_min + 1 || j + kTile > tiles.high || (j < tiles.low && j + kTile > tiles.sinks) ||
-                          (a.window && j + kTile > tiles.sinks && (int64_t)j <= (int64_t)p_max - a.window);
-        put_values(v);
+        put(v);
         if (more) load(v, a.v_pages, next_j, next_page);
 
-        bf16x8 w[RT];
+        // tokens that not all rows see
+        const bool edge = __any(page < 0) || j + kTile > p_min + 1 || j + kTile > tiles.high || (j < tiles.low && j + kTile > tiles.sinks) ||
+                          (a.window && j + kTile > tiles.sinks && (int64_t)j <= (int64_t)p_max - a.window);
+        uint32_t most_vs = 0;
+#pragma unroll
+        for (int h = 0; h < kQuarters; h++) most_vs = max(most_vs, __float_as_uint(scale_in(kQuarters + h)));
+        float less;
+        if (value_scale.grows(most_vs, less)) {
+#pragma unroll
+            for (int rt = 0; rt < RT; rt++)
+#pragma unroll
+                for (int dt = 0; dt < DT; dt++) o[rt][dt] *= less;
+        }
+        f16x8 w[RT][kQuarters / 2];
 #pragma unroll
         for (int rt = 0; rt < RT; rt++) {
             if (edge) {
 #pragma unroll
-                for (int h = 0; h < 2; h++)
+                for (int h = 0; h < kQuarters; h++) {
+                    const bool is_there = page_of(page, h) >= 0;
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
-                        const bool sees = seen[rt].token(j + 16 * h + 4 * (int32_t)g + i) & (page[h] >= 0);
+                        const bool sees = seen[rt].token(j + 16 * h + 4 * (int32_t)g + i) & is_there;
                         s[rt][h][i] = sees ? s[rt][h][i] : -INFINITY;
                     }
+                }
             }
-            float top = fmaxf(fmaxf(fmaxf(s[rt][0][0], s[rt][0][1]), fmaxf(s[rt][0][2], s[rt][0][3])),
-                              fmaxf(fmaxf(s[rt][1][0], s[rt][1][1]), fmaxf(s[rt][1][2], s[rt][1][3])));
+            float top = -INFINITY;
+#pragma unroll
+            for (int h = 0; h < kQuarters; h++) top = fmaxf(top, fmaxf(fmaxf(s[rt][h][0], s[rt][h][1]), fmaxf(s[rt][h][2], s[rt][h][3])));
             top = fmaxf(m[rt], max_over_16(top));
             const float ref = top == -INFINITY ? 0.0f : top;
-            const float fade = exp2_of((m[rt] - ref) * a.scale);
+            const float fade = exp2_of((m[rt] - ref) * row_scale[rt]);
             m[rt] = top;
-            f32x8 e;
+            float sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; i++) e[i] = exp2_of((s[rt][i / 4][i % 4] - ref) * a.scale);
-            l[rt] = l[rt] * fade + (((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
+            for (int u = 0; u < kQuarters / 2; u++) {
+                f32x8 e;
 #pragma unroll
-            for (int i = 0; i < 8; i++) e[i] *= vs[i / 4];
-            w[rt] = __builtin_convertvector(e, bf16x8);
+                for (int i = 0; i < 8; i++) e[i] = exp2_of((s[rt][2 * u + i / 4][i % 4] - ref) * row_scale[rt]);
+                sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+                const float vs[2] = {scale_in(kQuarters + 2 * u) * value_scale.by<kLiftFew>(), scale_in(kQuarters + 2 * u + 1) * value_scale.by<kLiftFew>()};
+#pragma unroll
+                for (int i = 0; i < 8; i++) e[i] *= vs[i / 4];
+                w[rt][u] = __builtin_convertvector(e, f16x8);
+            }
+            l[rt] = l[rt] * fade + sum;
 #pragma unroll
             for (int dt = 0; dt < DT; dt++) o[rt][dt] *= fade;
         }
-        const uint32_t i4 = c >> 2, half8 = (c & 1u) << 3;
+        // of 32 tokens the lane's group of 16 has 4 of each of two quarters, as the weights are
+        const uint32_t i8 = c >> 1, token8 = 4 * g + (i8 & 3u) + (i8 >> 2) * 16;
 #pragma unroll
-        for (int dt = 0; dt < DT; dt++) {
-            const uint32_t row = 4 * g + i4, chunk = 2 * dt + ((c & 3u) >> 1);
-            const uint32_t at = my_lds + row * kRowBytes + ((chunk ^ swizzle(row)) << 4) + half8;
-            const u32x2 lo = lds_column4(at), hi = lds_column4(at + 16 * kRowBytes);
-            const u32x4 x = {lo[0], lo[1], hi[0], hi[1]};
+        for (int u = 0; u < kQuarters / 2; u++)
 #pragma unroll
-            for (int rt = 0; rt < RT; rt++) o[rt][dt] = Mfma<__bf16>::m16(__builtin_bit_cast(bf16x8, x), w[rt], o[rt][dt]);
-        }
+            for (int dt = 0; dt < DT; dt++) {
+                const uint32_t token = token8 + 32 * u;
+                const u32x2 x = lds_column8(my_lds + token * D + (((uint32_t)dt ^ swizzle(token)) << 4) + ((c & 1u) << 3));
+                const f16x8 values = __builtin_bit_cast(f16x8, eight_f16(x[0], x[1]));
+#pragma unroll
+                for (int rt = 0; rt < RT; rt++) o[rt][dt] = Mfma<_Float16>::m16(values, w[rt][u], o[rt][dt]);
+            }
         __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int h = 0; h < 2; h++) page[h] = next_page[h], ks[h] = next_ks[h], vs[h] = next_vs[h];
-        if (more) pages_of(min(t + 8, t_end - 1), next_page);
+        page = next_page, scale = next_scale;
+        next_page = page_from(entry);
+        if (more) entry = entry_at((uint32_t)token_of(t + 12));
     }
 
     // the wavefronts' sums, brought to one maximum and added up in their order
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) {
         l[rt] = sum_over_16(l[rt]);
-        m[rt] *= a.scale; // what the weights are relative to
+        m[rt] *= row_scale[rt]; // what the weights are relative to
         if (l[rt] != l[rt] && m[rt] == -INFINITY) m[rt] = 0.0f; // saw scores, none of them a number
         if (g == 0) lds.m[wave][rt * 16 + c] = m[rt], lds.l[wave][rt * 16 + c] = l[rt];
     }
@@ -296,7 +382,8 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
     for (int rt = 0; rt < RT; rt++) {
         const uint32_t r = rt * 16 + c;
         const float top = fmaxf(fmaxf(lds.m[0][r], lds.m[1][r]), fmaxf(lds.m[2][r], lds.m[3][r]));
-        const float f = m[rt] == -INFINITY ? 0.0f : exp2_of(m[rt] - top);
+        // (the largest scale, and what the weights were lifted by, in two steps: neither product leaves the range)
+        const float f = m[rt] == -INFINITY ? 0.0f : exp2_of(m[rt] - top - kLiftFew) * value_scale.value();
         if (rt) __syncthreads();
 #pragma unroll
         for (int dt = 0; dt < DT; dt++)
@@ -329,12 +416,11 @@ template <int D> struct TileLds {
     static constexpr int kTile = D == 256 ? 32 : 64; // tokens
     uint8_t k[2][kTile * 2 * D], v[2][kTile * 2 * D];
     int32_t p[kTileRows];
-    f32x2 scale[2][4]; // of the tokens that each wavefront brings: of keys in units of the scores' powers of two, of values
+    f32x2 scale[2][4]; // of the tokens that each wavefront brings: of keys, of values
 };
 
 template <typename T, int D> __device__ __forceinline__ void many_rows(const AttentionArgs &a, TileLds<D> &lds, bool common, uint32_t block)
 {
-    typedef typename Vec8<T>::type TV;
     constexpr int kTile = TileLds<D>::kTile, KS = D / 16, DT = D / 32, HT = kTile / 32; // HT: 32-token products of a tile
     constexpr uint32_t kRows = kTileRows, kRowBytes = 2 * D, kChunks = D / 16, kRowsALoad = 64 / kChunks; // rows: in the LDS; chunks: of 16 bytes in the cache
     constexpr int kTokens = kTile / 4, kLoads = kTokens / (int)kRowsALoad; // tokens that a wavefront brings, in so many loads
@@ -428,25 +514,32 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
     const int32_t t_begin = (int32_t)min((uint64_t)split * part.chunk, (uint64_t)count);
     const int32_t t_end = split + 1 == part.n_splits ? count : (int32_t)min((uint64_t)t_begin + part.chunk, (uint64_t)count);
     auto first_token = [&](int32_t t) { return t < prefix_tiles.count ? prefix_tiles.first_token(t) : base + own_tiles.first_token(t - prefix_tiles.count); };
-    const Seen all_last(p_max, there, a.window, a.sinks); // of the workgroup's rows
+    const Seen all_first(p_min, there, a.window, a.sinks), all_last(p_max, there, a.window, a.sinks); // of the workgroup's rows
     const Seen first_sees(wave_p_min, there, a.window, a.sinks), last_sees(wave_p_max, there, a.window, a.sinks); // of the wavefront's
 
     const uint32_t my_head = kv * a.group + my_row % a.group;
     const uint64_t my_packed = row_first + my_row / a.group;
     const Seen seen(my_p, there, a.window, a.sinks);
-    TV q[KS];
+    f16x8 q[KS];
     f32x16 o[DT];
     float ref = 0.0f; // what the weights are relative to, in powers of two
     bool any = false; // a score has been seen
     float l = 0.0f;
     const T *q_src = static_cast<const T *>(a.q) + my_packed * a.q_row + my_head * a.q_head + 8 * half;
+    u32x4 raw[KS];
+    uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < KS; i++) {
-        u32x4 x = {};
-        if (my_row < n) x = *reinterpret_cast<const u32x4 *>(q_src + 16 * i);
-        if (a.negate) x ^= 0x80008000u;
-        q[i] = __builtin_bit_cast(TV, x);
+        raw[i] = u32x4{};
+        if (my_row < n) raw[i] = *reinterpret_cast<const u32x4 *>(q_src + 16 * i);
+        if (a.negate) raw[i] ^= 0x80008000u;
+        most = largest(most, raw[i]);
     }
+    const Queries<T> as_f16(largest_over_32(most));
+    const float row_scale = fminf(fmaxf(a.scale * as_f16.back, 0x1p-149f), 0x1p127f);
+#pragma unroll
+    for (int i = 0; i < KS; i++) q[i] = as_f16(raw[i]);
+    ValueScale value_scale;
 #pragma unroll
     for (int dt = 0; dt < DT; dt++) o[dt] = f32x16{};
 
@@ -481,11 +574,14 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
         const uint32_t place = (uint32_t)(j + (int32_t)(lane & 3u) * kTokens - (in_prefix ? 0 : base)) & place_mask;
         const uint64_t token = page_stride * (uint32_t)max(page, 0) + head_at + place, at = token * D;
         const uint32_t there4 = (uint32_t)(__ballot(page >= 0) >> (lane & 60u)) & 15u;
+        // scales of 16 tokens that no row sees may be anything
+        const int32_t j16 = j + (int32_t)((lane & 3u) * kTokens & ~15u);
+        const bool is_seen = page >= 0 && j16 < min(in_prefix ? base : 0x7FFFFFFF, all_last.high) && (j16 + 16 > all_first.low || j16 < all_last.sinks);
         const bool whole = there4 == 15u && (!in_prefix || j + kTile <= base);
         const bool some = t < t_end && j < last_sees.high && (j + kTile > first_sees.low || j < last_sees.sinks);
         const bool edge = !whole || j + kTile > first_sees.high || (j < last_sees.low && j + kTile > first_sees.sinks);
         return Known{(uint32_t)at, (uint32_t)(at >> 32), there4 | (in_prefix ? kPrefix : 0u) | (some ? kSome : 0u) | (edge ? kEdge : 0u),
-                     a.k_scales[token >> a.block_shift], a.v_scales[token >> a.block_shift]};
+                     is_seen ? sound_scale(a.k_scales[token >> a.block_shift]) : 0x1p-126f, is_seen ? sound_scale(a.v_scales[token >> a.block_shift]) : 0x1p-126f};
     };
     int32_t pages_ahead = pages_from(0);
     Known known = known_from(0, pages_ahead);
@@ -531,24 +627,22 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
         const int32_t l = 4 * (i & 15) + (int32_t)wave;
         const float ks = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(known.ks), l));
         const float vs = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(known.vs), l));
-        if (lane == 0) lds.scale[buffer][wave] = f32x2{fminf(fmaxf(sound_scale(ks) * a.scale, 0x1p-149f), 0x1p127f), sound_scale(vs)};
+        if (lane == 0) lds.scale[buffer][wave] = f32x2{ks, vs};
 #pragma unroll
-        for (int i = 0; i < kLoads; i++) {
-            const Sixteen<T> k(k_new[i]);
-            const Sixteen<__bf16> v(v_new[i]);
-            *(lds_u32x4 *)(uintptr_t)(lds_k + buffer * kBuffer + put_at[i][0]) = k.low;
-            *(lds_u32x4 *)(uintptr_t)(lds_k + buffer * kBuffer + put_at[i][1]) = k.high;
-            *(lds_u32x4 *)(uintptr_t)(lds_v + buffer * kBuffer + put_at[i][0]) = v.low;
-            *(lds_u32x4 *)(uintptr_t)(lds_v + buffer * kBuffer + put_at[i][1]) = v.high;
-        }
+        for (int i = 0; i < kLoads; i++)
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                *(lds_u32x4 *)(uintptr_t)(lds_k + buffer * kBuffer + put_at[i][h]) = eight_f16(k_new[i][2 * h], k_new[i][2 * h + 1]);
+                *(lds_u32x4 *)(uintptr_t)(lds_v + buffer * kBuffer + put_at[i][h]) = eight_f16(v_new[i][2 * h], v_new[i][2 * h + 1]);
+            }
     };
     auto k_operand = [&](int i, uint32_t buffer) {
-        return __builtin_bit_cast(TV, *(const lds_u32x4 *)(uintptr_t)(lds_k + buffer * kBuffer + 32 * (i / KS) * kRowBytes + k_at[i % KS]));
+        return __builtin_bit_cast(f16x8, *(const lds_u32x4 *)(uintptr_t)(lds_k + buffer * kBuffer + 32 * (i / KS) * kRowBytes + k_at[i % KS]));
     };
     auto v_operand = [&](int i, uint32_t buffer) {
         const u32x2 lo = lds_column4(lds_v + buffer * kBuffer + 16 * (i / DT) * kRowBytes + v_at[i % DT][0]);
         const u32x2 hi = lds_column4(lds_v + buffer * kBuffer + 16 * (i / DT) * kRowBytes + v_at[i % DT][1]);
-        return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+        return __builtin_bit_cast(f16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
     };
 
     // A step works on tile t, whose keys and values are in buffer B, while the next tile's go from registers into the other buffer and those
@@ -573,14 +667,17 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
             f32x16 s[HT];
             f32x2 scale[2 * HT]; // of 16 tokens each
 #pragma unroll
-            for (int i = 0; i < 2 * HT; i++) scale[i] = lds.scale[buffer][i * (16 / kTokens)];
-            TV x[kAhead];
+            for (int i = 0; i < 2 * HT; i++) {
+                scale[i] = lds.scale[buffer][i * (16 / kTokens)];
+                scale[i][0] = fmaxf(scale[i][0] * row_scale, 0x1p-149f);
+            }
+            f16x8 x[kAhead];
             // The operands come out of the LDS several products ahead of their use.
 #pragma unroll
             for (int i = 0; i < kAhead; i++) x[i] = k_operand(i, buffer);
 #pragma unroll
             for (int i = 0; i < kProducts; i++) {
-                s[i / KS] = Mfma<T>::m32(x[i % kAhead], q[i % KS], i % KS ? s[i / KS] : f32x16{});
+                s[i / KS] = Mfma<_Float16>::m32(x[i % kAhead], q[i % KS], i % KS ? s[i / KS] : f32x16{});
                 if (i + kAhead < kProducts) x[i % kAhead] = k_operand(i + kAhead, buffer);
             }
             if (flags & kEdge) {
@@ -616,7 +713,16 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
                 for (int dt = 0; dt < DT; dt++) o[dt] *= fade;
                 ref = next;
             }
-            bf16x8 w[kGroups], y[kAhead];
+            uint32_t most_vs = 0;
+#pragma unroll
+            for (int i = 0; i < 2 * HT; i++) most_vs = max(most_vs, __float_as_uint(scale[i][1]));
+            float less;
+            if (value_scale.grows(__builtin_amdgcn_readfirstlane(most_vs), less)) {
+#pragma unroll
+                for (int dt = 0; dt < DT; dt++) o[dt] *= less;
+            }
+            const float vs_by = value_scale.by<kLiftMany>();
+            f16x8 w[kGroups], y[kAhead];
 #pragma unroll
             for (int i = 0; i < kAhead; i++) y[i] = v_operand(i, buffer);
 #pragma unroll
@@ -625,11 +731,11 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
 #pragma unroll
                 for (int i = 0; i < 8; i++) e[i] = exp2_of(__builtin_fmaf(s[u / 2][8 * (u % 2) + i], scale[u][0], -ref));
                 l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-                w[u] = __builtin_convertvector(e * scale[u][1], bf16x8);
+                w[u] = __builtin_convertvector(e * (scale[u][1] * vs_by), f16x8);
             }
 #pragma unroll
             for (int i = 0; i < kGroups * DT; i++) {
-                o[i % DT] = Mfma<__bf16>::m32(y[i % kAhead], w[i / DT], o[i % DT]);
+                o[i % DT] = Mfma<_Float16>::m32(y[i % kAhead], w[i / DT], o[i % DT]);
                 if (i + kAhead < kGroups * DT) y[i % kAhead] = v_operand(i + kAhead, buffer);
             }
         }
@@ -657,7 +763,8 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
     uint32_t row = my_row; // where the results go is worked out here, not kept in registers from the beginning
     dcdev::anew(row);
     const uint32_t packed = row_first + row / a.group, head = kv * a.group + row % a.group;
-    auto sums = [&](int dt, int b) { return f32x4{o[dt][4 * b], o[dt][4 * b + 1], o[dt][4 * b + 2], o[dt][4 * b + 3]}; };
+    const float by = value_scale.value() * __uint_as_float((127u - kLiftMany) << 23);
+    auto sums = [&](int dt, int b) { return f32x4{o[dt][4 * b], o[dt][4 * b + 1], o[dt][4 * b + 2], o[dt][4 * b + 3]} * by; };
     if (a.n_slots == 1) {
         typedef T T4 __attribute__((ext_vector_type(4)));
         T *out = static_cast<T *>(a.out) + packed * a.out_row + head * a.out_head + 4 * half;

@@ -6,7 +6,7 @@ import numpy as np
 import oracle.attention as oa
 import oracle.cache_i8 as oc8
 import paper_2502_15443_amd as dc
-from tests.attention_cases import KIND, UNIT
+from tests.attention_cases import KIND, SMALLEST, UNIT
 
 ODD = [np.nan, np.inf, -1.0, 0.0, 3e38]
 
@@ -61,16 +61,16 @@ def pool_values(p):
     return oc8.values(p["k"], p["ks"]), oc8.values(p["v"], p["vs"])
 
 
-def check_attend_i8(type, d, got, got_lse, out, lse, size, least_scale=2.0 ** -10):
+def check_attend_i8(type, d, got, got_lse, out, lse, size, most_scale):
     """Keys and queries enter their product as they are.  With e = 2^-24: a score is off by at most (d + 12) e of its largest sum of |q k|
     (d additions, the scale of the block and of the call, the reference), and an error x of a score changes its weight by the factor 1 + x;
-    sums over n keys add at most n e, exp, log and the joining of parts a few e.  A weight times its value's scale is rounded to bf16, relative
-    2^-8 (absolute 2^-134 below its normal range, on whole numbers that are |v| over their scale), and the result to the rows' type once."""
+    sums over n keys add at most n e, exp, log and the joining of parts a few e.  A weight times its value's scale is rounded to f16, relative
+    2^-11.  Below f16's normal range that is 2^-25 at most of a number that stands for weight 2^-7 at the largest value scale, rounded up to a power of two
+    (`most_scale` at most), while the weights' sum is at least 1 and the numbers are at most 128: 2^-32 * most_scale * 128 a key.  The result is rounded to
+    the rows' type once."""
     e = 2.0 ** -24
     small = e * (2 * (d + 12) * size["s"] + 2 * size["n"][:, None] + 64 + 4 * np.abs(np.where(np.isfinite(lse), lse, 0)))
-    tol = size["v"] * (1.01 * (UNIT["bf16"] + UNIT[type]) + 2 * small[:, :, None]) + 2.0 ** -134 * size["sum"] / least_scale
-    if type == "f16":
-        tol = tol + 2.0 ** -25
+    tol = size["v"] * (1.01 * (UNIT["f16"] + UNIT[type]) + 2 * small[:, :, None]) + 2.0 ** -25 * most_scale * size["n"][:, None, None] + SMALLEST[type]
     served = ~np.isnan(lse)
     nothing = np.isneginf(lse) & served
     assert (got[nothing] == 0).all() and np.isneginf(got_lse[nothing]).all()
