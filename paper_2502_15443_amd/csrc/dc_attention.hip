@@ -905,10 +905,11 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
         // Up to three tiles to a wavefront, parts gain less than it costs to join them (8 heads, 200 tokens: 6.9 us, in parts 8.5; 400: 9.0 and 8.7).
         if (!prefix_len && n_tiles <= 12) return (uint64_t)1;
         uint64_t n = 1;
+        const uint64_t units = cache->type == DC_TYPE_I8 ? 512 : 256;
         // As few workgroups as give every compute unit the same number, to a tenth: a long run of keys is read faster by one workgroup
         // (256 of 8 heads' and 32 sequences' runs of 8000 tokens: 161 us, 512 halves of them 168, 1024 quarters 176), but an uneven number
         // leaves units idle (320 runs of 4100 tokens: 124 us, 960 thirds 108).
-        while (n < most && (items * n + 255) / 256 * 256 * 10 > items * n * 11) n++;
+        while (n < most && (items * n + units - 1) / units * units * 10 > items * n * 11) n++;
         // Where little is to be read, its latency counts: two workgroups to a unit (one token over 1999, 32 heads: 12.0 us with 256, 11.6 with 512).
         if (!prefix_len && items * n <= 256 && (n_tiles + n - 1) / n <= 16) n = std::min(2 * n, most);
         return n;

@@ -12,7 +12,7 @@ using namespace dcpages;
 
 namespace {
 
-constexpr uint32_t kLoads = 16, kRun = 64 * kLoads; // entries of a run
+constexpr uint32_t kLoads = 4, kRun = 64 * kLoads; // entries of a run
 constexpr uint32_t kScanThreads = 1024;
 constexpr int32_t kMostLength = 0x7FFFFFFF;
 
@@ -24,10 +24,16 @@ struct Sequence {
 struct Queue {
     uint32_t first, count;
 };
-// Entries of a run that take a page, and that give one back; behind the sums, of all runs before it.
+// Entries of a run that take a page, and that give one back; or of all runs before it.
 struct Moves {
     uint32_t taken, back;
 };
+
+// Of 4 neighbouring runs: their moves, and the rows of the sequences that end among them (2^25 for all that are more).
+struct Group {
+    uint32_t taken, back, rows, unused;
+};
+constexpr uint32_t kManyRows = 1u << 25; // more than row arrays can have; sums of a few of them stay inside 32 bits
 
 struct TablesArgs {
     const int32_t *held, *arriving, *pages_in, *prefix_pages, *queue_in;
@@ -35,34 +41,41 @@ struct TablesArgs {
     int64_t *slot;
     Queue *ws_queue;
     Sequence *ws_seqs;
+    struct Group *ws_groups;
     Moves *ws_moves;
     uint32_t n_seqs, n_rows, page_shift, stride, n_pages, prefix_len, window, sinks;
     uint32_t runs, n_items; // runs of a sequence, of all
 };
 
-// Tokens that a sequence holds, those that it gets, and those that it has with them.
-__device__ __forceinline__ uint32_t tokens_of(const TablesArgs &a, uint32_t seq, int32_t &held, int32_t &end)
+// Tokens that a sequence holds, and with all the new ones.
+__device__ __forceinline__ uint32_t arriving_at(const TablesArgs &a, uint32_t seq) { return (uint32_t)max(a.arriving[seq], 0); }
+__device__ __forceinline__ void tokens_of(const TablesArgs &a, uint32_t seq, int32_t &held, int32_t &end)
 {
-    const int32_t n = a.arriving[seq];
-    held = n < 0 ? 0 : max(a.held[seq], 0);
+    const int32_t n = a.arriving[seq], h = a.held[seq];
+    held = n < 0 ? 0 : max(h, 0);
     end = (int32_t)min((int64_t)held + max(n, 0), (int64_t)kMostLength);
-    return (uint32_t)max(n, 0);
+}
+__device__ __forceinline__ Queue queue_of(const TablesArgs &a)
+{
+    return Queue{(uint32_t)a.queue_in[0] % a.n_pages, (uint32_t)min((int64_t)max(a.queue_in[1], 0), (int64_t)a.n_pages)};
 }
 
 // What becomes of an entry.
 struct Entry {
-    bool there, wanted, takes;
+    bool there, wanted, takes, goes;
     __device__ __forceinline__ Entry(const TablesArgs &a, uint32_t i, int32_t page, int32_t held, int32_t end)
     {
+        const bool is = i < a.stride;
         const int32_t from = (int32_t)(a.prefix_len + (i << a.page_shift)); // inside the capacity, as the entry is
-        there = (uint32_t)page < a.n_pages;
+        there = is & ((uint32_t)page < a.n_pages);
         wanted = from < end;
         if (a.window) wanted = wanted & (((int64_t)from + (1 << a.page_shift) - 1 > (int64_t)held - a.window) | ((uint32_t)from < a.sinks));
-        takes = wanted & !there & (from >= held);
+        takes = is & wanted & !there & (from >= held);
+        goes = there & !wanted;
     }
 };
 
-// A wavefront's entries of run `item`: entry first + 64 k + lane in page[k]; those beyond the row are -2.
+// A wavefront's entries of run `item`: entry first + 64 k + lane in page[k].
 __device__ __forceinline__ void load_run(const TablesArgs &a, uint32_t item, uint32_t lane, uint32_t &seq, uint32_t &first, int32_t (&page)[kLoads])
 {
     seq = item / a.runs, first = item % a.runs * kRun;
@@ -70,29 +83,26 @@ __device__ __forceinline__ void load_run(const TablesArgs &a, uint32_t item, uin
 #pragma unroll
     for (uint32_t k = 0; k < kLoads; k++) {
         const uint32_t i = first + 64 * k + lane;
-        page[k] = i < a.stride ? row[i] : -2;
+        page[k] = -1;
+        if (i < a.stride) page[k] = row[i];
     }
 }
 
-__device__ __forceinline__ void count_run(const TablesArgs &a, uint32_t item, uint32_t lane)
+__device__ __forceinline__ Moves moves_of(const TablesArgs &a, uint32_t first, uint32_t lane, const int32_t (&page)[kLoads], int32_t held, int32_t end)
 {
-    uint32_t seq, first;
-    int32_t page[kLoads], held, end;
-    load_run(a, item, lane, seq, first, page);
-    tokens_of(a, seq, held, end);
     Moves m = {0, 0};
 #pragma unroll
     for (uint32_t k = 0; k < kLoads; k++) {
-        const uint32_t i = first + 64 * k + lane;
-        const Entry e(a, min(i, a.stride - 1), page[k], held, end);
-        m.taken += (uint32_t)__popcll(__ballot((i < a.stride) & e.takes));
-        m.back += (uint32_t)__popcll(__ballot((i < a.stride) & e.there & !e.wanted));
+        if (first + 64 * k >= a.stride) break;
+        const Entry e(a, first + 64 * k + lane, page[k], held, end);
+        m.taken += (uint32_t)__popcll(__ballot(e.takes));
+        m.back += (uint32_t)__popcll(__ballot(e.goes));
     }
-    if (lane == 0) a.ws_moves[item] = m;
+    return m;
 }
 
 // Inclusive sums over the threads of a workgroup, and the sum of all; every thread takes part.
-template <typename V> __device__ __forceinline__ V workgroup_sums(V v, V &all, V *lds)
+template <uint32_t WAVES, typename V> __device__ __forceinline__ V workgroup_sums(V v, V &all, V *lds)
 {
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
 #pragma unroll
@@ -104,7 +114,8 @@ template <typename V> __device__ __forceinline__ V workgroup_sums(V v, V &all, V
     __syncthreads();
     V before = 0;
     all = 0;
-    for (uint32_t w = 0; w < kScanThreads / 64; w++) {
+#pragma unroll
+    for (uint32_t w = 0; w < WAVES; w++) {
         const V t = lds[w];
         if (w < wave) before += t;
         all += t;
@@ -112,132 +123,272 @@ template <typename V> __device__ __forceinline__ V workgroup_sums(V v, V &all, V
     __syncthreads();
     return before + v;
 }
+typedef unsigned long long u64;
+// Both counts of moves in one number: neither reaches 2^31.
+__device__ __forceinline__ u64 packed(Moves m) { return (u64)m.back << 32 | m.taken; }
+__device__ __forceinline__ Moves unpacked(u64 v) { return Moves{(uint32_t)v, (uint32_t)(v >> 32)}; }
 
-// Rows of the sequences, and how many moves there are before each run: one workgroup of kScanThreads.
-__device__ __forceinline__ void sum_up(const TablesArgs &a, unsigned long long *lds)
+// A sequence's rows, of which `before` are those of the sequences before it; and its results.
+__device__ __forceinline__ Sequence sequence_from(const TablesArgs &a, uint32_t seq, int32_t held, int32_t end, u64 before, uint32_t arriving)
 {
-    unsigned long long rows = 0, all;
-    for (uint32_t b = 0; b < a.n_seqs; b += kScanThreads) {
-        const uint32_t seq = b + threadIdx.x;
-        int32_t held = 0, end = 0;
-        const unsigned long long arriving = seq < a.n_seqs ? tokens_of(a, seq, held, end) : 0, upto = rows + workgroup_sums<unsigned long long>(arriving, all, lds);
-        if (seq < a.n_seqs) {
-            const uint32_t first = (uint32_t)min(upto - arriving, (unsigned long long)a.n_rows), last = (uint32_t)min(upto, (unsigned long long)a.n_rows);
-            a.ws_seqs[seq] = Sequence{held, end, first, last - first};
-            a.len[seq] = min(end, (int32_t)min((int64_t)held + (last - first), (int64_t)kMostLength));
-            a.row_start[seq] = (int32_t)first;
-            if (seq == a.n_seqs - 1) a.row_start[a.n_seqs] = (int32_t)last;
-        }
-        rows += all;
-    }
-    // both counts in one number: neither reaches 2^31
-    unsigned long long moves = 0;
-    for (uint32_t b = 0; b < a.n_items; b += kScanThreads) {
-        const uint32_t item = b + threadIdx.x;
-        unsigned long long v = 0;
-        if (item < a.n_items) {
-            const Moves m = a.ws_moves[item];
-            v = (unsigned long long)m.back << 32 | m.taken;
-        }
-        const unsigned long long before = moves + workgroup_sums<unsigned long long>(v, all, lds) - v;
-        if (item < a.n_items) a.ws_moves[item] = Moves{(uint32_t)before, (uint32_t)(before >> 32)};
-        moves += all;
-    }
-    if (threadIdx.x == 0) {
-        const Queue q = {(uint32_t)a.queue_in[0] % a.n_pages, (uint32_t)min((int64_t)max(a.queue_in[1], 0), (int64_t)a.n_pages)};
-        *a.ws_queue = q;
-        const uint32_t taken = (uint32_t)moves, back = (uint32_t)(moves >> 32), got = min(taken, q.count);
-        a.queue[0] = (int32_t)(((uint64_t)q.first + got) % a.n_pages);
-        a.queue[1] = (int32_t)min((uint64_t)(q.count - got) + back, (uint64_t)a.n_pages);
-        a.queue[2] = (int32_t)(taken - got);
-    }
+    const uint32_t first = (uint32_t)min(before, (u64)a.n_rows), last = (uint32_t)min(before + arriving, (u64)a.n_rows);
+    return Sequence{held, end, first, last - first};
+}
+__device__ __forceinline__ void store_sequence(const TablesArgs &a, uint32_t seq, const Sequence &s)
+{
+    a.len[seq] = min(s.end, (int32_t)min((int64_t)s.held + s.rows, (int64_t)kMostLength));
+    a.row_start[seq] = (int32_t)s.first_row;
+    if (seq == a.n_seqs - 1) a.row_start[a.n_seqs] = (int32_t)(s.first_row + s.rows);
+}
+__device__ __forceinline__ void store_queue(const TablesArgs &a, const Queue &q, Moves m)
+{
+    const uint32_t got = min(m.taken, q.count);
+    a.queue[0] = (int32_t)(((u64)q.first + got) % a.n_pages);
+    a.queue[1] = (int32_t)min((u64)(q.count - got) + m.back, (u64)a.n_pages);
+    a.queue[2] = (int32_t)(m.taken - got);
 }
 
-// A run's entries as they become, and the places of the rows that lie on them.  lds: address of kRun entries of the wavefront's own.
-__device__ __forceinline__ void fill_run(const TablesArgs &a, uint32_t item, uint32_t lane, uint32_t lds)
+// Rows of a sequence that lie on a run's entries: positions begin .. end - 1, whose rows are less + position.
+struct RunRows {
+    uint32_t seq, first, begin, end, less;
+};
+
+// A run's entries as they become, and which rows lie on them.  at: moves of the runs before; lds: address of kRun entries of the wavefront's own.
+__device__ __forceinline__ void fill_run(const TablesArgs &a, uint32_t seq, uint32_t first, uint32_t lane, const int32_t (&page)[kLoads], const Sequence &s, const Queue &q,
+                                         Moves at, uint32_t lds, RunRows &rows)
 {
-    uint32_t seq, first;
-    int32_t page[kLoads];
-    load_run(a, item, lane, seq, first, page);
-    const Sequence s = a.ws_seqs[seq];
-    const Queue q = *a.ws_queue;
-    Moves at = a.ws_moves[item];
     const uint64_t below = (1ull << lane) - 1;
     int32_t *row = a.pages + (uint64_t)seq * a.stride;
+    // places in the ring: sums of two numbers up to n_pages stay inside 32 bits
+    auto in_ring = [&](uint32_t x) { return x >= a.n_pages ? x - a.n_pages : x; };
+    const uint32_t end = in_ring(q.first + q.count);
+    int32_t becomes[kLoads];
 #pragma unroll
     for (uint32_t k = 0; k < kLoads; k++) {
-        const uint32_t i = first + 64 * k + lane;
-        const bool is = i < a.stride;
-        const Entry e(a, min(i, a.stride - 1), page[k], s.held, s.end);
-        const uint64_t taking = __ballot(is & e.takes), giving = __ballot(is & e.there & !e.wanted);
+        becomes[k] = -1;
+        if (first + 64 * k >= a.stride) break;
+        const Entry e(a, first + 64 * k + lane, page[k], s.held, s.end);
+        const uint64_t taking = __ballot(e.takes), giving = __ballot(e.goes);
         const uint32_t rank = at.taken + (uint32_t)__popcll(taking & below), rank_back = at.back + (uint32_t)__popcll(giving & below);
-        int32_t p = (e.there & e.wanted) ? page[k] : -1;
-        if (is & e.takes & (rank < q.count)) p = a.free[((uint64_t)q.first + rank) % a.n_pages];
-        if (is & e.there & !e.wanted) a.free[((uint64_t)q.first + q.count + rank_back) % a.n_pages] = page[k];
-        if (is) row[i] = p;
-        *(dcdev::lds_u32 *)(uintptr_t)(lds + 4 * (64 * k + lane)) = (uint32_t)p;
+        if (e.there & e.wanted) becomes[k] = page[k];
+        if (e.takes & (rank < q.count)) becomes[k] = a.free[in_ring(q.first + rank)];
+        if (e.goes & (rank_back < a.n_pages)) a.free[in_ring(end + rank_back)] = page[k];
         at.taken += (uint32_t)__popcll(taking), at.back += (uint32_t)__popcll(giving);
     }
-    __builtin_amdgcn_wave_barrier();
-    if (!a.slot && !a.position && !a.seq) return;
-    // the sequence's rows from the run's first position on (the first run: from the beginning) to its last (the last run: to the end)
-    const int64_t from = first ? (int64_t)a.prefix_len + ((int64_t)first << a.page_shift) : 0;
-    const int64_t to = first + kRun < a.stride ? (int64_t)a.prefix_len + ((int64_t)(first + kRun) << a.page_shift) : INT64_MAX;
-    const int64_t p_first = max(from, (int64_t)s.held), p_end = min(to, (int64_t)s.held + s.rows);
-    for (int64_t pos = p_first + lane; pos < p_end; pos += 64) {
-        const uint32_t r = s.first_row + (uint32_t)(pos - s.held), p = (uint32_t)pos;
-        const uint32_t place = p < a.prefix_len ? p : p - a.prefix_len, i = place >> a.page_shift;
-        int32_t of = -1;
-        if (p < a.prefix_len) of = a.prefix_pages[i];
-        else if (i < a.stride) of = (int32_t)dcdev::lds_load32(lds + 4 * (i - first));
-        const uint32_t in_page = place & ((1u << a.page_shift) - 1u);
-        if (a.slot) a.slot[r] = (uint32_t)of < a.n_pages ? ((int64_t)of << a.page_shift) + in_page : -1;
-        if (a.position) a.position[r] = (int32_t)min(pos, (int64_t)kMostLength);
-        if (a.seq) a.seq[r] = (int32_t)seq;
+#pragma unroll
+    for (uint32_t k = 0; k < kLoads; k++) {
+        if (first + 64 * k >= a.stride) break;
+        if (first + 64 * k + lane < a.stride) row[first + 64 * k + lane] = becomes[k];
+        *(dcdev::lds_u32 *)(uintptr_t)(lds + 4 * (64 * k + lane)) = (uint32_t)becomes[k];
+    }
+    if (lane == 0) {
+        // the sequence's rows from the run's first position on (the first run: from the beginning) to its last (the last run: to the end)
+        const uint32_t from = first ? a.prefix_len + (first << a.page_shift) : 0;
+        const uint32_t to = first + kRun < a.stride ? a.prefix_len + ((first + kRun) << a.page_shift) : 0xFFFFFFFFu;
+        const uint32_t begin = max(from, (uint32_t)s.held), end = min(to, (uint32_t)s.held + s.rows);
+        rows = RunRows{seq, first, begin, begin < end ? end : begin, s.first_row - (uint32_t)s.held};
     }
 }
 
-// Rows of no sequence.
-__device__ __forceinline__ void fill_rest(const TablesArgs &a, uint32_t thread, uint32_t threads)
+// The places of the rows that lie on a run's entries, by all threads of the workgroup.
+template <uint32_t THREADS> __device__ __forceinline__ void fill_rows(const TablesArgs &a, const RunRows &rows, uint32_t lds)
 {
-    const Sequence s = a.ws_seqs[a.n_seqs - 1];
-    for (uint64_t r = (uint64_t)s.first_row + s.rows + thread; r < a.n_rows; r += threads) {
+    const RunRows n = rows;
+    for (uint32_t p = n.begin + threadIdx.x; p < n.end; p += THREADS) {
+        const uint32_t r = n.less + p, place = p < a.prefix_len ? p : p - a.prefix_len, i = place >> a.page_shift;
+        int32_t of = -1;
+        if (p < a.prefix_len) of = a.prefix_pages[i];
+        else if (i < a.stride) of = (int32_t)dcdev::lds_load32(lds + 4 * (i - n.first));
+        if (a.slot) a.slot[r] = (uint32_t)of < a.n_pages ? (int64_t)((uint64_t)(uint32_t)of << a.page_shift | (place & ((1u << a.page_shift) - 1u))) : -1;
+        if (a.position) a.position[r] = (int32_t)min(p, (uint32_t)kMostLength);
+        if (a.seq) a.seq[r] = (int32_t)n.seq;
+    }
+}
+
+// Rows of no sequence, from row `from` on.
+__device__ __forceinline__ void fill_rest(const TablesArgs &a, uint32_t from, uint32_t thread, uint32_t threads)
+{
+    for (u64 r = (u64)from + thread; r < a.n_rows; r += threads) {
         if (a.slot) a.slot[r] = -1;
         if (a.position) a.position[r] = -1;
         if (a.seq) a.seq[r] = -1;
     }
 }
 
-__global__ __launch_bounds__(256) void dc_kv_tables_count_kernel(TablesArgs a)
-{
-    for (uint32_t item = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); item < a.n_items; item += gridDim.x * 4) count_run(a, item, threadIdx.x & 63u);
-}
-
-__global__ __launch_bounds__(kScanThreads) void dc_kv_tables_sum_kernel(TablesArgs a)
-{
-    __shared__ unsigned long long lds[kScanThreads / 64];
-    sum_up(a, lds);
-}
-
-__global__ __launch_bounds__(256) void dc_kv_tables_fill_kernel(TablesArgs a)
-{
-    __shared__ int32_t lds[4][kRun];
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    for (uint32_t item = blockIdx.x * 4 + wave; item < a.n_items; item += gridDim.x * 4) fill_run(a, item, threadIdx.x & 63u, dcdev::lds_address(lds) + wave * (kRun * 4));
-    fill_rest(a, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
-}
-
+// Up to 16 runs: one workgroup with a run to a wavefront; what one part finds stays in registers and in the LDS.
+constexpr uint32_t kFewItems = kScanThreads / 64;
 __global__ __launch_bounds__(kScanThreads) void dc_kv_tables_kernel(TablesArgs a)
 {
-    __shared__ int32_t lds[kScanThreads / 64][kRun];
-    __shared__ unsigned long long sums[kScanThreads / 64];
+    __shared__ int32_t entries[kFewItems][kRun];
+    __shared__ Moves moves[kFewItems];
+    __shared__ RunRows run_rows[kFewItems];
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63u;
-    for (uint32_t item = wave; item < a.n_items; item += kScanThreads / 64) count_run(a, item, lane);
+    // every wavefront knows all sequences (at most 16): a lane to a sequence
+    const uint32_t arriving = lane < a.n_seqs ? arriving_at(a, lane) : 0;
+    const Queue q = queue_of(a);
+    uint32_t seq = 0, first = 0;
+    int32_t page[kLoads], held = 0, end = 0;
+    Moves mine = {0, 0};
+    if (wave < a.n_items) {
+        load_run(a, wave, lane, seq, first, page);
+        tokens_of(a, seq, held, end);
+        mine = moves_of(a, first, lane, page, held, end);
+    }
+    u64 rows_upto = arriving;
+#pragma unroll
+    for (int k = 1; k < (int)kFewItems; k <<= 1) {
+        const u64 t = __shfl_up(rows_upto, k);
+        if (lane >= (uint32_t)k) rows_upto += t;
+    }
+    const u64 rows = __shfl(rows_upto, kFewItems - 1), before = __shfl(rows_upto - arriving, (int)seq);
+    if (lane == 0) moves[wave] = mine;
+    __syncthreads(); // (behind it nobody reads what the results may lie on: lengths, queue, entries)
+    Moves at = {0, 0}, all = {0, 0};
+#pragma unroll
+    for (uint32_t w = 0; w < kFewItems; w++) {
+        const Moves m = moves[w];
+        if (w < wave) at.taken += m.taken, at.back += m.back;
+        all.taken += m.taken, all.back += m.back;
+    }
+    if (threadIdx.x == 0) store_queue(a, q, all);
+    if (wave < a.n_items) {
+        const Sequence s = sequence_from(a, seq, held, end, before, (uint32_t)__shfl((int)arriving, (int)seq));
+        if (lane == 0 && first == 0) store_sequence(a, seq, s);
+        fill_run(a, seq, first, lane, page, s, q, at, dcdev::lds_address(entries) + wave * (kRun * 4), run_rows[wave]);
+    }
+    fill_rest(a, (uint32_t)min(rows, (u64)a.n_rows), threadIdx.x, kScanThreads);
     __syncthreads();
-    sum_up(a, sums);
+    for (uint32_t i = 0; i < a.n_items; i++) fill_rows<kScanThreads>(a, run_rows[i], dcdev::lds_address(entries) + i * (kRun * 4));
+}
+
+// More: counts of all runs and what the results may lie on, ..
+__global__ __launch_bounds__(256) void dc_kv_tables_count_kernel(TablesArgs a)
+{
+    __shared__ Group runs[4];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.ws_queue = queue_of(a);
+    for (uint32_t item0 = blockIdx.x * 4; item0 < a.n_items; item0 += gridDim.x * 4) {
+        const uint32_t item = item0 + wave;
+        Group mine = {};
+        if (item < a.n_items) {
+            uint32_t seq, first;
+            int32_t page[kLoads], held, end;
+            load_run(a, item, lane, seq, first, page);
+            tokens_of(a, seq, held, end);
+            const Moves m = moves_of(a, first, lane, page, held, end);
+            const uint32_t rows = arriving_at(a, seq);
+            if (lane == 0) a.ws_moves[item] = m;
+            if (lane == 0 && first == 0) a.ws_seqs[seq] = Sequence{held, end, 0, rows};
+            mine = Group{m.taken, m.back, item % a.runs == a.runs - 1 ? min(rows, kManyRows) : 0u, 0};
+        }
+        if (lane == 0) runs[wave] = mine;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            Group g = {};
+#pragma unroll
+            for (int w = 0; w < 4; w++) g.taken += runs[w].taken, g.back += runs[w].back, g.rows += runs[w].rows;
+            g.rows = min(g.rows, kManyRows);
+            a.ws_groups[item0 / 4] = g;
+        }
+        __syncthreads();
+    }
+}
+
+// .. their sums, if their groups are too many for everyone to add up those before its own ..
+constexpr uint32_t kManyItems = 16384;
+__global__ __launch_bounds__(kScanThreads) void dc_kv_tables_sum_kernel(TablesArgs a)
+{
+    __shared__ u64 lds[kScanThreads / 64];
+    u64 rows = 0, all;
+    for (uint32_t b = 0; b < a.n_seqs; b += kScanThreads) {
+        const uint32_t seq = b + threadIdx.x;
+        Sequence s = {};
+        if (seq < a.n_seqs) s = a.ws_seqs[seq];
+        const u64 upto = rows + workgroup_sums<kScanThreads / 64, u64>(s.rows, all, lds);
+        if (seq < a.n_seqs) a.ws_seqs[seq] = sequence_from(a, seq, s.held, s.end, upto - s.rows, s.rows);
+        rows += all;
+    }
+    u64 moves = 0;
+    for (uint32_t b = 0; b < a.n_items; b += kScanThreads) {
+        const uint32_t item = b + threadIdx.x;
+        const u64 v = item < a.n_items ? packed(a.ws_moves[item]) : 0;
+        const u64 before = moves + workgroup_sums<kScanThreads / 64, u64>(v, all, lds) - v;
+        if (item < a.n_items) a.ws_moves[item] = unpacked(before);
+        moves += all;
+    }
+    if (threadIdx.x == 0) store_queue(a, *a.ws_queue, unpacked(moves));
+}
+
+// .. and the results.  SUMMED: the sums are there; else a workgroup adds up what its own group has before it.
+template <bool SUMMED> __global__ __launch_bounds__(256) void dc_kv_tables_fill_kernel(TablesArgs a)
+{
+    __shared__ int32_t lds[4][kRun];
+    __shared__ uint32_t sums[4][6];
+    __shared__ RunRows run_rows[4];
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63u, address = dcdev::lds_address(lds) + wave * (kRun * 4);
+    const Queue q = *a.ws_queue;
+    if (SUMMED) {
+        for (uint32_t item0 = blockIdx.x * 4; item0 < a.n_items; item0 += gridDim.x * 4) {
+            const uint32_t item = item0 + wave;
+            if (item < a.n_items) {
+                uint32_t seq, first;
+                int32_t page[kLoads];
+                load_run(a, item, lane, seq, first, page);
+                const Sequence s = a.ws_seqs[seq];
+                if (lane == 0 && first == 0) store_sequence(a, seq, s);
+                fill_run(a, seq, first, lane, page, s, q, a.ws_moves[item], address, run_rows[wave]);
+            }
+            __syncthreads();
+            for (uint32_t i = 0; i < min(4u, a.n_items - item0); i++) fill_rows<256>(a, run_rows[i], dcdev::lds_address(lds) + i * (kRun * 4));
+            __syncthreads();
+        }
+        const Sequence s = a.ws_seqs[a.n_seqs - 1];
+        fill_rest(a, s.first_row + s.rows, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
+        return;
+    }
+    const uint32_t item = blockIdx.x * 4 + wave; // the grid has a wavefront for each
+    uint32_t seq = 0, first = 0;
+    int32_t page[kLoads];
+    Sequence s = {};
+    if (item < a.n_items) {
+        load_run(a, item, lane, seq, first, page);
+        s = a.ws_seqs[seq];
+    }
+    // moves and rows of all groups of runs, and of those before the workgroup's
+    const uint32_t item0 = blockIdx.x * 4, groups = (a.n_items + 3) / 4;
+    uint32_t mine[6] = {};
+    for (uint32_t i = threadIdx.x; i < groups; i += 256) {
+        const Group g = a.ws_groups[i];
+        mine[3] += g.taken, mine[4] += g.back, mine[5] = min(mine[5] + g.rows, kManyRows);
+        if (i < blockIdx.x) mine[0] += g.taken, mine[1] += g.back, mine[2] = min(mine[2] + g.rows, kManyRows);
+    }
+#pragma unroll
+    for (int i = 0; i < 6; i++) {
+        const uint32_t v = dcdev::lanes_prefix_sum<false>(mine[i]);
+        if (lane == 63) sums[wave][i] = i % 3 == 2 ? min(v, kManyRows) : v;
+    }
     __syncthreads();
-    for (uint32_t item = wave; item < a.n_items; item += kScanThreads / 64) fill_run(a, item, lane, dcdev::lds_address(lds) + wave * (kRun * 4));
-    fill_rest(a, threadIdx.x, kScanThreads);
+    uint32_t total[6] = {};
+#pragma unroll
+    for (int w = 0; w < 4; w++)
+#pragma unroll
+        for (int i = 0; i < 6; i++) total[i] += sums[w][i];
+    if (item == 0 && lane == 0) store_queue(a, q, Moves{total[3], total[4]});
+    if (item < a.n_items) {
+        Moves at = {total[0], total[1]};
+        u64 rows = total[2];
+        for (uint32_t i = item0; i < item; i++) { // its own group's runs before it
+            const Moves v = a.ws_moves[i];
+            at.taken += v.taken, at.back += v.back;
+            if (i % a.runs == a.runs - 1) rows += a.ws_seqs[i / a.runs].rows;
+        }
+        s = sequence_from(a, seq, s.held, s.end, rows, s.rows);
+        if (lane == 0 && first == 0) store_sequence(a, seq, s);
+        fill_run(a, seq, first, lane, page, s, q, at, address, run_rows[wave]);
+    }
+    fill_rest(a, min(total[5], a.n_rows), blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
+    __syncthreads();
+    for (uint32_t i = 0; i < min(4u, a.n_items - item0); i++) fill_rows<256>(a, run_rows[i], dcdev::lds_address(lds) + i * (kRun * 4));
 }
 
 bool requests_ok(const dc_kv_requests *r)
@@ -257,7 +408,8 @@ bool requests_ok(const dc_kv_requests *r)
 uint32_t runs_of(const dc_kv_requests *r) { return (r->pages_stride + kRun - 1) / kRun; }
 uint64_t workspace_of(const dc_kv_requests *r)
 {
-    return sizeof(Queue) + sizeof(Sequence) * (uint64_t)r->n_seqs + sizeof(Moves) * (uint64_t)r->n_seqs * runs_of(r);
+    const uint64_t items = (uint64_t)r->n_seqs * runs_of(r);
+    return 16 + sizeof(Sequence) * (uint64_t)r->n_seqs + sizeof(Group) * ((items + 3) / 4) + sizeof(Moves) * items;
 }
 
 } // namespace
@@ -281,16 +433,21 @@ extern "C" int dc_kv_tables(const dc_kv_requests *requests, void *workspace_dev,
     a.n_seqs = r.n_seqs, a.n_rows = r.n_rows, a.page_shift = shift_of(r.page_tokens), a.stride = r.pages_stride, a.n_pages = r.n_pages;
     a.prefix_len = r.prefix_len, a.window = r.window, a.sinks = r.sinks, a.runs = runs_of(&r), a.n_items = r.n_seqs * a.runs;
     a.ws_queue = static_cast<Queue *>(workspace_dev);
-    a.ws_seqs = reinterpret_cast<Sequence *>(a.ws_queue + 1);
-    a.ws_moves = reinterpret_cast<Moves *>(a.ws_seqs + r.n_seqs);
+    a.ws_seqs = reinterpret_cast<Sequence *>(a.ws_queue + 2); // at 16 bytes
+    a.ws_groups = reinterpret_cast<Group *>(a.ws_seqs + r.n_seqs);
+    a.ws_moves = reinterpret_cast<Moves *>(a.ws_groups + (a.n_items + 3) / 4);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (a.n_items <= kScanThreads / 64) {
+    if (a.n_items <= kFewItems) {
         hipLaunchKernelGGL(dc_kv_tables_kernel, dim3(1), dim3(kScanThreads), 0, stream, a);
     } else {
         const dim3 grid(std::min<uint32_t>((a.n_items + 3) / 4, 1u << 20));
         hipLaunchKernelGGL(dc_kv_tables_count_kernel, grid, dim3(256), 0, stream, a);
-        hipLaunchKernelGGL(dc_kv_tables_sum_kernel, dim3(1), dim3(kScanThreads), 0, stream, a);
-        hipLaunchKernelGGL(dc_kv_tables_fill_kernel, grid, dim3(256), 0, stream, a);
+        if (a.n_items <= kManyItems) {
+            hipLaunchKernelGGL(dc_kv_tables_fill_kernel<false>, grid, dim3(256), 0, stream, a);
+        } else {
+            hipLaunchKernelGGL(dc_kv_tables_sum_kernel, dim3(1), dim3(kScanThreads), 0, stream, a);
+            hipLaunchKernelGGL(dc_kv_tables_fill_kernel<true>, grid, dim3(256), 0, stream, a);
+        }
     }
     return dc_launch_status();
 }
