@@ -577,7 +577,8 @@ typedef struct {
  * query and key head becomes (a c_i - b s_i, b c_i + a s_i), evaluated in fp32 and rounded once to the cache's type; values are only
  * rounded.  Queries go to q_out_dev, keys and values into the pages.  A row whose cosines lie outside the table (rot_dim > 0) is
  * left out as a whole, one whose page is not there is not put into the cache.  Positions below prefix_len belong to the prefix
- * and are written there.  Two rows of one call must not share a place in the cache.  One launch.
+ * and are written there.  Two rows of one call must not share a place in the cache.  One launch; into
+ * a cache of DC_TYPE_I8 up to three.
  * Into a cache of DC_TYPE_I8, block by block: with A the largest magnitude among the finite values that the call puts into the block (keys as they
  * are turned, in fp32, each product and each sum rounded), s is the smallest power of two with A <= 127 s, 2^-126 at least; where the block's first
  * token is not the call's, s is at least the block's scale so far.  A new value x is held as the whole number nearest to x / s (ties to

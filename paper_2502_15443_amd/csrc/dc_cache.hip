@@ -158,7 +158,8 @@ extern "C" int dc_kv_append(const dc_kv_cache *cache, const dc_kv_batch *batch, 
     const bool neighbours = rows->pairing == DC_ROPE_NEIGHBOURS;
     if (cache->type == DC_TYPE_I8) {
         a.k_scales = cache->k_scale_dev, a.v_scales = cache->v_scale_dev, a.block_shift = shift_of(cache->scale_tokens);
-        launch_i8(a, rows->type, cache->rows_type, d, neighbours, stream);
+        a.rows_f16 = cache->rows_type == DC_TYPE_F16;
+        launch_i8(a, rows->type, d, neighbours, stream);
     } else if (cache->type == DC_TYPE_BF16) launch_x<__bf16>(a, rows->type, d, neighbours, stream);
     else launch_x<_Float16>(a, rows->type, d, neighbours, stream);
     return dc_launch_status();

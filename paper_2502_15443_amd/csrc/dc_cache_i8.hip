@@ -17,25 +17,23 @@ namespace {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// A leader with at most this many rows takes care of its block beside the row's queries; one with more has a workgroup's threads for its block.
-constexpr uint32_t kFewRows = 4;
+// A leader with at most this many rows takes care of its block beside the row's queries; one with more has threads for its block.
+constexpr uint32_t kFewRows = 4, kMostThreads = 1024;
 
-// Where a row belongs, and the block that it leads, if it is a leader.
+// Where a row belongs, and the block that it leads, if it is a leader.  Its page is looked at last: the row's values need not wait for it.
 struct Place {
-    uint32_t seq, count; // count: rows of the block, from this one on; 0 for a row that leads none, or whose page is not there
-    int32_t pos, page;
+    uint32_t count; // rows of the block, from this one on; 0 for a row that leads none
+    int32_t pos, entry;
     uint32_t in_page;
-    __device__ __forceinline__ Place(const AppendArgs &a, uint32_t row, uint32_t seq) : seq(seq), count(0), pos(-1), page(-1), in_page(0)
+    __device__ __forceinline__ Place(const AppendArgs &a, uint32_t row, uint32_t seq, uint32_t first, uint32_t end, int32_t length) : count(0), entry(-1), in_page(0)
     {
-        if (seq >= a.batch.n_seqs) return;
-        const uint32_t first = a.batch.first_row(seq), end = a.batch.rows_end(seq);
         // row - end >= -n_rows and length >= 0: no overflow; negative for rows of a sequence that is shorter than its rows
-        pos = a.batch.length(seq) - (int32_t)(end - row);
+        pos = length - (int32_t)(end - row);
         if (pos < 0 || pos >= a.batch.capacity()) return;
-        page = a.batch.page_of(seq, (uint32_t)pos);
+        entry = a.batch.page_of(seq, (uint32_t)pos);
         in_page = a.batch.place_in_page((uint32_t)pos);
         const uint32_t block = 1u << a.block_shift, in_block = in_page & (block - 1u);
-        if (page < 0 || (in_block && row != first)) return;
+        if (in_block && row != first) return;
         count = min(block - in_block, first + min(end - first, a.max_new) - row);
         if ((uint32_t)pos < a.batch.prefix_len) count = min(count, a.batch.prefix_len - (uint32_t)pos);
     }
@@ -47,12 +45,46 @@ __device__ __forceinline__ float scale_for(float most)
     const uint32_t u = __float_as_uint(most);
     return __uint_as_float((uint32_t)max(1, (int32_t)(u >> 23) - 6 + ((u & 0x7FFFFFu) > 0x7E0000u)) << 23);
 }
+// 1 / s, for a power of two without a division.
+__device__ __forceinline__ float reciprocal(float s)
+{
+    const uint32_t u = __float_as_uint(s);
+    return u & 0x7FFFFFu || u > 253u << 23 ? 1.0f / s : __uint_as_float((254u << 23) - u);
+}
+// Largest of the lanes' numbers, which are at least 0; the same in all lanes.
+__device__ __forceinline__ uint32_t largest_of_lanes(uint32_t v)
+{
+    v = max(v, dcdev::dpp_or_zero<0x111, 0xF>(v));
+    v = max(v, dcdev::dpp_or_zero<0x112, 0xF>(v));
+    v = max(v, dcdev::dpp_or_zero<0x114, 0xF>(v));
+    v = max(v, dcdev::dpp_or_zero<0x118, 0xF>(v));
+    v = max(v, dcdev::dpp_or_zero<0x142, 0xA>(v));
+    v = max(v, dcdev::dpp_or_zero<0x143, 0xC>(v));
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
 // A scale that is read: a number above 0.
 __device__ __forceinline__ float sound_scale(float s) { return fminf(fmaxf(s, 0x1p-126f), 0x1p127f); }
 
 // A thread's 16 values of a head, in two groups of 8 that hold whole pairs.
 struct Values {
     f32x8 x, y;
+};
+
+template <typename T> __device__ __forceinline__ dcdev::u32x4 rounded(const f32x8 &x)
+{
+    return __builtin_bit_cast(dcdev::u32x4, __builtin_convertvector(x, typename Vec8<T>::type));
+}
+
+// The same as they lie in memory.
+template <typename X> struct Raw {
+    typename Vec8<X>::type x, y;
+    __device__ __forceinline__ void load(const X *p, const X *q) { x = *reinterpret_cast<const typename Vec8<X>::type *>(p), y = *reinterpret_cast<const typename Vec8<X>::type *>(q); }
+    __device__ __forceinline__ Values values() const { return Values{__builtin_convertvector(x, f32x8), __builtin_convertvector(y, f32x8)}; }
+};
+template <> struct Raw<float> {
+    f32x8 x, y;
+    __device__ __forceinline__ void load(const float *p, const float *q) { x = widened(p), y = widened(q); }
+    __device__ __forceinline__ Values values() const { return Values{x, y}; }
 };
 
 // Which values those are; what does not turn is taken as it lies.
@@ -102,33 +134,52 @@ template <bool NEIGHBOURS> __device__ __forceinline__ Values turned(const Values
     return r;
 }
 
-// Largest magnitude of the values that are numbers.
-__device__ __forceinline__ float largest_number(const Values &v)
-{
-    float m = 0.0f;
+// Largest magnitude of the values, and whether all are numbers.  (A sum of magnitudes is no number if one of them is none; if it only leaves the range,
+// the values are looked at one by one for nothing.)
+struct Most {
+    float value;
+    bool numbers;
+    __device__ __forceinline__ explicit Most(const Values &v) : value(0.0f)
+    {
+        float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const float a = fabsf(v.x[i]), b = fabsf(v.y[i]);
-        m = fmaxf(m, fmaxf(a < INFINITY ? a : 0.0f, b < INFINITY ? b : 0.0f));
-    }
-    return m;
-}
-
-// The whole numbers nearest to 8 values times `by`, as bytes; NaN is 0.
-__device__ __forceinline__ u32x2 whole_numbers(const f32x8 &x, float by)
-{
-    uint32_t w[2];
+        for (int i = 0; i < 8; i++) value = fmaxf(fmaxf(value, fabsf(v.x[i])), fabsf(v.y[i])), sum += fabsf(v.x[i]) + fabsf(v.y[i]);
+        numbers = sum < INFINITY;
+        if (!numbers) {
+            dcdev::keep_order(); // a branch, not selections: it is hardly ever taken
+            value = 0.0f;
 #pragma unroll
-    for (int h = 0; h < 2; h++) {
-        w[h] = 0;
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const float r = rintf(x[4 * h + i] * by);
-            const int32_t n = r == r ? (int32_t)fminf(fmaxf(r, -127.0f), 127.0f) : 0;
-            w[h] |= ((uint32_t)n & 255u) << (8 * i);
+            for (int i = 0; i < 8; i++) {
+                const float x = fabsf(v.x[i]), y = fabsf(v.y[i]);
+                value = fmaxf(value, fmaxf(x < INFINITY ? x : 0.0f, y < INFINITY ? y : 0.0f));
+            }
         }
     }
-    return u32x2{w[0], w[1]};
+};
+
+// The whole numbers nearest to 8 values times `by`, as bytes: added to 1.5 2^23, a number of up to 127 is rounded to the nearest whole one, ties to even,
+// and its low byte is what is wanted.  Infinities are 127 with their sign, NaN is 0.
+__device__ __forceinline__ u32x2 whole_numbers(const f32x8 &x, float by, bool numbers)
+{
+#pragma clang fp contract(off)
+    uint32_t n[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) n[i] = __float_as_uint(x[i] * by + 12582912.0f);
+    if (!numbers) {
+        dcdev::keep_order();
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const uint32_t u = __float_as_uint(x[i]);
+            if ((u & 0x7FFFFFFFu) >= 0x7F800000u) n[i] = u & 0x7FFFFFu ? 0u : (u >> 31 ? (uint32_t)-127 : 127u);
+        }
+    }
+    u32x2 w;
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        const uint32_t low = __builtin_amdgcn_perm(n[4 * h + 1], n[4 * h], 0x0C0C0400u), high = __builtin_amdgcn_perm(n[4 * h + 3], n[4 * h + 2], 0x0C0C0400u);
+        w[h] = __builtin_amdgcn_perm(high, low, 0x05040100u);
+    }
+    return w;
 }
 // 16 bytes' whole numbers times `by`, rounded.
 __device__ __forceinline__ dcdev::u32x4 in_larger_steps(const dcdev::u32x4 &from, float by)
@@ -143,39 +194,40 @@ __device__ __forceinline__ dcdev::u32x4 in_larger_steps(const dcdev::u32x4 &from
     return to;
 }
 
-// A row's queries, and blocks with few new rows.  A thread owns 16 values of a head of the row, D / 16 neighbouring ones a head.
-template <typename X, typename T, int D, bool NEIGHBOURS> __device__ __forceinline__ void append_row(const AppendArgs &a, uint32_t row, uint32_t slot_first, uint32_t slots_end,
-                                                                                                 uint32_t step)
+// A row's queries (QUERIES), and blocks with few new rows (KEYS).  A thread owns 16 values of a head of the row, D / 16 neighbouring ones a head.
+template <typename X, int D, bool NEIGHBOURS, bool QUERIES, bool KEYS> __device__ __forceinline__ void append_row(const AppendArgs &a, uint32_t row, uint32_t slot_first, uint32_t slots_end, uint32_t step)
 {
-    typedef typename Vec8<T>::type TV;
     constexpr uint32_t kUnits = D / 16;
     const uint32_t seq = a.batch.sequence_of(row, a.max_new);
     if (seq >= a.batch.n_seqs) return;
-    const Place p(a, row, seq);
+    const Place p(a, row, seq, a.batch.first_row(seq), a.batch.rows_end(seq), a.batch.length(seq));
     const uint32_t unit = threadIdx.x % kUnits;
     const Unit<NEIGHBOURS> u(a, unit);
     const Angles mine = angles_of(a, row, p.pos, unit, u.turns);
     const uint32_t block = 1u << a.block_shift, in_block = p.in_page & (block - 1u);
-    for (uint32_t slot = slot_first; slot < slots_end; slot += step) {
-        const bool is_q = slot < a.n_heads, is_k = !is_q && slot < a.n_heads + a.n_kv_heads;
-        const uint32_t head = is_q ? slot : slot - a.n_heads - (is_k ? 0u : a.n_kv_heads);
-        if (is_q) {
-            if (!mine.given) continue;
+    uint32_t slot = slot_first;
+    if (QUERIES && mine.given) {
+#pragma unroll 4
+        for (; slot < min(slots_end, a.n_heads); slot += step) {
+            const uint32_t head = slot;
             const X *src = static_cast<const X *>(a.q) + row * a.q_row + head * a.q_head;
-            T *dst = static_cast<T *>(a.q_out) + row * a.q_out_row + head * a.q_out_head;
+            uint16_t *dst = static_cast<uint16_t *>(a.q_out) + row * a.q_out_row + head * a.q_out_head;
             Values v{widened(src + u.first), widened(src + u.second)};
             if (u.turns) v = turned<NEIGHBOURS>(v, mine);
-            __builtin_nontemporal_store(__builtin_convertvector(v.x, TV), reinterpret_cast<TV *>(dst + u.first));
-            __builtin_nontemporal_store(__builtin_convertvector(v.y, TV), reinterpret_cast<TV *>(dst + u.second));
-            continue;
+            dcdev::u32x4 x, y;
+            if (a.rows_f16) x = rounded<_Float16>(v.x), y = rounded<_Float16>(v.y);
+            else x = rounded<__bf16>(v.x), y = rounded<__bf16>(v.y);
+            __builtin_nontemporal_store(x, reinterpret_cast<dcdev::u32x4 *>(dst + u.first));
+            __builtin_nontemporal_store(y, reinterpret_cast<dcdev::u32x4 *>(dst + u.second));
         }
-        if (p.count == 0 || p.count > kFewRows) continue;
+    }
+    if (!KEYS || p.count == 0 || p.count > kFewRows) return;
+    for (slot = slot_first; slot < slots_end; slot += step) {
+        if (slot < a.n_heads) continue;
+        const bool is_k = slot < a.n_heads + a.n_kv_heads;
+        const uint32_t head = slot - a.n_heads - (is_k ? 0u : a.n_kv_heads);
         const uint64_t row_stride = is_k ? a.k_row : a.v_row;
         const X *src = (is_k ? static_cast<const X *>(a.k) + head * a.k_head : static_cast<const X *>(a.v) + head * a.v_head) + row * row_stride;
-        const uint64_t head_at = (uint64_t)(uint32_t)p.page * a.n_kv_heads + head;
-        float *scale_at = (is_k ? a.k_scales : a.v_scales) + (head_at << (a.batch.page_shift - a.block_shift)) + (p.in_page >> a.block_shift);
-        uint8_t *dst = static_cast<uint8_t *>(is_k ? a.k_pages : a.v_pages) + ((head_at << a.batch.page_shift) + p.in_page) * D;
-        const float before = in_block ? sound_scale(*scale_at) : 0.0f;
         auto values = [&](uint32_t i, bool &given) {
             const Angles t = i ? angles_of(a, row + i, p.pos + (int32_t)i, unit, u.turns) : mine;
             given = t.given;
@@ -184,27 +236,36 @@ template <typename X, typename T, int D, bool NEIGHBOURS> __device__ __forceinli
         };
         bool given;
         Values v = values(0, given);
-        float most = given ? largest_number(v) : 0.0f;
-        bool any = given;
+        const uint64_t head_at = (uint64_t)(uint32_t)max(p.entry, 0) * a.n_kv_heads + head;
+        float *scale_at = (is_k ? a.k_scales : a.v_scales) + (head_at << (a.batch.page_shift - a.block_shift)) + (p.in_page >> a.block_shift);
+        const float before = in_block ? sound_scale(*scale_at) : 0.0f;
+        const Most m(v);
+        float most = given ? m.value : 0.0f;
+        bool any = given, numbers = m.numbers;
+#pragma unroll 1
         for (uint32_t i = 1; i < p.count; i++) {
             bool g;
             const Values w = values(i, g);
-            if (g) most = fmaxf(most, largest_number(w)), any = true;
+            if (!g) continue;
+            const Most m(w);
+            most = fmaxf(most, m.value), any = true, numbers &= m.numbers;
         }
 #pragma unroll
         for (uint32_t k = 1; k < kUnits; k <<= 1) most = fmaxf(most, __shfl_xor(most, k));
-        if (!any) continue;
-        const float scale = fmaxf(scale_for(most), before), by = 1.0f / scale;
+        if (!any || p.entry < 0) continue;
+        uint8_t *dst = static_cast<uint8_t *>(is_k ? a.k_pages : a.v_pages) + ((head_at << a.batch.page_shift) + p.in_page) * D;
+        const float scale = fmaxf(scale_for(most), before), by = reciprocal(scale);
+#pragma unroll 1
         for (uint32_t i = 0; i < p.count; i++) {
             if (i) v = values(i, given);
             if (!given) continue;
-            *reinterpret_cast<u32x2 *>(dst + i * D + u.first) = whole_numbers(v.x, by);
-            *reinterpret_cast<u32x2 *>(dst + i * D + u.second) = whole_numbers(v.y, by);
+            *reinterpret_cast<u32x2 *>(dst + i * D + u.first) = whole_numbers(v.x, by, numbers);
+            *reinterpret_cast<u32x2 *>(dst + i * D + u.second) = whole_numbers(v.y, by, numbers);
         }
         if (in_block && scale != before) {
             const float less = before * by;
             uint8_t *at = dst - in_block * D + 16 * unit;
-#pragma unroll 4
+#pragma unroll 2
             for (uint32_t i = 0; i < in_block; i++) {
                 dcdev::u32x4 *e = reinterpret_cast<dcdev::u32x4 *>(at + i * D);
                 *e = in_larger_steps(*e, less);
@@ -214,33 +275,41 @@ template <typename X, typename T, int D, bool NEIGHBOURS> __device__ __forceinli
     }
 }
 
-// The blocks led by a row among `block` neighbouring ones that have more than a few new rows, for as many heads of keys or values as a workgroup
-// has threads for: a thread has 16 values of every so many of a block's rows.
-template <typename X, int D, bool NEIGHBOURS> __device__ __forceinline__ void append_blocks(const AppendArgs &a, uint32_t group, uint32_t slot_group, float *lds_most)
+// The blocks led by a row among `block` neighbouring ones that have more than a few new rows, of some heads of the keys or of the values, one after the
+// other.  A team of threads has a head's block, each of them 16 values of ROWS rows, whose cosines and sines it keeps for all heads.
+// Small blocks (up to 2048 values) are a wavefront's: no barrier; else the team is the workgroup, of 256 to 1024 threads, and the next head's values
+// are on their way while this head's maximum is found.  BIG: a block has more than 16 values for each of 1024 threads; those of its further rows are
+// read twice.
+template <typename X, int D, bool NEIGHBOURS, int ROWS, bool BIG> __device__ __forceinline__ void append_blocks(const AppendArgs &a, uint32_t group, bool is_k, uint32_t head_first,
+                                                                                                                uint32_t heads, uint32_t (&lds_most)[2][kMostThreads / 64])
 {
+    constexpr bool kWave = ROWS > 0; // ROWS 0: the workgroup, a row to a thread
+    constexpr int kRows = kWave ? ROWS : 1;
     constexpr uint32_t kUnits = D / 16;
     const uint32_t block = 1u << a.block_shift, lane = threadIdx.x & 63u;
-    const uint32_t slot_threads = min(kThreads, kUnits * block), tokens = slot_threads / kUnits; // of a head; of those, rows at a time
-    const uint32_t slot = slot_group * (kThreads / slot_threads) + threadIdx.x / slot_threads;
-    const bool is = slot < 2 * a.n_kv_heads, is_k = slot < a.n_kv_heads;
-    const uint32_t head = is_k ? slot : slot - a.n_kv_heads;
-    const uint32_t t = threadIdx.x % slot_threads, unit = t % kUnits, token = t / kUnits;
+    const uint32_t t = kWave ? lane : threadIdx.x, tokens = (kWave ? 64u : blockDim.x) / kUnits; // rows at a time
+    const uint32_t unit = t % kUnits, token = t / kUnits;
     const Unit<NEIGHBOURS> u(a, unit);
-    const uint64_t row_stride = is_k ? a.k_row : a.v_row;
-    const X *heads = is_k ? static_cast<const X *>(a.k) + head * a.k_head : static_cast<const X *>(a.v) + head * a.v_head;
+    const bool turns = is_k && u.turns, all_turn = is_k && a.rot_dim == D;
+    const uint64_t row_stride = is_k ? a.k_row : a.v_row, head_stride = is_k ? a.k_head : a.v_head;
+    const X *rows = static_cast<const X *>(is_k ? a.k : a.v);
+    float *scales = is_k ? a.k_scales : a.v_scales;
+    uint8_t *pages = static_cast<uint8_t *>(is_k ? a.k_pages : a.v_pages);
 
     for (uint32_t r = group * block; r < min((group + 1) * block, a.batch.n_rows); r += 64) {
         // a lane to a row: its sequence, by halving
         const uint32_t my_row = r + lane;
-        const bool mine = lane < block && my_row < a.batch.n_rows;
         uint32_t low = 0, high = a.batch.n_seqs; // the last sequence that begins at or before the row, and as rows follow one another the only one that has it
         while (high - low > 1) {
             const uint32_t mid = (low + high) / 2;
             if (a.batch.first_row(mid) <= my_row) low = mid;
             else high = mid;
         }
-        const bool has = mine && a.batch.first_row(low) <= my_row && my_row < a.batch.rows_end(low) && my_row - a.batch.first_row(low) < a.max_new;
-        const Place p(a, has ? my_row : 0, has ? low : a.batch.n_seqs);
+        const uint32_t first_row = a.batch.first_row(low), rows_end = a.batch.rows_end(low);
+        const int32_t length = a.batch.length(low);
+        const bool has = lane < block && my_row < a.batch.n_rows && first_row <= my_row && my_row < rows_end && my_row - first_row < a.max_new;
+        // (a row that no sequence has is as if at a position below zero)
+        const Place p(a, has ? my_row : 0, low, has ? first_row : 0, has ? rows_end : 1, has ? length : 0);
         uint64_t leaders = __ballot(p.count > kFewRows);
         while (leaders) {
             const int l = __builtin_ctzll(leaders);
@@ -248,105 +317,231 @@ template <typename X, int D, bool NEIGHBOURS> __device__ __forceinline__ void ap
             const uint32_t row = r + (uint32_t)l, count = (uint32_t)__builtin_amdgcn_readlane((int)p.count, l);
             const uint32_t in_page = (uint32_t)__builtin_amdgcn_readlane((int)p.in_page, l), in_block = in_page & (block - 1u);
             const int32_t pos = __builtin_amdgcn_readlane(p.pos, l);
-            const uint64_t head_at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(p.page, l) * a.n_kv_heads + head;
-            float *scale_at = (is_k ? a.k_scales : a.v_scales) + (head_at << (a.batch.page_shift - a.block_shift)) + (in_page >> a.block_shift);
-            uint8_t *dst = static_cast<uint8_t *>(is_k ? a.k_pages : a.v_pages) + ((head_at << a.batch.page_shift) + in_page) * D;
-            const float before = is && in_block ? sound_scale(*scale_at) : 0.0f;
-            auto values = [&](uint32_t i, bool &given) {
-                const Angles t = angles_of(a, row + i, pos + (int32_t)i, unit, u.turns);
-                given = t.given;
-                const X *src = heads + (row + i) * row_stride;
-                Values v{widened(src + u.first), widened(src + u.second)};
-                return is_k && u.turns ? turned<NEIGHBOURS>(v, t) : v;
-            };
-            float most = -1.0f; // none
-            if (is)
-                for (uint32_t i = token; i < count; i += tokens) {
-                    bool given;
-                    const Values v = values(i, given);
-                    if (given) most = fmaxf(most, largest_number(v));
-                }
+            const uint32_t heads_end = head_first + heads;
+            Angles angles[kRows];
+            bool given[kRows];
 #pragma unroll
-            for (int k = 1; k < 64; k <<= 1) most = fmaxf(most, __shfl_xor(most, k));
-            if (lane == 0) lds_most[threadIdx.x >> 6] = most;
-            __syncthreads();
-            for (uint32_t w = 0; w < slot_threads / 64; w++) most = fmaxf(most, lds_most[(threadIdx.x / slot_threads) * (slot_threads / 64) + w]);
-            __syncthreads();
-            if (!is || most < 0.0f) continue;
-            const float scale = fmaxf(scale_for(most), before), by = 1.0f / scale;
-            for (uint32_t i = token; i < count; i += tokens) {
-                bool given;
-                const Values v = values(i, given);
-                if (!given) continue;
-                *reinterpret_cast<u32x2 *>(dst + i * D + u.first) = whole_numbers(v.x, by);
-                *reinterpret_cast<u32x2 *>(dst + i * D + u.second) = whole_numbers(v.y, by);
+            for (int i = 0; i < kRows; i++) {
+                const uint32_t n = min(token + i * tokens, count - 1);
+                angles[i] = angles_of(a, row + n, pos + (int32_t)n, unit, turns);
+                given[i] = token + i * tokens < count && angles[i].given;
             }
-            if (in_block && scale != before) {
-                const float less = before * by;
-                for (uint32_t i = token; i < in_block; i += tokens) {
-                    dcdev::u32x4 *e = reinterpret_cast<dcdev::u32x4 *>(dst - (in_block - i) * D + 16 * unit);
-                    *e = in_larger_steps(*e, less);
+            const X *first = rows + (row + token) * row_stride;
+            Raw<X> next[kRows] = {};
+            auto load = [&](uint32_t head) {
+                const X *src = first + head * head_stride;
+#pragma unroll
+                for (int i = 0; i < kRows; i++)
+                    if (given[i]) next[i].load(src + i * tokens * row_stride + u.first, src + i * tokens * row_stride + u.second);
+            };
+            load(head_first);
+            const int32_t entry = __builtin_amdgcn_readlane(p.entry, l);
+            if (entry < 0) continue;
+            const uint64_t page = (uint32_t)entry;
+            auto scale_at = [&](uint32_t head) {
+                return scales + (((page * a.n_kv_heads + head) << (a.batch.page_shift - a.block_shift)) + (in_page >> a.block_shift));
+            };
+            // of the rows that a thread comes to behind its first one
+            auto further = [&](const X *src, auto use) {
+                if constexpr (BIG) {
+#pragma unroll 1
+                    for (uint32_t n = token + tokens; n < count; n += tokens) {
+                        const Angles w = angles_of(a, row + n, pos + (int32_t)n, unit, turns);
+                        if (!w.given) continue;
+                        const X *at = src + (n - token) * row_stride;
+                        const Values x{widened(at + u.first), widened(at + u.second)};
+                        use(n, turns ? turned<NEIGHBOURS>(x, w) : x);
+                    }
                 }
+            };
+            uint32_t buffer = 0;
+#pragma unroll 1
+            for (uint32_t head = head_first; head < heads_end; head++, buffer ^= 1u) {
+                const X *src = first + head * head_stride;
+                const float before = in_block ? sound_scale(*scale_at(head)) : 0.0f;
+                Values v[kRows];
+                uint32_t most = 0; // bits of the largest magnitude and 1 more; 0: there are no values
+                bool numbers = true;
+                auto look = [&](const Values &v) {
+                    const Most m(v);
+                    most = max(most, __float_as_uint(m.value) + 1u), numbers &= m.numbers;
+                };
+#pragma unroll
+                for (int i = 0; i < kRows; i++) {
+                    v[i] = next[i].values();
+                    if (all_turn) {
+                        v[i] = turned<NEIGHBOURS>(v[i], angles[i]);
+                    } else if (turns) {
+                        dcdev::keep_order();
+                        v[i] = turned<NEIGHBOURS>(v[i], angles[i]);
+                    }
+                }
+                if (head + 1 < heads_end) load(head + 1);
+#pragma unroll
+                for (int i = 0; i < kRows; i++)
+                    if (given[i]) look(v[i]);
+                further(src, [&](uint32_t, const Values &x) { look(x); });
+                most = largest_of_lanes(most);
+                if constexpr (!kWave) {
+                    if (lane == 0) lds_most[buffer][threadIdx.x >> 6] = most;
+                    __syncthreads();
+                    const uint32_t of_wave = lds_most[buffer][lane & 15u];
+                    most = largest_of_lanes((lane & 15u) < blockDim.x / 64 ? of_wave : 0u);
+                }
+                if (!most) continue;
+                const float scale = fmaxf(scale_for(__uint_as_float(most - 1u)), before), by = reciprocal(scale);
+                uint8_t *dst = pages + (((page * a.n_kv_heads + head) << a.batch.page_shift) + in_page) * D;
+                auto store = [&](uint32_t n, const Values &x) {
+                    *reinterpret_cast<u32x2 *>(dst + n * D + u.first) = whole_numbers(x.x, by, numbers);
+                    *reinterpret_cast<u32x2 *>(dst + n * D + u.second) = whole_numbers(x.y, by, numbers);
+                };
+#pragma unroll
+                for (int i = 0; i < kRows; i++)
+                    if (given[i]) store(token + i * tokens, v[i]);
+                further(src, store);
+                if (in_block && scale != before) {
+                    const float less = before * by;
+#pragma unroll 1
+                    for (uint32_t i = token; i < in_block; i += tokens) {
+                        dcdev::u32x4 *e = reinterpret_cast<dcdev::u32x4 *>(dst - (in_block - i) * D + 16 * unit);
+                        *e = in_larger_steps(*e, less);
+                    }
+                }
+                if (t == 0) *scale_at(head) = scale;
             }
-            if (t == 0) *scale_at = scale;
+            if constexpr (!kWave) __syncthreads(); // the next leader begins with the first buffer again
         }
     }
 }
 
-// A launch's items: rows, each in row_parts parts of part_slots heads (queries, then keys, then values); and `block` neighbouring rows for each
-// of slot_groups groups of heads.
-struct Work {
-    uint64_t row_items, block_items;
-    uint32_t row_parts, part_slots, slot_groups;
+// Blocks: items are `block` neighbouring rows for each of head_groups groups of `heads` heads of keys and of values by turns; those of the same rows go to
+// one XCD (a workgroup's is its number modulo 8), for they read the same cosines.
+struct BlockWork {
+    uint64_t items;
+    uint32_t head_groups, heads;
 };
-
-template <typename X, typename T, int D, bool NEIGHBOURS> __global__ __launch_bounds__(kThreads) void dc_kv_append_i8_kernel(AppendArgs a, Work w)
+template <typename X, int D, bool NEIGHBOURS, int ROWS, bool BIG> __device__ __forceinline__ void block_item(const AppendArgs &a, const BlockWork &w, uint64_t item,
+                                                                                                             uint32_t (&most)[2][kMostThreads / 64])
 {
-    __shared__ float most[kThreads / 64];
-    constexpr uint32_t kStep = kThreads / (D / 16);
-    for (uint64_t item = blockIdx.x; item < w.row_items + w.block_items; item += gridDim.x) {
-        if (item < w.row_items) {
-            const uint32_t row = (uint32_t)(item / w.row_parts), begin = (uint32_t)(item % w.row_parts) * w.part_slots;
-            append_row<X, T, D, NEIGHBOURS>(a, row, begin + threadIdx.x / (D / 16), min(a.n_heads + 2 * a.n_kv_heads, begin + w.part_slots), kStep);
-        } else {
-            append_blocks<X, D, NEIGHBOURS>(a, (uint32_t)((item - w.row_items) / w.slot_groups), (uint32_t)((item - w.row_items) % w.slot_groups), most);
+    constexpr uint32_t kTeams = ROWS ? kThreads / 64 : 1;
+    const uint32_t wave = ROWS ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+    const uint32_t eight = (uint32_t)(item >> 3) * kTeams + wave; // of eight groups of rows
+    const uint32_t part = eight % (2 * w.head_groups), head = part / 2 * w.heads;
+    append_blocks<X, D, NEIGHBOURS, ROWS, BIG>(a, eight / (2 * w.head_groups) * 8 + (uint32_t)(item & 7u), part % 2 == 0, head, min(w.heads, a.n_kv_heads - head), most);
+}
+
+// Rows: each in `parts` parts of part_slots heads (queries, then keys, then values, from number first_slot on), which row_threads threads go through.
+struct RowWork {
+    uint64_t items;
+    uint32_t first_slot, slots_end, parts, part_slots, row_threads;
+};
+template <typename X, int D, bool NEIGHBOURS, bool QUERIES, bool KEYS> __device__ __forceinline__ void row_item(const AppendArgs &a, const RowWork &w, uint64_t item)
+{
+    const uint32_t team = __builtin_amdgcn_readfirstlane(threadIdx.x / w.row_threads), thread = threadIdx.x % w.row_threads;
+    const uint64_t i = item * (blockDim.x / w.row_threads) + team, row = i / w.parts;
+    const uint32_t begin = w.first_slot + (uint32_t)(i % w.parts) * w.part_slots;
+    if (row < a.batch.n_rows)
+        append_row<X, D, NEIGHBOURS, QUERIES, KEYS>(a, (uint32_t)row, begin + thread / (D / 16), min(w.slots_end, begin + w.part_slots), w.row_threads / (D / 16));
+}
+
+template <typename X, int D, bool NEIGHBOURS, int ROWS, bool BIG> __global__ __launch_bounds__(ROWS ? kThreads : kMostThreads) void dc_kv_append_i8_blocks_kernel(AppendArgs a, BlockWork w)
+{
+    __shared__ uint32_t most[2][kMostThreads / 64];
+    for (uint64_t item = blockIdx.x; item < w.items; item += gridDim.x) block_item<X, D, NEIGHBOURS, ROWS, BIG>(a, w, item, most);
+}
+template <typename X, int D, bool NEIGHBOURS, bool QUERIES, bool KEYS> __global__ __launch_bounds__(kThreads) void dc_kv_append_i8_rows_kernel(AppendArgs a, RowWork w)
+{
+    for (uint64_t item = blockIdx.x; item < w.items; item += gridDim.x) row_item<X, D, NEIGHBOURS, QUERIES, KEYS>(a, w, item);
+}
+// Both in one launch, where there is little to do.
+template <typename X, int D, bool NEIGHBOURS, int ROWS> __global__ __launch_bounds__(ROWS ? kThreads : kMostThreads) void dc_kv_append_i8_both_kernel(AppendArgs a, BlockWork b, RowWork r)
+{
+    __shared__ uint32_t most[2][kMostThreads / 64];
+    if (blockIdx.x < b.items) block_item<X, D, NEIGHBOURS, ROWS, false>(a, b, blockIdx.x, most);
+    else row_item<X, D, NEIGHBOURS, true, true>(a, r, blockIdx.x - b.items);
+}
+
+constexpr uint64_t kMostItems = 1u << 21; // of a grid; what is beyond is the same workgroups' too
+
+// Rows' heads from number `first` to `end` on.
+template <int D> RowWork row_work(uint32_t rows, uint32_t first, uint32_t end, uint32_t row_threads, uint32_t threads)
+{
+    const uint32_t step = row_threads / (D / 16), slots = end - first, teams = threads / row_threads;
+    RowWork r = {};
+    r.first_slot = first, r.slots_end = end, r.row_threads = row_threads;
+    r.parts = rows < 512 ? (slots + step - 1) / step : 1;
+    r.part_slots = r.parts > 1 ? step : slots;
+    r.items = ((uint64_t)rows * r.parts + teams - 1) / teams;
+    return r;
+}
+template <typename X, int D, bool NEIGHBOURS, bool QUERIES, bool KEYS> void launch_rows(const AppendArgs &a, const RowWork &r, hipStream_t stream)
+{
+    hipLaunchKernelGGL((dc_kv_append_i8_rows_kernel<X, D, NEIGHBOURS, QUERIES, KEYS>), dim3((uint32_t)std::min(r.items, kMostItems)), dim3(kThreads), 0, stream, a, r);
+}
+
+template <typename X, int D, bool NEIGHBOURS, int ROWS, bool BIG> void launch_n(const AppendArgs &a, const BlockWork &b, uint32_t threads, hipStream_t stream)
+{
+    const uint32_t rows = a.batch.n_rows, slots = a.n_heads + 2 * a.n_kv_heads;
+    // One launch is shorter than several (264 rows of 32/8 heads: 5.1 and 10.0 us); with several each part has its own number of registers and threads.
+    if constexpr (!BIG) {
+        const RowWork r = row_work<D>(rows, 0, slots, kThreads, threads);
+        if (rows < 512 && b.items + r.items <= kMostItems) {
+            hipLaunchKernelGGL((dc_kv_append_i8_both_kernel<X, D, NEIGHBOURS, ROWS>), dim3((uint32_t)(b.items + r.items)), dim3(threads), 0, stream, a, b, r);
+            return;
         }
+    }
+    hipLaunchKernelGGL((dc_kv_append_i8_blocks_kernel<X, D, NEIGHBOURS, ROWS, BIG>), dim3((uint32_t)std::min(b.items, kMostItems)), dim3(threads), 0, stream, a, b);
+    // Queries apart from the blocks with few rows, which take twice the registers, if they are worth a launch (8192 rows of 40/40 heads of 128: 101
+    // instead of 107 us; 2048 rows of 32/8 17.6 instead of 16.1, 32768 rows of 16/2 of 64 58 instead of 47).
+    if (rows >= 4096 && a.n_heads * D >= 4096) {
+        launch_rows<X, D, NEIGHBOURS, false, true>(a, row_work<D>(rows, a.n_heads, slots, 64, kThreads), stream);
+        launch_rows<X, D, NEIGHBOURS, true, false>(a, row_work<D>(rows, 0, a.n_heads, kThreads, kThreads), stream);
+    } else {
+        launch_rows<X, D, NEIGHBOURS, true, true>(a, row_work<D>(rows, 0, slots, rows >= 512 && slots * (D / 16) <= 128 ? 64 : kThreads, kThreads), stream);
     }
 }
 
-template <typename X, typename T, int D> void launch_d(const AppendArgs &a, bool neighbours, hipStream_t stream)
+template <typename X, int D, bool NEIGHBOURS> void launch_d(const AppendArgs &a, hipStream_t stream)
 {
-    const uint32_t block = 1u << a.block_shift, rows = a.batch.n_rows, slots = a.n_heads + 2 * a.n_kv_heads, step = kThreads / (D / 16);
-    Work w = {};
-    w.row_parts = rows < 512 ? (slots + step - 1) / step : 1;
-    w.part_slots = w.row_parts > 1 ? step : slots;
-    w.row_items = (uint64_t)rows * w.row_parts;
-    const uint32_t slot_threads = std::min<uint32_t>(kThreads, D / 16 * block), a_group = kThreads / slot_threads;
-    w.slot_groups = (2 * a.n_kv_heads + a_group - 1) / a_group;
-    if (a.max_new > kFewRows) w.block_items = (uint64_t)((rows + block - 1) / block) * w.slot_groups;
-    const dim3 grid((uint32_t)std::min<uint64_t>(w.row_items + w.block_items, 1u << 23)); // what is beyond is the same workgroups' too
-    if (neighbours) hipLaunchKernelGGL((dc_kv_append_i8_kernel<X, T, D, true>), grid, dim3(kThreads), 0, stream, a, w);
-    else hipLaunchKernelGGL((dc_kv_append_i8_kernel<X, T, D, false>), grid, dim3(kThreads), 0, stream, a, w);
+    const uint32_t block = 1u << a.block_shift, rows = a.batch.n_rows, slots = a.n_heads + 2 * a.n_kv_heads;
+    if (a.max_new <= kFewRows) { // no block has more
+        launch_rows<X, D, NEIGHBOURS, true, true>(a, row_work<D>(rows, 0, slots, rows >= 512 && slots * (D / 16) <= 128 ? 64 : kThreads, kThreads), stream);
+        return;
+    }
+    const bool small = block * D <= 2048;
+    const uint32_t threads = small ? kThreads : std::min(D / 16 * block, kMostThreads), teams = small ? kThreads / 64 : 1;
+    const uint64_t groups = (rows + block - 1) / block;
+    BlockWork b = {};
+    b.heads = 1;
+    while (b.heads < a.n_kv_heads && b.heads < 8 && groups * 2 * ((a.n_kv_heads + b.heads - 1) / b.heads) * (small ? 64 : threads) > 2048 * kThreads) b.heads++;
+    b.head_groups = (a.n_kv_heads + b.heads - 1) / b.heads;
+    b.items = ((groups + 7) / 8 * 2 * b.head_groups + teams - 1) / teams * 8;
+    if (!small && D / 16 * block > kMostThreads) launch_n<X, D, NEIGHBOURS, 0, true>(a, b, threads, stream);
+    else if (!small) launch_n<X, D, NEIGHBOURS, 0, false>(a, b, threads, stream);
+    else if constexpr (D < 256) {
+        if (D == 128 || block == 32) launch_n<X, D, NEIGHBOURS, 2, false>(a, b, threads, stream);
+        else if constexpr (D == 64) launch_n<X, D, NEIGHBOURS, 1, false>(a, b, threads, stream);
+    }
 }
 
-template <typename X, typename T> void launch(const AppendArgs &a, uint32_t head_dim, bool neighbours, hipStream_t stream)
+template <typename X, int D> void launch_p(const AppendArgs &a, bool neighbours, hipStream_t stream)
 {
-    if (head_dim == 64) launch_d<X, T, 64>(a, neighbours, stream);
-    else if (head_dim == 128) launch_d<X, T, 128>(a, neighbours, stream);
-    else launch_d<X, T, 256>(a, neighbours, stream);
+    if (neighbours) launch_d<X, D, true>(a, stream);
+    else launch_d<X, D, false>(a, stream);
 }
 
-template <typename X> void launch_t(const AppendArgs &a, uint32_t rows_type, uint32_t head_dim, bool neighbours, hipStream_t stream)
+template <typename X> void launch(const AppendArgs &a, uint32_t head_dim, bool neighbours, hipStream_t stream)
 {
-    if (rows_type == DC_TYPE_BF16) launch<X, __bf16>(a, head_dim, neighbours, stream);
-    else launch<X, _Float16>(a, head_dim, neighbours, stream);
+    if (head_dim == 64) launch_p<X, 64>(a, neighbours, stream);
+    else if (head_dim == 128) launch_p<X, 128>(a, neighbours, stream);
+    else launch_p<X, 256>(a, neighbours, stream);
 }
 
 } // namespace
 
-void dccache::launch_i8(const AppendArgs &a, uint32_t x_type, uint32_t rows_type, uint32_t head_dim, bool neighbours, hipStream_t stream)
+void dccache::launch_i8(const AppendArgs &a, uint32_t x_type, uint32_t head_dim, bool neighbours, hipStream_t stream)
 {
-    if (x_type == DC_TYPE_BF16) launch_t<__bf16>(a, rows_type, head_dim, neighbours, stream);
-    else if (x_type == DC_TYPE_F16) launch_t<_Float16>(a, rows_type, head_dim, neighbours, stream);
-    else launch_t<float>(a, rows_type, head_dim, neighbours, stream);
+    if (x_type == DC_TYPE_BF16) launch<__bf16>(a, head_dim, neighbours, stream);
+    else if (x_type == DC_TYPE_F16) launch<_Float16>(a, head_dim, neighbours, stream);
+    else launch<float>(a, head_dim, neighbours, stream);
 }
