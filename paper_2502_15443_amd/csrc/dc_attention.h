@@ -189,7 +189,11 @@ constexpr uint32_t kTileRows = 128; // of a workgroup of the kernel for many row
 enum Kind { kFew16 = 0, kFew32 = 1, kTile = 2 };
 struct Plan {
     Kind prefix_kind, own_kind;
+    uint32_t tile_rows; // of a workgroup of the kernel for many rows
 };
+// Over a cache of 8 bits a workgroup has up to this many rows (of heads of 64 and 256 a half less: a wavefront's part of a tile is no whole load, or registers
+// are for four wavefronts only).
+constexpr uint32_t wide_tile_rows(uint32_t head_dim) { return head_dim == 128 ? 2 * kTileRows : kTileRows; }
 
 // Tokens of a tile of the kernel for few rows over a cache of 8 bits: 64, or with 32 rows, which leave fewer registers, 32.
 constexpr int few_tile(int row_tiles) { return row_tiles == 1 ? 64 : 32; }

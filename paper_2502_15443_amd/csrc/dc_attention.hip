@@ -888,11 +888,13 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     auto kind_of = [&](uint64_t rows) { return rows <= 16 ? kFew16 : rows <= 32 && d < 256 ? kFew32 : kTile; };
     const uint64_t all_rows = batch->n_rows * group, seq_rows = batch->max_new * group;
     const Kind prefix_kind = kind_of(all_rows), own_kind = kind_of(seq_rows);
-    plan = Plan{prefix_kind, own_kind};
+    // (only where the kernel for many rows has the launch to itself)
+    const uint64_t tile_rows = cache->type == DC_TYPE_I8 && own_kind == kTile && seq_rows > kTileRows ? wide_tile_rows((uint32_t)d) : kTileRows;
+    plan = Plan{prefix_kind, own_kind, (uint32_t)tile_rows};
     const uint64_t own_len = batch->max_len > prefix_len ? batch->max_len - prefix_len : 1;
-    const uint64_t seq_tiles = (seq_rows + kTileRows - 1) / kTileRows; // workgroups to a sequence's rows
+    const uint64_t seq_tiles = (seq_rows + tile_rows - 1) / tile_rows; // workgroups to a sequence's rows
     // upper bound of the workgroups' number, as the kernel counts them off
-    const uint64_t row_tiles = !batch->row_start_dev ? batch->n_seqs * seq_tiles : std::min<uint64_t>(all_rows / kTileRows + batch->n_seqs, all_rows);
+    const uint64_t row_tiles = !batch->row_start_dev ? batch->n_seqs * seq_tiles : std::min<uint64_t>(all_rows / tile_rows + batch->n_seqs, all_rows);
     const uint64_t tile_many = d == 256 ? 32 : 64;
     const Kind few_kind = prefix_len && prefix_kind != kTile ? prefix_kind : own_kind; // of the kernel for few rows, if one runs
     const uint64_t tile_few = cache->type == DC_TYPE_I8 ? few_tile(few_kind == kFew16 ? 1 : 2) : 32;
@@ -938,9 +940,9 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     auto seen = [&](uint64_t tokens, uint64_t rows) { return t->window ? std::min(tokens, (uint64_t)t->window + rows + t->sinks + 64) : tokens; };
     // a sequence's many rows, over their own pages or over the prefix along with them
     auto many_part = [&](bool along) {
-        const uint64_t longest = along ? prefix_len + own_len : own_len, rows = kTileRows / group + 1;
+        const uint64_t longest = along ? prefix_len + own_len : own_len, rows = tile_rows / group + 1;
         const uint64_t tokens = seen(longest, rows), fewer = seen(longest > batch->max_new ? longest - batch->max_new : 1, rows);
-        const uint64_t filled = std::max<uint64_t>(1, all_rows / kTileRows); // of the workgroups counted off, about
+        const uint64_t filled = std::max<uint64_t>(1, all_rows / tile_rows); // of the workgroups counted off, about
         return part(cache->n_kv_heads * row_tiles, tokens, tile_many, cut_many(cache->n_kv_heads * filled, tokens, fewer, a.prefix.blocks != 0), a.prefix.n_splits);
     };
     // A sequence's many rows read the prefix along with their own pages where that is estimated to cost less than to read it once for all sequences' rows
@@ -952,7 +954,7 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     // 36 rows behind 512 40 and 66, behind 16384 500 and 208, there with a window of 12000 371 and 163, of 1500 54 and 68.
     if (prefix_len && own_kind == kTile) {
         const Part along = many_part(true);
-        const uint64_t shared_tiles = (all_rows + kTileRows - 1) / kTileRows;
+        const uint64_t shared_tiles = (all_rows + tile_rows - 1) / tile_rows;
         const uint64_t more_tiles = batch->n_seqs * seq_tiles - std::min(batch->n_seqs * seq_tiles, shared_tiles);
         const int64_t behind = (int64_t)own_len - (int64_t)(batch->max_new + 1) / 2;
         const uint64_t prefix_seen = t->window ? std::min<uint64_t>(prefix_len, std::max<int64_t>((int64_t)t->window - behind, 0) + t->sinks) : prefix_len;
@@ -965,7 +967,7 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     if (prefix_len && !a.whole) {
         const uint64_t tokens = seen(prefix_len, batch->max_new);
         if (prefix_kind == kTile) {
-            const uint64_t items = cache->n_kv_heads * ((all_rows + kTileRows - 1) / kTileRows);
+            const uint64_t items = cache->n_kv_heads * ((all_rows + tile_rows - 1) / tile_rows);
             a.prefix = part(items, tokens, tile_many, cut_many(items, tokens, tokens, true), 0);
         } else {
             a.prefix = part(cache->n_kv_heads, tokens, tile_few, cut_few(cache->n_kv_heads, tokens), 0);

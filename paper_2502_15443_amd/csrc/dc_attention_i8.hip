@@ -412,18 +412,20 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
 // units bound this kernel.  Keys and values go through the LDS in tiles that its four wavefronts share, made 16 bits wide on their way, double buffered
 // with one barrier a tile; a wavefront owns 32 rows.  Scores as [token][row] = K Q^T, results as [head_dim][row] = V^T P^T in the 32x32x16 shape; maxima and
 // sums stay in a lane but for one exchange between the halves.
-template <int D> struct TileLds {
+template <int D, int WAVES> struct TileLds {
     static constexpr int kTile = D == 256 ? 32 : 64; // tokens
     uint8_t k[2][kTile * 2 * D], v[2][kTile * 2 * D];
-    int32_t p[kTileRows];
-    f32x2 scale[2][4]; // of the tokens that each wavefront brings: of keys, of values
+    int32_t p[32 * WAVES];
+    f32x2 scale[2][WAVES]; // of the tokens that each wavefront brings: of keys, of values
 };
 
-template <typename T, int D> __device__ __forceinline__ void many_rows(const AttentionArgs &a, TileLds<D> &lds, bool common, uint32_t block)
+template <typename T, int D, int WAVES> __device__ __forceinline__ void many_rows(const AttentionArgs &a, TileLds<D, WAVES> &lds, bool common, uint32_t block)
 {
-    constexpr int kTile = TileLds<D>::kTile, KS = D / 16, DT = D / 32, HT = kTile / 32; // HT: 32-token products of a tile
-    constexpr uint32_t kRows = kTileRows, kRowBytes = 2 * D, kChunks = D / 16, kRowsALoad = 64 / kChunks; // rows: in the LDS; chunks: of 16 bytes in the cache
-    constexpr int kTokens = kTile / 4, kLoads = kTokens / (int)kRowsALoad; // tokens that a wavefront brings, in so many loads
+    typedef TileLds<D, WAVES> Lds;
+    constexpr int kTile = Lds::kTile, KS = D / 16, DT = D / 32, HT = kTile / 32; // HT: 32-token products of a tile
+    constexpr uint32_t kRows = 32 * WAVES, kRowBytes = 2 * D, kChunks = D / 16, kRowsALoad = 64 / kChunks; // rows: in the LDS; chunks: of 16 bytes in the cache
+    constexpr int kTokens = kTile / WAVES, kLoads = kTokens / (int)kRowsALoad; // tokens that a wavefront brings, in so many loads
+    constexpr int kKnown = 64 / WAVES; // tiles that are known at once
     constexpr uint32_t kBuffer = kTile * kRowBytes;
 
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31u, half = lane >> 5;
@@ -482,18 +484,23 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
     int32_t p_min, p_max, wave_p_min, wave_p_max, my_p;
     const uint32_t my_row = i_first + wave * 32 + c;
     if (common) {
-        for (uint32_t i = threadIdx.x; i < kRows; i += 256) lds.p[i] = kNoPosition;
+        for (uint32_t i = threadIdx.x; i < kRows; i += 64 * WAVES) lds.p[i] = kNoPosition;
         __syncthreads();
         const uint32_t r_low = i_first / a.group, r_high = min((i_first + kRows - 1) / a.group + 1, a.batch.n_rows);
-        for (uint32_t b = threadIdx.x; b < a.batch.n_seqs; b += 256) {
+        for (uint32_t b = threadIdx.x; b < a.batch.n_seqs; b += 64 * WAVES) {
             const uint32_t first = a.batch.first_row(b), end = a.batch.rows_end(b);
             const int32_t len = first < end ? a.batch.length(b) : 0;
             for (uint32_t r = max(first, r_low); r < min(end, r_high); r++)
                 for (uint32_t i = max(r * a.group, i_first); i < min((r + 1) * a.group, i_first + kRows); i++) lds.p[i - i_first] = len - (int32_t)(end - r);
         }
         __syncthreads();
-        const int32_t p0 = lds.p[lane], p1 = lds.p[lane + 64];
-        range_of_positions(p0 == kNoPosition ? p1 : p1 == kNoPosition ? p0 : min(p0, p1), max(p0, p1), p_min, p_max);
+        int32_t p_low = kNoPosition, p_high = kNoPosition;
+#pragma unroll
+        for (uint32_t i = 0; i < kRows; i += 64) {
+            const int32_t p = lds.p[i + lane];
+            p_low = p_low == kNoPosition ? p : p == kNoPosition ? p_low : min(p_low, p), p_high = max(p_high, p);
+        }
+        range_of_positions(p_low, p_high, p_min, p_max);
         const int32_t p = lds.p[wave * 32 + c];
         range_of_positions(p, p, wave_p_min, wave_p_max);
         my_p = lds.p[wave * 32 + c];
@@ -547,52 +554,52 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
     const uint64_t page_stride = (uint64_t)a.n_kv_heads << a.batch.page_shift;
     const uint64_t head_at = (uint64_t)kv << a.batch.page_shift;
     const uint32_t place_mask = (1u << a.batch.page_shift) - 1u;
-    // What there is to know of 16 tiles, 16 tiles ahead: lane l has, of tile i + l / 4 counted from t_begin, where the tokens that wavefront l mod 4
-    // brings lie in the pools (in bytes; where there is no page, those of page 0, which are then taken for hidden), and the tile's
+    // What there is to know of kKnown tiles, so many tiles ahead: lane l has, of tile i + l / WAVES counted from t_begin, where the tokens that wavefront
+    // l mod WAVES brings lie in the pools (in bytes; where there is no page, those of page 0, which are then taken for hidden), and the tile's
     // flags.  A tile's step takes its own with three reads of a lane.  (Scalar loads would do for the pages, but the LDS's data are waited
     // for by the same counter, all of it.)
     enum : uint32_t {
-        kThere = 15,    // a bit for each wavefront's tokens: they are there
-        kPrefix = 16,   // of the prefix's table
-        kSome = 64,     // this wavefront's rows see some of it,
-        kEdge = 128     // and not all of it
+        kThere = (1 << WAVES) - 1, // a bit for each wavefront's tokens: they are there
+        kPrefix = 256,  // of the prefix's table
+        kSome = 512,    // this wavefront's rows see some of it,
+        kEdge = 1024    // and not all of it
     };
     struct Known {
         uint32_t low, high, flags;
         float ks, vs;
     };
     auto pages_from = [&](int32_t i) {
-        const int32_t t = t_begin + i + (int32_t)(lane >> 2), j = first_token(t) + (int32_t)(lane & 3u) * kTokens;
+        const int32_t t = t_begin + i + (int32_t)(lane / WAVES), j = first_token(t) + (int32_t)(lane % WAVES) * kTokens;
         const bool in_prefix = t < prefix_tiles.count;
         int32_t e = -1;
         if (t < t_end && j < (in_prefix ? base : all_last.high)) e = in_prefix ? prefix_table[(uint32_t)j >> a.batch.page_shift] : own_table[(uint32_t)(j - base) >> a.batch.page_shift];
         return (uint32_t)e < a.batch.n_pages ? e : -1;
     };
     auto known_from = [&](int32_t i, int32_t page) {
-        const int32_t t = t_begin + i + (int32_t)(lane >> 2), j = first_token(t);
+        const int32_t t = t_begin + i + (int32_t)(lane / WAVES), j = first_token(t);
         const bool in_prefix = t < prefix_tiles.count;
-        const uint32_t place = (uint32_t)(j + (int32_t)(lane & 3u) * kTokens - (in_prefix ? 0 : base)) & place_mask;
+        const uint32_t place = (uint32_t)(j + (int32_t)(lane % WAVES) * kTokens - (in_prefix ? 0 : base)) & place_mask;
         const uint64_t token = page_stride * (uint32_t)max(page, 0) + head_at + place, at = token * D;
-        const uint32_t there4 = (uint32_t)(__ballot(page >= 0) >> (lane & 60u)) & 15u;
+        const uint32_t all_there = (uint32_t)(__ballot(page >= 0) >> (lane / WAVES * WAVES)) & kThere;
         // scales of 16 tokens that no row sees may be anything
-        const int32_t j16 = j + (int32_t)((lane & 3u) * kTokens & ~15u);
+        const int32_t j16 = j + (int32_t)(lane % WAVES * kTokens & ~15u);
         const bool is_seen = page >= 0 && j16 < min(in_prefix ? base : 0x7FFFFFFF, all_last.high) && (j16 + 16 > all_first.low || j16 < all_last.sinks);
-        const bool whole = there4 == 15u && (!in_prefix || j + kTile <= base);
+        const bool whole = all_there == kThere && (!in_prefix || j + kTile <= base);
         const bool some = t < t_end && j < last_sees.high && (j + kTile > first_sees.low || j < last_sees.sinks);
         const bool edge = !whole || j + kTile > first_sees.high || (j < last_sees.low && j + kTile > first_sees.sinks);
-        return Known{(uint32_t)at, (uint32_t)(at >> 32), there4 | (in_prefix ? kPrefix : 0u) | (some ? kSome : 0u) | (edge ? kEdge : 0u),
+        return Known{(uint32_t)at, (uint32_t)(at >> 32), all_there | (in_prefix ? kPrefix : 0u) | (some ? kSome : 0u) | (edge ? kEdge : 0u),
                      is_seen ? sound_scale(a.k_scales[token >> a.block_shift]) : 0x1p-126f, is_seen ? sound_scale(a.v_scales[token >> a.block_shift]) : 0x1p-126f};
     };
     int32_t pages_ahead = pages_from(0);
     Known known = known_from(0, pages_ahead);
-    pages_ahead = pages_from(16);
-    auto flags_of = [&](int32_t i) { return (uint32_t)__builtin_amdgcn_readlane((int)known.flags, 4 * (i & 15)); };
+    pages_ahead = pages_from(kKnown);
+    auto flags_of = [&](int32_t i) { return (uint32_t)__builtin_amdgcn_readlane((int)known.flags, WAVES * (i & (kKnown - 1))); };
     // tokens from here on are not of the tile's table
     auto end_of = [&](uint32_t flags) { return flags & kPrefix ? base : 0x7FFFFFFF; };
     u32x4 k_new[kLoads], v_new[kLoads];
     const uint32_t lane_at = lane * 16;
     auto bring = [&](int32_t i) {
-        const int32_t l = 4 * (i & 15) + (int32_t)wave;
+        const int32_t l = WAVES * (i & (kKnown - 1)) + (int32_t)wave;
         const uint64_t at = (uint32_t)__builtin_amdgcn_readlane((int)known.low, l) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)known.high, l) << 32;
         const uint8_t *k_at = static_cast<const uint8_t *>(a.k_pages) + at, *v_at = static_cast<const uint8_t *>(a.v_pages) + at;
 #pragma unroll
@@ -604,7 +611,7 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
     auto swizzle = [](uint32_t token) {
         return D == 64 ? (token >> 1 & 1u) << 2 | (token >> 2 & 3u) : (token & 3u) << 2 | (token >> 2 & 3u);
     };
-    const uint32_t lds_k = dcdev::lds_address(&lds) + offsetof(TileLds<D>, k), lds_v = dcdev::lds_address(&lds) + offsetof(TileLds<D>, v);
+    const uint32_t lds_k = dcdev::lds_address(&lds) + offsetof(Lds, k), lds_v = dcdev::lds_address(&lds) + offsetof(Lds, v);
     // where a lane puts what it brings, and where it reads its part of the first operands
     uint32_t put_at[kLoads][2], k_at[KS], v_at[DT][2];
 #pragma unroll
@@ -624,7 +631,7 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
             v_at[dt][h] = token * kRowBytes + ((chunk ^ swizzle(token)) << 4) + (i16 & 1u) * 8;
         }
     auto put = [&](int32_t i, uint32_t buffer) {
-        const int32_t l = 4 * (i & 15) + (int32_t)wave;
+        const int32_t l = WAVES * (i & (kKnown - 1)) + (int32_t)wave;
         const float ks = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(known.ks), l));
         const float vs = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(known.vs), l));
         if (lane == 0) lds.scale[buffer][wave] = f32x2{ks, vs};
@@ -651,13 +658,11 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
     auto step = [&](auto B, int32_t t) {
         constexpr uint32_t buffer = decltype(B)::value;
         constexpr int kProducts = HT * KS, kGroups = 2 * HT, kAhead = 4;
-        if (t + 1 < t_end) {
-            put(t + 1 - t_begin, buffer ^ 1u);
-        }
+        if (t + 1 < t_end) put(t + 1 - t_begin, buffer ^ 1u);
         const int32_t i_after = t + 2 - t_begin;
-        if ((i_after & 15) == 0) {
+        if ((i_after & (kKnown - 1)) == 0) {
             known = known_from(i_after, pages_ahead);
-            pages_ahead = pages_from(i_after + 16);
+            pages_ahead = pages_from(i_after + kKnown);
         }
         const uint32_t flags_after = flags_of(i_after);
         if (t + 2 < t_end) bring(i_after);
@@ -680,6 +685,13 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
                 s[i / KS] = Mfma<_Float16>::m32(x[i % kAhead], q[i % KS], i % KS ? s[i / KS] : f32x16{});
                 if (i + kAhead < kProducts) x[i % kAhead] = k_operand(i + kAhead, buffer);
             }
+            __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+            for (int i = 0; i < kProducts - kAhead; i++) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
             if (flags & kEdge) {
                 const int32_t j = first_token(t);
                 Seen here = seen;
@@ -696,10 +708,10 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
             float top = -INFINITY;
 #pragma unroll
             for (int u = 0; u < 2 * HT; u++) {
-                float tops[2] = {s[u / 2][8 * (u % 2)], s[u / 2][8 * (u % 2) + 1]};
+                float most = s[u / 2][8 * (u % 2)];
 #pragma unroll
-                for (int i = 2; i < 8; i++) tops[i % 2] = fmaxf(tops[i % 2], s[u / 2][8 * (u % 2) + i]);
-                top = fmaxf(top, fmaxf(tops[0], tops[1]) * scale[u][0]);
+                for (int i = 1; i < 7; i += 2) most = fmaxf(fmaxf(most, s[u / 2][8 * (u % 2) + i]), s[u / 2][8 * (u % 2) + i + 1]); // one operation
+                top = fmaxf(top, fmaxf(most, s[u / 2][8 * (u % 2) + 7]) * scale[u][0]);
             }
             top = max_over_32(top);
             // The reference moves, to the largest score so far, only when one is so far above it that its weight would exceed 2^8: what has been
@@ -738,6 +750,7 @@ template <typename T, int D> __device__ __forceinline__ void many_rows(const Att
                 o[i % DT] = Mfma<_Float16>::m32(y[i % kAhead], w[i / DT], o[i % DT]);
                 if (i + kAhead < kGroups * DT) y[i % kAhead] = v_operand(i + kAhead, buffer);
             }
+            dcdev::in_register<false>(l); // the additions among the products, not behind them
         }
         flags = flags_next, flags_next = flags_after;
         __syncthreads();
@@ -794,11 +807,11 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
     few_rows<T, D, RT>(a, lds, common, common ? blockIdx.x : blockIdx.x - a.prefix.blocks);
 }
 
-template <typename T, int D> __global__ __launch_bounds__(256, workgroups_a_unit<D>()) void dc_attention_i8_tile_kernel(AttentionArgs a)
+template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, workgroups_a_unit<D>()) void dc_attention_i8_tile_kernel(AttentionArgs a)
 {
-    __shared__ __align__(16) TileLds<D> lds;
+    __shared__ __align__(16) TileLds<D, WAVES> lds;
     const bool common = blockIdx.x < a.prefix.blocks;
-    many_rows<T, D>(a, lds, common, common ? blockIdx.x : blockIdx.x - a.prefix.blocks);
+    many_rows<T, D, WAVES>(a, lds, common, common ? blockIdx.x : blockIdx.x - a.prefix.blocks);
 }
 
 // A common prefix with many rows and few rows in each sequence, the two kinds of workgroups in turn by eights (a workgroup's XCD is its number modulo 8,
@@ -807,13 +820,13 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
 {
     __shared__ __align__(16) union {
         FewLds<D, RT> few;
-        TileLds<D> many;
+        TileLds<D, 4> many;
     } lds;
     const uint32_t eight = blockIdx.x >> 3, prefix_eights = (a.prefix.blocks + 7) / 8, own_eights = (a.own.blocks + 7) / 8, less = min(prefix_eights, own_eights);
     const bool common = eight < 2 * less ? (eight & 1u) == 0 : prefix_eights > own_eights;
     const uint32_t block = (eight < 2 * less ? eight / 2 : eight - less) * 8 + (blockIdx.x & 7u);
     if (common) {
-        if (block < a.prefix.blocks) many_rows<T, D>(a, lds.many, true, block);
+        if (block < a.prefix.blocks) many_rows<T, D, 4>(a, lds.many, true, block);
     } else {
         if (block < a.own.blocks) few_rows<T, D, RT>(a, lds.few, false, block);
     }
@@ -830,7 +843,15 @@ template <typename T, int D> void launch(const AttentionArgs &a, const Plan &pla
         const Kind kind = a.prefix.blocks ? std::max(plan.prefix_kind, plan.own_kind) : plan.own_kind;
         const dim3 grid(a.prefix.blocks + a.own.blocks);
         if (kind == kFew16) hipLaunchKernelGGL((dc_attention_i8_few_kernel<T, D, 1>), grid, threads, 0, stream, a);
-        else if (kind == kTile) hipLaunchKernelGGL((dc_attention_i8_tile_kernel<T, D>), grid, threads, 0, stream, a);
+        else if (kind == kTile) {
+            if constexpr (wide_tile_rows(D) > kTileRows) {
+                if (plan.tile_rows > kTileRows) {
+                    hipLaunchKernelGGL((dc_attention_i8_tile_kernel<T, D, 8>), grid, dim3(512), 0, stream, a);
+                    return;
+                }
+            }
+            hipLaunchKernelGGL((dc_attention_i8_tile_kernel<T, D, 4>), grid, threads, 0, stream, a);
+        }
         else if constexpr (D < 256) hipLaunchKernelGGL((dc_attention_i8_few_kernel<T, D, 2>), grid, threads, 0, stream, a);
     }
 }
