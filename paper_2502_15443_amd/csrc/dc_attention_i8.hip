@@ -416,7 +416,6 @@ template <int D, int WAVES> struct TileLds {
     static constexpr int kTile = D == 256 ? 32 : 64; // tokens
     uint8_t k[2][kTile * 2 * D], v[2][kTile * 2 * D];
     int32_t p[32 * WAVES];
-    f32x2 scale[2][WAVES]; // of the tokens that each wavefront brings: of keys, of values
 };
 
 template <typename T, int D, int WAVES> __device__ __forceinline__ void many_rows(const AttentionArgs &a, TileLds<D, WAVES> &lds, bool common, uint32_t block)
@@ -607,9 +606,11 @@ template <typename T, int D, int WAVES> __device__ __forceinline__ void many_row
 #pragma unroll
         for (int i = 0; i < kLoads; i++) v_new[i] = *reinterpret_cast<const u32x4 *>(v_at + lane_at + i * 1024);
     };
-    // Keys and values lie in the LDS in 16 bits, of which a chunk of the cache gives two chunks.  The 16-byte chunks of a token lie exchanged in the LDS, so that 16 tokens' same chunks are on different banks, and the same four of 4 tokens'.
-    auto swizzle = [](uint32_t token) {
-        return D == 64 ? (token >> 1 & 1u) << 2 | (token >> 2 & 3u) : (token & 3u) << 2 | (token >> 2 & 3u);
+    // Keys and values lie in the LDS in 16 bits, a chunk of the cache as two of 16 bytes.  A token's chunks lie exchanged, so that 16 tokens' same chunks are on
+    // different banks, the same four of 4 tokens', and every other one that 8 lanes store.
+    auto place_of = [](uint32_t token, uint32_t chunk) {
+        const uint32_t other = D == 64 ? (token >> 1 & 1u) << 2 | ((token >> 2 & 3u) ^ (token & 1u)) : ((token & 3u) << 2 | (token >> 2 & 3u)) ^ (chunk >> 3 & 1u);
+        return token * kRowBytes + ((chunk ^ other) << 4);
     };
     const uint32_t lds_k = dcdev::lds_address(&lds) + offsetof(Lds, k), lds_v = dcdev::lds_address(&lds) + offsetof(Lds, v);
     // where a lane puts what it brings, and where it reads its part of the first operands
@@ -619,22 +620,26 @@ template <typename T, int D, int WAVES> __device__ __forceinline__ void many_row
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             const uint32_t token = wave * kTokens + i * kRowsALoad + lane / kChunks, chunk = 2 * (lane % kChunks) + h;
-            put_at[i][h] = token * kRowBytes + ((chunk ^ swizzle(token)) << 4);
+            put_at[i][h] = place_of(token, chunk);
         }
 #pragma unroll
-    for (int i = 0; i < KS; i++) k_at[i] = c * kRowBytes + (((2 * i + half) ^ swizzle(c)) << 4);
+    for (int i = 0; i < KS; i++) k_at[i] = place_of(c, 2 * i + half);
 #pragma unroll
     for (int dt = 0; dt < DT; dt++)
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             const uint32_t i16 = lane & 15u, token = 4 * half + (i16 >> 2) + 8 * h, chunk = 4 * dt + 2 * (lane >> 4 & 1u) + (i16 >> 1 & 1u);
-            v_at[dt][h] = token * kRowBytes + ((chunk ^ swizzle(token)) << 4) + (i16 & 1u) * 8;
+            v_at[dt][h] = place_of(token, chunk) + (i16 & 1u) * 8;
         }
+    uint32_t next_ks[2 * HT], next_vs[2 * HT];
     auto put = [&](int32_t i, uint32_t buffer) {
-        const int32_t l = WAVES * (i & (kKnown - 1)) + (int32_t)wave;
-        const float ks = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(known.ks), l));
-        const float vs = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(known.vs), l));
-        if (lane == 0) lds.scale[buffer][wave] = f32x2{ks, vs};
+        // scales of its 16 tokens each, of keys and of values
+#pragma unroll
+        for (int u = 0; u < 2 * HT; u++) {
+            const int32_t l = WAVES * (i & (kKnown - 1)) + u * (16 / kTokens);
+            next_ks[u] = (uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(known.ks), l);
+            next_vs[u] = (uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(known.vs), l);
+        }
 #pragma unroll
         for (int i = 0; i < kLoads; i++)
 #pragma unroll
@@ -658,6 +663,9 @@ template <typename T, int D, int WAVES> __device__ __forceinline__ void many_row
     auto step = [&](auto B, int32_t t) {
         constexpr uint32_t buffer = decltype(B)::value;
         constexpr int kProducts = HT * KS, kGroups = 2 * HT, kAhead = 4;
+        uint32_t ks[2 * HT], vs[2 * HT];
+#pragma unroll
+        for (int u = 0; u < 2 * HT; u++) ks[u] = next_ks[u], vs[u] = next_vs[u];
         if (t + 1 < t_end) put(t + 1 - t_begin, buffer ^ 1u);
         const int32_t i_after = t + 2 - t_begin;
         if ((i_after & (kKnown - 1)) == 0) {
@@ -670,12 +678,9 @@ template <typename T, int D, int WAVES> __device__ __forceinline__ void many_row
         // a wavefront whose rows see nothing of the tile has nothing to do
         if (flags & kSome) {
             f32x16 s[HT];
-            f32x2 scale[2 * HT]; // of 16 tokens each
+            float scale[2 * HT]; // of 16 tokens' scores
 #pragma unroll
-            for (int i = 0; i < 2 * HT; i++) {
-                scale[i] = lds.scale[buffer][i * (16 / kTokens)];
-                scale[i][0] = fmaxf(scale[i][0] * row_scale, 0x1p-149f);
-            }
+            for (int u = 0; u < 2 * HT; u++) scale[u] = fmaxf(__uint_as_float(ks[u]) * row_scale, 0x1p-149f);
             f16x8 x[kAhead];
             // The operands come out of the LDS several products ahead of their use.
 #pragma unroll
@@ -711,7 +716,7 @@ template <typename T, int D, int WAVES> __device__ __forceinline__ void many_row
                 float most = s[u / 2][8 * (u % 2)];
 #pragma unroll
                 for (int i = 1; i < 7; i += 2) most = fmaxf(fmaxf(most, s[u / 2][8 * (u % 2) + i]), s[u / 2][8 * (u % 2) + i + 1]); // one operation
-                top = fmaxf(top, fmaxf(most, s[u / 2][8 * (u % 2) + 7]) * scale[u][0]);
+                top = fmaxf(top, fmaxf(most, s[u / 2][8 * (u % 2) + 7]) * scale[u]);
             }
             top = max_over_32(top);
             // The reference moves, to the largest score so far, only when one is so far above it that its weight would exceed 2^8: what has been
@@ -727,9 +732,9 @@ template <typename T, int D, int WAVES> __device__ __forceinline__ void many_row
             }
             uint32_t most_vs = 0;
 #pragma unroll
-            for (int i = 0; i < 2 * HT; i++) most_vs = max(most_vs, __float_as_uint(scale[i][1]));
+            for (int u = 0; u < 2 * HT; u++) most_vs = max(most_vs, vs[u]);
             float less;
-            if (value_scale.grows(__builtin_amdgcn_readfirstlane(most_vs), less)) {
+            if (value_scale.grows(most_vs, less)) {
 #pragma unroll
                 for (int dt = 0; dt < DT; dt++) o[dt] *= less;
             }
@@ -741,9 +746,9 @@ template <typename T, int D, int WAVES> __device__ __forceinline__ void many_row
             for (int u = 0; u < kGroups; u++) {
                 f32x8 e;
 #pragma unroll
-                for (int i = 0; i < 8; i++) e[i] = exp2_of(__builtin_fmaf(s[u / 2][8 * (u % 2) + i], scale[u][0], -ref));
+                for (int i = 0; i < 8; i++) e[i] = exp2_of(__builtin_fmaf(s[u / 2][8 * (u % 2) + i], scale[u], -ref));
                 l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-                w[u] = __builtin_convertvector(e * (scale[u][1] * vs_by), f16x8);
+                w[u] = __builtin_convertvector(e * (__uint_as_float(vs[u]) * vs_by), f16x8);
             }
 #pragma unroll
             for (int i = 0; i < kGroups * DT; i++) {
