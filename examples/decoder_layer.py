@@ -3,9 +3,9 @@
 The seven matrices of a Llama-shaped layer are quantised and compressed once.  A prompt decodes them to bf16 (dc_decompress_dequant_bf16_layer)
 and multiplies its rows together; a generated token goes through the products that decode as they multiply (dc_decompress_gemv_layer).
 Between the products, both ways: rotary positions and the append to the paged cache (dc_kv_append) and the attention over it
-(dc_attention_paged), with a sliding window and sinks if wanted.
+(dc_attention_paged), with a sliding window and sinks if wanted.  The cache is of bf16, or of 8 bits with a scale for every 32 tokens of a head.
 
-  python examples/decoder_layer.py [--hidden 4096 --heads 32 --kv-heads 32 --ffn 11008 --prompt 1024 --tokens 32 --window 0 --sinks 0]
+  python examples/decoder_layer.py [--hidden 4096 --heads 32 --kv-heads 32 --ffn 11008 --prompt 1024 --tokens 32 --window 0 --sinks 0 --cache bf16|i8]
 """
 import argparse
 import os
@@ -19,7 +19,7 @@ import torch  # noqa: E402
 
 import paper_2502_15443_amd as dc  # noqa: E402
 
-PAGE = 64
+PAGE, SCALE_TOKENS = 64, 32
 
 
 def compressed(matrices, seed):
@@ -53,7 +53,7 @@ def compressed(matrices, seed):
 
 
 class DecoderLayer:
-    def __init__(self, hidden, heads, kv_heads, ffn, pages, n_positions, window=0, sinks=0, seed=0, head_dim=128):
+    def __init__(self, hidden, heads, kv_heads, ffn, pages, n_positions, window=0, sinks=0, seed=0, head_dim=128, cache="bf16"):
         self.hidden, self.heads, self.kv_heads, self.d = hidden, heads, kv_heads, head_dim
         self.window, self.sinks = window, sinks
         width, kv_width = heads * head_dim, kv_heads * head_dim
@@ -67,8 +67,13 @@ class DecoderLayer:
         angle = torch.arange(n_positions, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(head_dim // 2, dtype=torch.float64) / (head_dim // 2))
         self.cos, self.sin, self.n_positions = angle.cos().float().cuda(), angle.sin().float().cuda(), n_positions
         shape = (pages, kv_heads, PAGE, head_dim)
-        self.k_pool, self.v_pool = (torch.zeros(shape, dtype=torch.bfloat16, device="cuda") for _ in range(2))
-        self.cache = dc.KVCache(self.k_pool, self.v_pool, pages, kv_heads, head_dim, PAGE)
+        self.k_pool, self.v_pool = (torch.zeros(shape, dtype=torch.int8 if cache == "i8" else torch.bfloat16, device="cuda") for _ in range(2))
+        if cache == "i8":
+            self.k_scale, self.v_scale = (torch.zeros((pages, kv_heads, PAGE // SCALE_TOKENS), device="cuda") for _ in range(2))
+            self.cache = dc.KVCache(self.k_pool, self.v_pool, pages, kv_heads, head_dim, PAGE, dc.TYPE_I8, rows_type=dc.TYPE_BF16,
+                                    scale_tokens=SCALE_TOKENS, k_scale_dev=self.k_scale, v_scale_dev=self.v_scale)
+        else:
+            self.cache = dc.KVCache(self.k_pool, self.v_pool, pages, kv_heads, head_dim, PAGE)
 
     def gemv(self, which, x, out):
         """One token: products of consecutive matrices with the same activations, decoded as they are multiplied; fp32 results."""
@@ -139,10 +144,11 @@ def main():
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     for name, default in (("hidden", 4096), ("heads", 32), ("kv-heads", 32), ("ffn", 11008), ("prompt", 1024), ("tokens", 32), ("window", 0), ("sinks", 0)):
         ap.add_argument("--" + name, type=int, default=default)
+    ap.add_argument("--cache", choices=("bf16", "i8"), default="bf16")
     a = ap.parse_args()
     total = a.prompt + a.tokens
     table = [list(range(-(-total // PAGE)))]
-    layer = DecoderLayer(a.hidden, a.heads, a.kv_heads, a.ffn, len(table[0]), total, a.window, a.sinks)
+    layer = DecoderLayer(a.hidden, a.heads, a.kv_heads, a.ffn, len(table[0]), total, a.window, a.sinks, cache=a.cache)
     g = torch.Generator(device="cuda").manual_seed(1)
     x = torch.randn(total, a.hidden, generator=g, device="cuda")
     for turn in range(2):  # the first turn warms up
