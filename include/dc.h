@@ -607,7 +607,8 @@ typedef struct {
  * included: tokens beyond a sequence's length, behind its window, or on pages that are not there may hold anything.
  * Scores, sums and results are held in fp32; exp(s_j - reference) is rounded to the cache's type for the product with the values (f16: to at least
  * 2^-32 of the row's largest, so that many small ones are not lost beside a large one).  Over a cache of DC_TYPE_I8 queries and keys enter their product
- * as they are, and exp(s_j - reference) times the value's scale is rounded to bf16.  The sum of exp(s_j - max s) |v_j| has to stay below 2^120
+ * as they are (bf16 queries below 2^-29 of their row's largest value are rounded to 2^-40 of it), and exp(s_j - reference) times the value's scale is
+ * rounded to f16, to at least 2^-32 of the largest weight at the largest scale.  The sum of exp(s_j - max s) |v_j| has to stay below 2^120
  * (bf16 values near the type's largest).
  * A common prefix (prefix_len > 0) is read once for all sequences' rows together, or where that takes longer by each sequence's rows
  * along with its own pages.

@@ -175,7 +175,7 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
 
     // queries, and what the lane's rows see
     f16x8 q[RT][KS];
-    float row_scale[RT]; // of the scores as they come out of the products, times their keys' scales: to powers of two
+    float row_scale[RT]; // with a key's scale it makes powers of two of the scores as they come out of the products
     Seen seen[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) {
@@ -295,7 +295,7 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
             }
             const float ks = scale_in(h);
 #pragma unroll
-            for (int rt = 0; rt < RT; rt++) s[rt][h] *= ks;
+            for (int rt = 0; rt < RT; rt++) s[rt][h] *= fminf(ks * row_scale[rt], 0x1p127f); // powers of two from here on
         }
         __builtin_amdgcn_wave_barrier();
         put(v);
@@ -333,14 +333,14 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
             for (int h = 0; h < kQuarters; h++) top = fmaxf(top, fmaxf(fmaxf(s[rt][h][0], s[rt][h][1]), fmaxf(s[rt][h][2], s[rt][h][3])));
             top = fmaxf(m[rt], max_over_16(top));
             const float ref = top == -INFINITY ? 0.0f : top;
-            const float fade = exp2_of((m[rt] - ref) * row_scale[rt]);
+            const float fade = exp2_of(m[rt] - ref);
             m[rt] = top;
             float sum = 0.0f;
 #pragma unroll
             for (int u = 0; u < kQuarters / 2; u++) {
                 f32x8 e;
 #pragma unroll
-                for (int i = 0; i < 8; i++) e[i] = exp2_of((s[rt][2 * u + i / 4][i % 4] - ref) * row_scale[rt]);
+                for (int i = 0; i < 8; i++) e[i] = exp2_of(s[rt][2 * u + i / 4][i % 4] - ref);
                 sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
                 const float vs[2] = {scale_in(kQuarters + 2 * u) * value_scale.by<kLiftFew>(), scale_in(kQuarters + 2 * u + 1) * value_scale.by<kLiftFew>()};
 #pragma unroll
@@ -373,7 +373,6 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) {
         l[rt] = sum_over_16(l[rt]);
-        m[rt] *= row_scale[rt]; // what the weights are relative to
         if (l[rt] != l[rt] && m[rt] == -INFINITY) m[rt] = 0.0f; // saw scores, none of them a number
         if (g == 0) lds.m[wave][rt * 16 + c] = m[rt], lds.l[wave][rt * 16 + c] = l[rt];
     }
@@ -680,7 +679,7 @@ template <typename T, int D, int WAVES> __device__ __forceinline__ void many_row
             f32x16 s[HT];
             float scale[2 * HT]; // of 16 tokens' scores
 #pragma unroll
-            for (int u = 0; u < 2 * HT; u++) scale[u] = fmaxf(__uint_as_float(ks[u]) * row_scale, 0x1p-149f);
+            for (int u = 0; u < 2 * HT; u++) scale[u] = fminf(fmaxf(__uint_as_float(ks[u]) * row_scale, 0x1p-149f), 0x1p127f);
             f16x8 x[kAhead];
             // The operands come out of the LDS several products ahead of their use.
 #pragma unroll

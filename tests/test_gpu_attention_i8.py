@@ -231,6 +231,62 @@ def test_queries_that_are_no_numbers_reach_only_their_rows():
         check_attend_i8("bf16", 64, got, got_lse, out, lse, size, 2.0 ** -4)
 
 
+@pytest.mark.parametrize("news", [1, 20, 130])
+@pytest.mark.parametrize("power", [-126, -100, -30, 30, 100, 120])
+def test_queries_of_any_size(news, power):
+    """Queries far from 1, rows of very different sizes, and a scale that makes ordinary scores of the largest ones."""
+    p = paged_i8(38, 2, 128, 16, 16, [200, 140], [news, news])
+    q = queries(p, 4).float()
+    q = (q * 2.0 ** power).to(torch.bfloat16)
+    q[::3, 1] = (q[::3, 1].float() * 2.0 ** -20).to(torch.bfloat16)
+    q[0, 0] = 0
+    scale = 2.0 ** -power * 0.1
+    got, got_lse = attend(p, 4, q, scale, uniform=news == 1)
+    out, lse, size = oa.attend(*pool_values(p), p["batch"], f64(q), np.float64(np.float32(scale)))
+    check_attend_i8("bf16", 128, got, got_lse, out, lse, size, 2.0 ** -4)
+
+
+@pytest.mark.parametrize("news", [1, 130])
+def test_keys_of_large_and_small_scales(news):
+    """Scales of the keys far from 1, with a scale of the scores that brings them back: no product on the way leaves the range."""
+    for power in (-110, 110):
+        p = paged_i8(39, 1, 64, 16, 16, [150], [news])
+        p["ks"] = np.where(np.isfinite(p["ks"]) & (p["ks"] > 0) & (p["ks"] < 1), p["ks"] * np.float32(2.0 ** power), p["ks"]).astype(np.float32)
+        q = queries(p, 2)
+        scale = 0.125 * 2.0 ** -power
+        got, got_lse = attend(p, 2, q, scale, uniform=news == 1)
+        out, lse, size = oa.attend(*pool_values(p), p["batch"], f64(q), np.float64(np.float32(scale)))
+        check_attend_i8("bf16", 64, got, got_lse, out, lse, size, 2.0 ** -4)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("news,window,sinks", [(1, 100, 0), (20, 300, 5), (200, 64, 0), (300, 1, 20)])
+def test_the_last_positions_there_are(d, news, window, sinks):
+    """A sequence that ends at the last position, through a window; all pages but the first and the last ones have been given back."""
+    print(f"case i8 last positions d={d} news={news} window={window} sinks={sinks}", flush=True)
+    most, page, kept = 2 ** 31 - 2 ** 16, 256, 3
+    stride = most // page
+    p = paged_i8(40, 1, d, page, 64, [(kept + 1) * page], [news])
+    order = p["batch"]["pages"][0]
+    q = queries(p, 2)
+    table = torch.full((1, stride), -1, dtype=torch.int32, device="cuda")
+    table[0, 0] = int(order[0])
+    table[0, -kept:] = torch.from_numpy(order[1:].copy()).cuda()
+    cache, t = device_cache_i8(p)
+    starts, lens = torch.tensor([0, news], dtype=torch.int32, device="cuda"), torch.tensor([most], dtype=torch.int32, device="cuda")
+    batch = dc.KVBatch(1, news, news, most, lens, table, stride, row_start_dev=starts)
+    qd = q.cuda()
+    out, lse = torch.empty_like(qd), torch.empty((news, 2), dtype=torch.float32, device="cuda")
+    a = dc.Attention(2, qd, out, lse, d ** -0.5, window=window, sinks=sinks)
+    n = dc.attention_paged_workspace(cache, batch, a)
+    ws = torch.empty(n + 16, dtype=torch.uint8, device="cuda")
+    dc.attention_paged(cache, batch, a, ws, n, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    # the same rows in a sequence without the pages between
+    want = oa.attend(*pool_values(p), p["batch"], f64(q), np.float64(np.float32(d ** -0.5)), window, sinks)
+    check_attend_i8("bf16", d, f64(out), f64(lse), *want, 2.0 ** -4)
+
+
 def test_lse_may_be_left_out_and_results_repeat():
     for news, prefix in ((1, 0), (1, 64), (150, 0)):
         p = paged_i8(28, 2, 128, 16, 16, [900, 300], [news, news], prefix)
