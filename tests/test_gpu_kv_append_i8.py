@@ -123,6 +123,14 @@ def test_many_rows():
     run(10, "bf16", "bf16", 2, 1, 64, 32, 32, [20 + i for i in range(70)] + [200] + [5] * 10, [1] * 70 + [170] + [1] * 10, 64)
 
 
+def test_rows_of_every_kind_of_launch():
+    # many single tokens, of few and of many heads
+    run(30, "bf16", "bf16", 2, 1, 64, 16, 16, [1 + i % 37 for i in range(700)], [1] * 700, 64, uniform=True)
+    run(31, "f16", "f32", 33, 3, 64, 16, 16, [2 + i % 37 for i in range(600)], [2] * 600, 32)
+    # many rows of many query heads: queries apart from the rest, single tokens between
+    run(32, "bf16", "bf16", 64, 1, 64, 32, 32, [2100, 40, 1999], [2100, 1, 1999], 64)
+
+
 def test_prefix_and_absent_pages():
     run(11, "bf16", "f32", 4, 2, 64, 16, 16, [130, 100, 75], [20, 25, 1], 32, prefix=70, absent=[(0, 1), (1, 1)])
     # rows that begin inside the prefix: its last block ends with it, and the own pages begin with a block
