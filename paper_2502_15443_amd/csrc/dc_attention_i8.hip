@@ -818,29 +818,25 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES,
     many_rows<T, D, WAVES>(a, lds, common, common ? blockIdx.x : blockIdx.x - a.prefix.blocks);
 }
 
-// A common prefix with many rows and few rows in each sequence, the two kinds of workgroups in turn by eights (a workgroup's XCD is its number modulo 8,
-// and those of one key/value head's prefix stay on one).
+// A common prefix with many rows and few rows in each sequence: the first is bound by the matrix units, the second by memory, and a compute unit has some of each.
+// The prefix's workgroups come first.  (In turn by eights they fell on every other group of compute units, two to a unit: 64 sequences behind 16384
+// tokens 62.5 us, so 48.8, 5 of them the join; 256 of them 167 and 118, 40 sequences and heads behind 4096 82 and 79, 64 of 4000 behind 16384 104 and 109.)
+// A workgroup's XCD is its number modulo 8, and those of one key/value head's prefix stay on one.
 template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void dc_attention_i8_both_kernel(AttentionArgs a)
 {
     __shared__ __align__(16) union {
         FewLds<D, RT> few;
         TileLds<D, 4> many;
     } lds;
-    const uint32_t eight = blockIdx.x >> 3, prefix_eights = (a.prefix.blocks + 7) / 8, own_eights = (a.own.blocks + 7) / 8, less = min(prefix_eights, own_eights);
-    const bool common = eight < 2 * less ? (eight & 1u) == 0 : prefix_eights > own_eights;
-    const uint32_t block = (eight < 2 * less ? eight / 2 : eight - less) * 8 + (blockIdx.x & 7u);
-    if (common) {
-        if (block < a.prefix.blocks) many_rows<T, D, 4>(a, lds.many, true, block);
-    } else {
-        if (block < a.own.blocks) few_rows<T, D, RT>(a, lds.few, false, block);
-    }
+    if (blockIdx.x < a.prefix.blocks) many_rows<T, D, 4>(a, lds.many, true, blockIdx.x);
+    else few_rows<T, D, RT>(a, lds.few, false, blockIdx.x - a.prefix.blocks);
 }
 
 template <typename T, int D> void launch(const AttentionArgs &a, const Plan &plan, hipStream_t stream)
 {
     const dim3 threads(256);
     if (a.prefix.blocks && plan.prefix_kind == kTile && plan.own_kind != kTile) {
-        const dim3 grid(8 * ((a.prefix.blocks + 7) / 8 + (a.own.blocks + 7) / 8));
+        const dim3 grid(a.prefix.blocks + a.own.blocks);
         if (plan.own_kind == kFew16) hipLaunchKernelGGL((dc_attention_i8_both_kernel<T, D, 1>), grid, threads, 0, stream, a);
         else if constexpr (D < 256) hipLaunchKernelGGL((dc_attention_i8_both_kernel<T, D, 2>), grid, threads, 0, stream, a);
     } else { // a sequence's rows are never more than the batch's: both parts are of the kind of their rows together, or the prefix is alone
