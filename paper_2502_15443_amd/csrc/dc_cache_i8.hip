@@ -275,12 +275,12 @@ template <typename X, int D, bool NEIGHBOURS, bool QUERIES, bool KEYS> __device_
     }
 }
 
-// The blocks led by a row among `block` neighbouring ones that have more than a few new rows, of some heads of the keys or of the values, one after the
+// The blocks led by a row among `block` neighbouring ones that have more than `few` new rows, of some heads of the keys or of the values, one after the
 // other.  A team of threads has a head's block, each of them 16 values of ROWS rows, whose cosines and sines it keeps for all heads.
 // Small blocks (up to 2048 values) are a wavefront's: no barrier; else the team is the workgroup, of 256 to 1024 threads, and the next head's values
 // are on their way while this head's maximum is found.  BIG: a block has more than 16 values for each of 1024 threads; those of its further rows are
 // read twice.
-template <typename X, int D, bool NEIGHBOURS, int ROWS, bool BIG> __device__ __forceinline__ void append_blocks(const AppendArgs &a, uint32_t group, bool is_k, uint32_t head_first,
+template <typename X, int D, bool NEIGHBOURS, int ROWS, bool BIG> __device__ __forceinline__ void append_blocks(const AppendArgs &a, uint32_t few, uint32_t group, bool is_k, uint32_t head_first,
                                                                                                                 uint32_t heads, uint32_t (&lds_most)[2][kMostThreads / 64])
 {
     constexpr bool kWave = ROWS > 0; // ROWS 0: the workgroup, a row to a thread
@@ -310,7 +310,7 @@ template <typename X, int D, bool NEIGHBOURS, int ROWS, bool BIG> __device__ __f
         const bool has = lane < block && my_row < a.batch.n_rows && first_row <= my_row && my_row < rows_end && my_row - first_row < a.max_new;
         // (a row that no sequence has is as if at a position below zero)
         const Place p(a, has ? my_row : 0, low, has ? first_row : 0, has ? rows_end : 1, has ? length : 0);
-        uint64_t leaders = __ballot(p.count > kFewRows);
+        uint64_t leaders = __ballot(p.count > few);
         while (leaders) {
             const int l = __builtin_ctzll(leaders);
             leaders &= leaders - 1;
@@ -418,7 +418,7 @@ template <typename X, int D, bool NEIGHBOURS, int ROWS, bool BIG> __device__ __f
 // one XCD (a workgroup's is its number modulo 8), for they read the same cosines.
 struct BlockWork {
     uint64_t items;
-    uint32_t head_groups, heads;
+    uint32_t head_groups, heads, few;
 };
 template <typename X, int D, bool NEIGHBOURS, int ROWS, bool BIG> __device__ __forceinline__ void block_item(const AppendArgs &a, const BlockWork &w, uint64_t item,
                                                                                                              uint32_t (&most)[2][kMostThreads / 64])
@@ -427,7 +427,7 @@ template <typename X, int D, bool NEIGHBOURS, int ROWS, bool BIG> __device__ __f
     const uint32_t wave = ROWS ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
     const uint32_t eight = (uint32_t)(item >> 3) * kTeams + wave; // of eight groups of rows
     const uint32_t part = eight % (2 * w.head_groups), head = part / 2 * w.heads;
-    append_blocks<X, D, NEIGHBOURS, ROWS, BIG>(a, eight / (2 * w.head_groups) * 8 + (uint32_t)(item & 7u), part % 2 == 0, head, min(w.heads, a.n_kv_heads - head), most);
+    append_blocks<X, D, NEIGHBOURS, ROWS, BIG>(a, w.few, eight / (2 * w.head_groups) * 8 + (uint32_t)(item & 7u), part % 2 == 0, head, min(w.heads, a.n_kv_heads - head), most);
 }
 
 // Rows: each in `parts` parts of part_slots heads (queries, then keys, then values, from number first_slot on), which row_threads threads go through.
@@ -490,14 +490,20 @@ template <typename X, int D, bool NEIGHBOURS, int ROWS, bool BIG> void launch_n(
             return;
         }
     }
-    hipLaunchKernelGGL((dc_kv_append_i8_blocks_kernel<X, D, NEIGHBOURS, ROWS, BIG>), dim3((uint32_t)std::min(b.items, kMostItems)), dim3(threads), 0, stream, a, b);
+    const uint32_t row_threads = rows >= 512 && slots * (D / 16) <= 128 ? 64 : kThreads;
+    // A sequence has at most two blocks with few rows, its first and its last one: beside many blocks they are the same kernel's.
+    BlockWork all = b;
+    if ((uint64_t)a.batch.n_seqs * 16 <= rows >> a.block_shift) all.few = 0;
+    hipLaunchKernelGGL((dc_kv_append_i8_blocks_kernel<X, D, NEIGHBOURS, ROWS, BIG>), dim3((uint32_t)std::min(b.items, kMostItems)), dim3(threads), 0, stream, a, all);
+    if (all.few == 0) {
+        launch_rows<X, D, NEIGHBOURS, true, false>(a, row_work<D>(rows, 0, a.n_heads, row_threads, kThreads), stream);
     // Queries apart from the blocks with few rows, which take twice the registers, if they are worth a launch (8192 rows of 40/40 heads of 128: 101
     // instead of 107 us; 2048 rows of 32/8 17.6 instead of 16.1, 32768 rows of 16/2 of 64 58 instead of 47).
-    if (rows >= 4096 && a.n_heads * D >= 4096) {
+    } else if (rows >= 4096 && a.n_heads * D >= 4096) {
         launch_rows<X, D, NEIGHBOURS, false, true>(a, row_work<D>(rows, a.n_heads, slots, 64, kThreads), stream);
         launch_rows<X, D, NEIGHBOURS, true, false>(a, row_work<D>(rows, 0, a.n_heads, kThreads, kThreads), stream);
     } else {
-        launch_rows<X, D, NEIGHBOURS, true, true>(a, row_work<D>(rows, 0, slots, rows >= 512 && slots * (D / 16) <= 128 ? 64 : kThreads, kThreads), stream);
+        launch_rows<X, D, NEIGHBOURS, true, true>(a, row_work<D>(rows, 0, slots, row_threads, kThreads), stream);
     }
 }
 
@@ -512,6 +518,7 @@ template <typename X, int D, bool NEIGHBOURS> void launch_d(const AppendArgs &a,
     const uint32_t threads = small ? kThreads : std::min(D / 16 * block, kMostThreads), teams = small ? kThreads / 64 : 1;
     const uint64_t groups = (rows + block - 1) / block;
     BlockWork b = {};
+    b.few = kFewRows;
     b.heads = 1;
     while (b.heads < a.n_kv_heads && b.heads < 8 && groups * 2 * ((a.n_kv_heads + b.heads - 1) / b.heads) * (small ? 64 : threads) > 2048 * kThreads) b.heads++;
     b.head_groups = (a.n_kv_heads + b.heads - 1) / b.heads;
