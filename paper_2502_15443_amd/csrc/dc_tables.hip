@@ -2,7 +2,9 @@
 //
 // Pages are taken and given back in the order of sequences and entries, so an entry's place in the queue is the number of entries before it that
 // take (give back) a page: counts, their prefix sums, and the entries once more.  A wavefront works on a run of neighbouring entries of one
-// sequence; few runs are one workgroup's, many a launch's for each of the three parts.
+// sequence; few runs are one workgroup's (one sequence of 64 entries 4.3 us), more take a launch for the counts and one for the results (256 sequences of
+// 512 entries 8.7 us, 1024 of 1024 with 215616 rows 12.1 us), and from 16384 runs on one for the sums between them.  Latency bounds all of it: launches, and
+// in each a few loads that wait for one another; what the largest of those reads and writes would take 1.8 us.
 #include "dc_device.h"
 #include "dc_pages.h"
 
