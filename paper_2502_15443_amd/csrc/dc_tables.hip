@@ -356,8 +356,15 @@ template <bool SUMMED> __global__ __launch_bounds__(256) void dc_kv_tables_fill_
         load_run(a, item, lane, seq, first, page);
         s = a.ws_seqs[seq];
     }
+    // the runs of the workgroup's own group: each in the lanes with its number modulo 4
+    const uint32_t item0 = blockIdx.x * 4, groups = (a.n_items + 3) / 4, near = item0 + (lane & 3u);
+    Moves near_moves = {0, 0};
+    uint32_t near_rows = 0;
+    if (near < a.n_items) {
+        near_moves = a.ws_moves[near];
+        if (near % a.runs == a.runs - 1) near_rows = a.ws_seqs[near / a.runs].rows;
+    }
     // moves and rows of all groups of runs, and of those before the workgroup's
-    const uint32_t item0 = blockIdx.x * 4, groups = (a.n_items + 3) / 4;
     uint32_t mine[6] = {};
     for (uint32_t i = threadIdx.x; i < groups; i += 256) {
         const Group g = a.ws_groups[i];
@@ -379,10 +386,11 @@ template <bool SUMMED> __global__ __launch_bounds__(256) void dc_kv_tables_fill_
     if (item < a.n_items) {
         Moves at = {total[0], total[1]};
         u64 rows = total[2];
-        for (uint32_t i = item0; i < item; i++) { // its own group's runs before it
-            const Moves v = a.ws_moves[i];
-            at.taken += v.taken, at.back += v.back;
-            if (i % a.runs == a.runs - 1) rows += a.ws_seqs[i / a.runs].rows;
+#pragma unroll
+        for (uint32_t w = 0; w < 3; w++) { // its own group's runs before it
+            if (w >= wave) break;
+            at.taken += (uint32_t)__builtin_amdgcn_readlane((int)near_moves.taken, (int)w), at.back += (uint32_t)__builtin_amdgcn_readlane((int)near_moves.back, (int)w);
+            rows += (uint32_t)__builtin_amdgcn_readlane((int)near_rows, (int)w);
         }
         s = sequence_from(a, seq, s.held, s.end, rows, s.rows);
         if (lane == 0 && first == 0) store_sequence(a, seq, s);
