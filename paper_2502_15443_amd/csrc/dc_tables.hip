@@ -3,7 +3,7 @@
 // Pages are taken and given back in the order of sequences and entries, so an entry's place in the queue is the number of entries before it that
 // take (give back) a page: counts, their prefix sums, and the entries once more.  A wavefront works on a run of neighbouring entries of one
 // sequence; few runs are one workgroup's (one sequence of 64 entries 4.3 us), more take a launch for the counts and one for the results (256 sequences of
-// 512 entries 8.7 us, 1024 of 1024 with 215616 rows 12.1 us), and from 16384 runs on one for the sums between them.  Latency bounds all of it: launches, and
+// 512 entries 8.4 us, 1024 of 1024 with 215616 rows 12.1 us), and from 16384 runs on one for the sums between them.  Latency bounds all of it: launches, and
 // in each a few loads that wait for one another; what the largest of those reads and writes would take 1.8 us.
 #include "dc_device.h"
 #include "dc_pages.h"
@@ -155,21 +155,19 @@ struct RunRows {
     uint32_t seq, first, begin, end, less;
 };
 
-// A run's entries as they become, and which rows lie on them.  at: moves of the runs before; lds: address of kRun entries of the wavefront's own.
-__device__ __forceinline__ void fill_run(const TablesArgs &a, uint32_t seq, uint32_t first, uint32_t lane, const int32_t (&page)[kLoads], const Sequence &s, const Queue &q,
-                                         Moves at, uint32_t lds, RunRows &rows)
+// A run's entries as they become.  at: moves of the runs before.
+__device__ __forceinline__ void entries_of(const TablesArgs &a, uint32_t first, uint32_t lane, const int32_t (&page)[kLoads], int32_t held, int32_t end_token, const Queue &q,
+                                           Moves at, int32_t (&becomes)[kLoads])
 {
     const uint64_t below = (1ull << lane) - 1;
-    int32_t *row = a.pages + (uint64_t)seq * a.stride;
     // places in the ring: sums of two numbers up to n_pages stay inside 32 bits
     auto in_ring = [&](uint32_t x) { return x >= a.n_pages ? x - a.n_pages : x; };
     const uint32_t end = in_ring(q.first + q.count);
-    int32_t becomes[kLoads];
 #pragma unroll
     for (uint32_t k = 0; k < kLoads; k++) {
         becomes[k] = -1;
         if (first + 64 * k >= a.stride) break;
-        const Entry e(a, first + 64 * k + lane, page[k], s.held, s.end);
+        const Entry e(a, first + 64 * k + lane, page[k], held, end_token);
         const uint64_t taking = __ballot(e.takes), giving = __ballot(e.goes);
         const uint32_t rank = at.taken + (uint32_t)__popcll(taking & below), rank_back = at.back + (uint32_t)__popcll(giving & below);
         if (e.there & e.wanted) becomes[k] = page[k];
@@ -177,6 +175,11 @@ __device__ __forceinline__ void fill_run(const TablesArgs &a, uint32_t seq, uint
         if (e.goes & (rank_back < a.n_pages)) a.free[in_ring(end + rank_back)] = page[k];
         at.taken += (uint32_t)__popcll(taking), at.back += (uint32_t)__popcll(giving);
     }
+}
+// Stores them, also to the kRun entries of the run in the LDS, at address lds; and which rows lie on them.
+__device__ __forceinline__ void store_run(const TablesArgs &a, uint32_t seq, uint32_t first, uint32_t lane, const int32_t (&becomes)[kLoads], const Sequence &s, uint32_t lds, RunRows &rows)
+{
+    int32_t *row = a.pages + (uint64_t)seq * a.stride;
 #pragma unroll
     for (uint32_t k = 0; k < kLoads; k++) {
         if (first + 64 * k >= a.stride) break;
@@ -191,16 +194,23 @@ __device__ __forceinline__ void fill_run(const TablesArgs &a, uint32_t seq, uint
         rows = RunRows{seq, first, begin, begin < end ? end : begin, s.first_row - (uint32_t)s.held};
     }
 }
+__device__ __forceinline__ void fill_run(const TablesArgs &a, uint32_t seq, uint32_t first, uint32_t lane, const int32_t (&page)[kLoads], const Sequence &s, const Queue &q,
+                                         Moves at, uint32_t lds, RunRows &rows)
+{
+    int32_t becomes[kLoads];
+    entries_of(a, first, lane, page, s.held, s.end, q, at, becomes);
+    store_run(a, seq, first, lane, becomes, s, lds, rows);
+}
 
-// The places of the rows that lie on a run's entries, by all threads of the workgroup.
-template <uint32_t THREADS> __device__ __forceinline__ void fill_rows(const TablesArgs &a, const RunRows &rows, uint32_t lds)
+// The places of the rows that lie on a run's entries: those of number `from`, `from` + STEP ..
+template <uint32_t STEP> __device__ __forceinline__ void fill_rows(const TablesArgs &a, const RunRows &rows, uint32_t lds, uint32_t from, uint32_t most = 0xFFFFFFFFu)
 {
     const RunRows n = rows;
-    for (uint32_t p = n.begin + threadIdx.x; p < n.end; p += THREADS) {
-        const uint32_t r = n.less + p, place = p < a.prefix_len ? p : p - a.prefix_len, i = place >> a.page_shift;
+    for (uint32_t i = from; i < min(n.end - n.begin, most); i += STEP) {
+        const uint32_t p = n.begin + i, r = n.less + p, place = p < a.prefix_len ? p : p - a.prefix_len, e = place >> a.page_shift;
         int32_t of = -1;
-        if (p < a.prefix_len) of = a.prefix_pages[i];
-        else if (i < a.stride) of = (int32_t)dcdev::lds_load32(lds + 4 * (i - n.first));
+        if (p < a.prefix_len) of = a.prefix_pages[e];
+        else if (e < a.stride) of = (int32_t)dcdev::lds_load32(lds + 4 * (e - n.first));
         if (a.slot) a.slot[r] = (uint32_t)of < a.n_pages ? (int64_t)((uint64_t)(uint32_t)of << a.page_shift | (place & ((1u << a.page_shift) - 1u))) : -1;
         if (a.position) a.position[r] = (int32_t)min(p, (uint32_t)kMostLength);
         if (a.seq) a.seq[r] = (int32_t)n.seq;
@@ -217,50 +227,79 @@ __device__ __forceinline__ void fill_rest(const TablesArgs &a, uint32_t from, ui
     }
 }
 
-// Up to 16 runs: one workgroup with a run to a wavefront; what one part finds stays in registers and in the LDS.
-constexpr uint32_t kFewItems = kScanThreads / 64;
-__global__ __launch_bounds__(kScanThreads) void dc_kv_tables_kernel(TablesArgs a)
+// Up to 32 runs: one workgroup with RUNS of them to a wavefront, number wave + 16 k; what one part finds stays in registers and in the LDS.
+// (32 sequences of 64 entries 6.2 us, of 256 9.0; in two launches 8.3 and 9.1.  64 runs of 128 entries are 11.5 in one workgroup, whose operations bound it then, and 8.6.)
+constexpr uint32_t kWaves = kScanThreads / 64, kFewItems = 32;
+template <uint32_t RUNS> __global__ __launch_bounds__(kScanThreads) void dc_kv_tables_kernel(TablesArgs a)
 {
-    __shared__ int32_t entries[kFewItems][kRun];
-    __shared__ Moves moves[kFewItems];
-    __shared__ RunRows run_rows[kFewItems];
+    constexpr uint32_t kItems = RUNS * kWaves;
+    __shared__ int32_t entries[kItems][kRun];
+    __shared__ Moves moves[kItems];
+    __shared__ RunRows run_rows[kItems];
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63u;
-    // every wavefront knows all sequences (at most 16): a lane to a sequence
+    // every wavefront knows all sequences (at most 32): a lane to a sequence
     const uint32_t arriving = lane < a.n_seqs ? arriving_at(a, lane) : 0;
     const Queue q = queue_of(a);
-    uint32_t seq = 0, first = 0;
-    int32_t page[kLoads], held = 0, end = 0;
-    Moves mine = {0, 0};
-    if (wave < a.n_items) {
-        load_run(a, wave, lane, seq, first, page);
-        tokens_of(a, seq, held, end);
-        mine = moves_of(a, first, lane, page, held, end);
+    uint32_t seq[RUNS], first[RUNS];
+    int32_t page[RUNS][kLoads], held[RUNS], end[RUNS];
+    int32_t lane_held = 0, lane_end = 0;
+    if (lane < a.n_seqs) tokens_of(a, lane, lane_held, lane_end);
+    // (loads without branches between them: all are under way at once; where there is no such run, the last one's)
+#pragma unroll
+    for (uint32_t k = 0; k < RUNS; k++) load_run(a, min(wave + kWaves * k, a.n_items - 1), lane, seq[k], first[k], page[k]);
+#pragma unroll
+    for (uint32_t k = 0; k < RUNS; k++) {
+        held[k] = __builtin_amdgcn_readlane(lane_held, (int)seq[k]), end[k] = __builtin_amdgcn_readlane(lane_end, (int)seq[k]);
+        Moves mine = {0, 0};
+        if (wave + kWaves * k < a.n_items) mine = moves_of(a, first[k], lane, page[k], held[k], end[k]);
+        if (lane == 0) moves[wave + kWaves * k] = mine;
     }
     u64 rows_upto = arriving;
 #pragma unroll
-    for (int k = 1; k < (int)kFewItems; k <<= 1) {
+    for (int k = 1; k < (int)kItems; k <<= 1) {
         const u64 t = __shfl_up(rows_upto, k);
         if (lane >= (uint32_t)k) rows_upto += t;
     }
-    const u64 rows = __shfl(rows_upto, kFewItems - 1), before = __shfl(rows_upto - arriving, (int)seq);
-    if (lane == 0) moves[wave] = mine;
+    const u64 rows = __shfl(rows_upto, kItems - 1);
     __syncthreads(); // (behind it nobody reads what the results may lie on: lengths, queue, entries)
-    Moves at = {0, 0}, all = {0, 0};
+    // moves of the runs before the lane's, and of all
+    Moves mine = {0, 0};
+    if (lane < kItems) mine = moves[lane];
+    const uint32_t taken = dcdev::lanes_prefix_sum<false>(mine.taken), back = dcdev::lanes_prefix_sum<false>(mine.back);
+    if (threadIdx.x == 63) store_queue(a, q, Moves{taken, back});
+    const uint32_t lds = dcdev::lds_address(entries);
+    int32_t becomes[RUNS][kLoads];
 #pragma unroll
-    for (uint32_t w = 0; w < kFewItems; w++) {
-        const Moves m = moves[w];
-        if (w < wave) at.taken += m.taken, at.back += m.back;
-        all.taken += m.taken, all.back += m.back;
+    for (uint32_t k = 0; k < RUNS; k++) {
+        const uint32_t item = wave + kWaves * k;
+        if (item >= a.n_items) break;
+        const Moves at = {(uint32_t)__builtin_amdgcn_readlane((int)(taken - mine.taken), (int)item), (uint32_t)__builtin_amdgcn_readlane((int)(back - mine.back), (int)item)};
+        entries_of(a, first[k], lane, page[k], held[k], end[k], q, at, becomes[k]);
     }
-    if (threadIdx.x == 0) store_queue(a, q, all);
-    if (wave < a.n_items) {
-        const Sequence s = sequence_from(a, seq, held, end, before, (uint32_t)__shfl((int)arriving, (int)seq));
-        if (lane == 0 && first == 0) store_sequence(a, seq, s);
-        fill_run(a, seq, first, lane, page, s, q, at, dcdev::lds_address(entries) + wave * (kRun * 4), run_rows[wave]);
+#pragma unroll
+    for (uint32_t k = 0; k < RUNS; k++) {
+        const uint32_t item = wave + kWaves * k;
+        if (item >= a.n_items) break;
+        const Sequence s = sequence_from(a, seq[k], held[k], end[k], __shfl(rows_upto - arriving, (int)seq[k]), (uint32_t)__shfl((int)arriving, (int)seq[k]));
+        if (lane == 0 && first[k] == 0) store_sequence(a, seq[k], s);
+        store_run(a, seq[k], first[k], lane, becomes[k], s, lds + item * (kRun * 4), run_rows[item]);
     }
     fill_rest(a, (uint32_t)min(rows, (u64)a.n_rows), threadIdx.x, kScanThreads);
     __syncthreads();
-    for (uint32_t i = 0; i < a.n_items; i++) fill_rows<kScanThreads>(a, run_rows[i], dcdev::lds_address(entries) + i * (kRun * 4));
+    // a run's rows: the first ones by its wavefront, further ones by all
+#pragma unroll
+    for (uint32_t k = 0; k < RUNS; k++) {
+        const uint32_t item = wave + kWaves * k;
+        if (item < a.n_items) fill_rows<64>(a, run_rows[item], lds + item * (kRun * 4), lane, 64);
+    }
+    bool more = false;
+    if (lane < a.n_items) more = run_rows[lane].end - run_rows[lane].begin > 64;
+    uint64_t longer = __ballot(more);
+    while (longer) {
+        const uint32_t i = (uint32_t)__builtin_ctzll(longer);
+        longer &= longer - 1;
+        fill_rows<kScanThreads>(a, run_rows[i], lds + i * (kRun * 4), 64 + threadIdx.x);
+    }
 }
 
 // More: counts of all runs and what the results may lie on, ..
@@ -341,7 +380,7 @@ template <bool SUMMED> __global__ __launch_bounds__(256) void dc_kv_tables_fill_
                 fill_run(a, seq, first, lane, page, s, q, a.ws_moves[item], address, run_rows[wave]);
             }
             __syncthreads();
-            for (uint32_t i = 0; i < min(4u, a.n_items - item0); i++) fill_rows<256>(a, run_rows[i], dcdev::lds_address(lds) + i * (kRun * 4));
+            for (uint32_t i = 0; i < min(4u, a.n_items - item0); i++) fill_rows<256>(a, run_rows[i], dcdev::lds_address(lds) + i * (kRun * 4), threadIdx.x);
             __syncthreads();
         }
         const Sequence s = a.ws_seqs[a.n_seqs - 1];
@@ -398,7 +437,7 @@ template <bool SUMMED> __global__ __launch_bounds__(256) void dc_kv_tables_fill_
     }
     fill_rest(a, min(total[5], a.n_rows), blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
     __syncthreads();
-    for (uint32_t i = 0; i < min(4u, a.n_items - item0); i++) fill_rows<256>(a, run_rows[i], dcdev::lds_address(lds) + i * (kRun * 4));
+    for (uint32_t i = 0; i < min(4u, a.n_items - item0); i++) fill_rows<256>(a, run_rows[i], dcdev::lds_address(lds) + i * (kRun * 4), threadIdx.x);
 }
 
 bool requests_ok(const dc_kv_requests *r)
@@ -447,8 +486,10 @@ extern "C" int dc_kv_tables(const dc_kv_requests *requests, void *workspace_dev,
     a.ws_groups = reinterpret_cast<Group *>(a.ws_seqs + r.n_seqs);
     a.ws_moves = reinterpret_cast<Moves *>(a.ws_groups + (a.n_items + 3) / 4);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (a.n_items <= kFewItems) {
-        hipLaunchKernelGGL(dc_kv_tables_kernel, dim3(1), dim3(kScanThreads), 0, stream, a);
+    if (a.n_items <= kWaves) {
+        hipLaunchKernelGGL(dc_kv_tables_kernel<1>, dim3(1), dim3(kScanThreads), 0, stream, a);
+    } else if (a.n_items <= kFewItems) {
+        hipLaunchKernelGGL(dc_kv_tables_kernel<kFewItems / kWaves>, dim3(1), dim3(kScanThreads), 0, stream, a);
     } else {
         const dim3 grid(std::min<uint32_t>((a.n_items + 3) / 4, 1u << 20));
         hipLaunchKernelGGL(dc_kv_tables_count_kernel, grid, dim3(256), 0, stream, a);

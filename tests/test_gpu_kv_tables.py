@@ -126,6 +126,15 @@ def test_rows_of_the_table(entries, window, sinks):
         run(3, seqs, 16, entries, held, new, window=window, sinks=sinks, in_place=seqs == 3)
 
 
+@pytest.mark.parametrize("seqs,entries", [(31, 7), (32, 256), (63, 7), (64, 256), (65, 9), (31, 300), (32, 512), (33, 257), (22, 700), (16, 1024), (13, 1200)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_runs_of_one_workgroup_and_beyond(seqs, entries, in_place):
+    for most_new in (1, 63, 200):
+        held, new = batch(seqs + most_new, seqs, entries * 16, most_new)
+        run(14, seqs, 16, entries, held, new, window=500 * (most_new % 2), sinks=20, in_place=in_place, absent=0.1)
+        run(15, seqs, 16, entries, held // 2, new * 8, prefix=33 if most_new > 1 else 0, in_place=in_place)
+
+
 @pytest.mark.parametrize("prefix", [1, 15, 16, 100])
 def test_a_common_prefix(prefix):
     held, new = batch(prefix, 30, 100, 50)
