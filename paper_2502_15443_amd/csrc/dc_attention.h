@@ -43,7 +43,8 @@ struct AttentionArgs {
     float scale;       // above 0; with `negate` of queries that are taken with the other sign
     bool negate;
     bool whole;        // the prefix is read with the sequences' own pages, not as a part of its own
-    Part prefix, own;
+    Part prefix, own, few;  // few: of sequences with at most least_many rows among others with many
+    uint32_t least_many;
     // of a cache of 8 bits: scale of [page][head][token >> block_shift]
     const float *k_scales, *v_scales;
     uint32_t block_shift;

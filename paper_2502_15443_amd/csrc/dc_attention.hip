@@ -979,6 +979,15 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     }
     if (own_kind == kTile) {
         if (!a.whole) a.own = many_part(false);
+        // Over a cache of 8 bits sequences of at most 16 rows, which may be among them, are taken as few rows, in as many parts.
+        if (cache->type == DC_TYPE_I8 && !a.whole && batch->row_start_dev && batch->n_seqs > 1 && group <= 16) {
+            const uint64_t n_tiles = std::max<uint64_t>(1, (seen(own_len, 16) + few_tile(1) - 1) / few_tile(1)), n = a.own.n_splits;
+            const uint64_t blocks = (uint64_t)cache->n_kv_heads * batch->n_seqs * n;
+            if (a.own.blocks + (uint64_t)a.prefix.blocks + blocks < 1u << 24) {
+                a.few = Part{(uint32_t)blocks, (uint32_t)n, (uint32_t)((n_tiles + n - 1) / n), a.own.first_slot};
+                a.least_many = 16;
+            }
+        }
     } else {
         const uint64_t tokens = seen(own_len, batch->max_new), items = (uint64_t)cache->n_kv_heads * batch->n_seqs;
         a.own = part(items, tokens, tile_few, cut_few(items, tokens), a.prefix.n_splits);

@@ -121,13 +121,13 @@ template <int D, int RT> struct FewLds {
     int32_t p[16 * RT];
 };
 
-template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(const AttentionArgs &a, FewLds<D, RT> &lds, bool common, uint32_t item)
+template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(const AttentionArgs &a, const Part &part, FewLds<D, RT> &lds, bool common, uint32_t item)
 {
     constexpr int kTile = few_tile(RT), kQuarters = kTile / 16, KS = D / 32, DT = D / 16;
     constexpr int kChunks = D / 16, kTokensALoad = 64 / kChunks, kLoads = kTile / kTokensALoad; // chunks: of 16 bytes
 
-    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15u, g = lane >> 4;
-    const Part &part = common ? a.prefix : a.own;
+    // (a workgroup may have two of these, of 256 threads each)
+    const uint32_t thread = threadIdx.x & 255u, lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(thread >> 6), c = lane & 15u, g = lane >> 4;
     const uint32_t kv = item % a.n_kv_heads;
     item /= a.n_kv_heads;
     const uint32_t seq = common ? 0 : item % a.batch.n_seqs, split = common ? item : item / a.batch.n_seqs;
@@ -150,9 +150,9 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
         n = a.batch.n_rows * a.group;
         there = (int32_t)a.batch.prefix_len;
         // positions of the rows, sequence by sequence
-        if (threadIdx.x < 16 * RT) lds.p[threadIdx.x] = kNoPosition;
+        if (thread < 16 * RT) lds.p[thread] = kNoPosition;
         __syncthreads();
-        for (uint32_t b = threadIdx.x; b < a.batch.n_seqs; b += 256) {
+        for (uint32_t b = thread; b < a.batch.n_seqs; b += 256) {
             const uint32_t first = a.batch.first_row(b), end = a.batch.rows_end(b);
             for (uint32_t r = first; r < end; r++) lds.p[r] = a.batch.length(b) - (int32_t)(end - r);
         }
@@ -166,6 +166,7 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
         if (end <= row_first) return;
         const uint32_t rows = min(end - row_first, a.max_new);
         n = rows * a.group;
+        if (n > 16 * RT) return; // it is among those with many rows
         base = (int32_t)a.batch.prefix_len;
         there = min(max(len - base, 0), (int32_t)(a.batch.pages_stride << a.batch.page_shift));
         p_first = len - (int32_t)(end - row_first);
@@ -391,7 +392,7 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
             *reinterpret_cast<f32x4 *>(&lds.sums[wave][c][16 * dt + 4 * g]) = m[rt] == -INFINITY ? f32x4{} : o[rt][dt] * f;
         __syncthreads();
         constexpr uint32_t kQuads = D / 4;
-        for (uint32_t i = threadIdx.x; i < 16 * kQuads; i += 256) {
+        for (uint32_t i = thread; i < 16 * kQuads; i += 256) {
             const uint32_t col = i / kQuads, at = i % kQuads * 4, rr = rt * 16 + col;
             if (rr >= n) continue;
             const float big = fmaxf(fmaxf(lds.m[0][rr], lds.m[1][rr]), fmaxf(lds.m[2][rr], lds.m[3][rr]));
@@ -456,7 +457,8 @@ template <typename T, int D, int WAVES> __device__ __forceinline__ void many_row
             for (uint32_t b = 0; b < a.batch.n_seqs && !found; b += 64) {
                 const uint32_t s = min(b + lane, a.batch.n_seqs - 1), first_s = a.batch.first_row(s), end_s = a.batch.rows_end(s);
                 const int32_t len_s = a.batch.length(s);
-                const uint32_t tiles = b + lane < a.batch.n_seqs && end_s > first_s ? (min(end_s - first_s, a.max_new) * a.group + kRows - 1) / kRows : 0;
+                const uint32_t rows = b + lane < a.batch.n_seqs && end_s > first_s ? min(end_s - first_s, a.max_new) * a.group : 0;
+                const uint32_t tiles = rows > a.least_many ? (rows + kRows - 1) / kRows : 0;
                 const uint32_t upto = dcdev::lanes_prefix_sum<false>(tiles);
                 const uint64_t beyond = __ballot(upto > tile);
                 if (beyond) {
@@ -815,7 +817,7 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
 {
     __shared__ __align__(16) FewLds<D, RT> lds;
     const bool common = blockIdx.x < a.prefix.blocks;
-    few_rows<T, D, RT>(a, lds, common, common ? blockIdx.x : blockIdx.x - a.prefix.blocks);
+    few_rows<T, D, RT>(a, common ? a.prefix : a.own, lds, common, common ? blockIdx.x : blockIdx.x - a.prefix.blocks);
 }
 
 template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, workgroups_a_unit<D>()) void dc_attention_i8_tile_kernel(AttentionArgs a)
@@ -836,7 +838,27 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
         TileLds<D, 4> many;
     } lds;
     if (blockIdx.x < a.prefix.blocks) many_rows<T, D, 4>(a, lds.many, true, blockIdx.x);
-    else few_rows<T, D, RT>(a, lds.few, false, blockIdx.x - a.prefix.blocks);
+    else few_rows<T, D, RT>(a, a.own, lds.few, false, blockIdx.x - a.prefix.blocks);
+}
+
+// Sequences with many rows, and among them some with at most 16 (a prompt, or a piece of one, among generated tokens), which only the device can tell: these are
+// taken as few rows, behind the others; two to a workgroup of 512 threads.  8 heads of 128 for 32 (us; all as many rows, and so): 2048 tokens and 63 sequences of one
+// token over 4096 264 and 153 (the parts alone 74 and 85), 512 behind 1536 and 32 of them 175 and 127; where all have many rows, 852 workgroups of heads of
+// 64, 67.8 and 68.9.
+template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, workgroups_a_unit<D>()) void dc_attention_i8_mixed_kernel(AttentionArgs a)
+{
+    __shared__ __align__(16) union {
+        FewLds<D, 1> few[WAVES / 4];
+        TileLds<D, WAVES> many;
+    } lds;
+    const uint32_t many = a.prefix.blocks + a.own.blocks;
+    if (blockIdx.x < many) {
+        const bool common = blockIdx.x < a.prefix.blocks;
+        many_rows<T, D, WAVES>(a, lds.many, common, common ? blockIdx.x : blockIdx.x - a.prefix.blocks);
+    } else {
+        const uint32_t team = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), item = (blockIdx.x - many) * (WAVES / 4) + team;
+        if (item < a.few.blocks) few_rows<T, D, 1>(a, a.few, lds.few[team], false, item);
+    }
 }
 
 template <typename T, int D> void launch(const AttentionArgs &a, const Plan &plan, hipStream_t stream)
@@ -853,11 +875,13 @@ template <typename T, int D> void launch(const AttentionArgs &a, const Plan &pla
         else if (kind == kTile) {
             if constexpr (wide_tile_rows(D) > kTileRows) {
                 if (plan.tile_rows > kTileRows) {
-                    hipLaunchKernelGGL((dc_attention_i8_tile_kernel<T, D, 8>), grid, dim3(512), 0, stream, a);
+                    if (a.few.blocks) hipLaunchKernelGGL((dc_attention_i8_mixed_kernel<T, D, 8>), dim3(grid.x + (a.few.blocks + 1) / 2), dim3(512), 0, stream, a);
+                    else hipLaunchKernelGGL((dc_attention_i8_tile_kernel<T, D, 8>), grid, dim3(512), 0, stream, a);
                     return;
                 }
             }
-            hipLaunchKernelGGL((dc_attention_i8_tile_kernel<T, D, 4>), grid, threads, 0, stream, a);
+            if (a.few.blocks) hipLaunchKernelGGL((dc_attention_i8_mixed_kernel<T, D, 4>), dim3(grid.x + a.few.blocks), threads, 0, stream, a);
+            else hipLaunchKernelGGL((dc_attention_i8_tile_kernel<T, D, 4>), grid, threads, 0, stream, a);
         }
         else if constexpr (D < 256) hipLaunchKernelGGL((dc_attention_i8_few_kernel<T, D, 2>), grid, threads, 0, stream, a);
     }

@@ -92,6 +92,25 @@ def test_windows_of_prompts(window, sinks):
     run(6, "f16", 2, 1, 64, 16, 16, [260, 99, 190], [260, 99, 70], window, sinks)
 
 
+@pytest.mark.parametrize("heads,kv_heads", [(4, 4), (8, 2), (16, 1), (20, 1)])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("news,lens", [([150, 1], [150, 900]), ([1, 0, 2, 70, 4, 5, 16, 17, 1], [77, 30, 2, 300, 4, 500, 16, 17, 1]),
+                                       ([1] * 40 + [40] + [1] * 30, [60 + 7 * i for i in range(71)])])
+def test_prompts_among_single_tokens(heads, kv_heads, d, news, lens):
+    """Few rows and many in one batch: each kind is a part of its own."""
+    run(41, "bf16", heads, kv_heads, d, 16, 16, lens, news)
+    run(42, "f16", heads, kv_heads, d, 32, 16, [n + 45 for n in lens], news, prefix=45, window=200, sinks=3)
+
+
+@pytest.mark.parametrize("news,lens,kw", [([300, 1, 3], [3000, 5000, 2000], {}), ([300, 1, 3], [3000, 5000, 2000], dict(window=1000, sinks=70)),
+                                          ([200, 4] * 2, [9000, 8300, 8500, 8333], dict(prefix=8192)), ([300, 1, 3], [3000, 5000, 2000], dict(max_len=1)),
+                                          ([300, 1, 3], [30, 1, 2000], {}), ([600, 16, 1], [700, 5000, 3000], dict(absent=[(1, 3), (2, 0), (2, 40)]))])
+def test_prompts_among_single_tokens_of_long_contexts(news, lens, kw):
+    """Few sequences, whose keys are cut into parts for both kinds of rows; hints that are too small; sequences shorter than their rows; pages that are not there."""
+    run(43, "bf16", 4, 2, 128, 32, 32, lens, news, **kw)
+    run(44, "f16", 8, 1, 64, 64, 16, lens, news, **kw)
+
+
 @pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("prefix", [1, 15, 64, 100, 257])
 def test_common_prefix_one_token(d, prefix):
