@@ -843,7 +843,7 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
 
 // Sequences with many rows, and among them some with at most 16 (a prompt, or a piece of one, among generated tokens), which only the device can tell: these are
 // taken as few rows, behind the others; two to a workgroup of 512 threads.  8 heads of 128 for 32 (us; all as many rows, and so): 2048 tokens and 63 sequences of one
-// token over 4096 264 and 153 (the parts alone 74 and 85), 512 behind 1536 and 32 of them 175 and 127; where all have many rows, 852 workgroups of heads of
+// token over 4096 264 and 153 (the parts alone 74 and 85), 512 behind 1536 and 32 of them 175 and 114; where all have many rows, 852 workgroups of heads of
 // 64, 67.8 and 68.9.
 template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, workgroups_a_unit<D>()) void dc_attention_i8_mixed_kernel(AttentionArgs a)
 {

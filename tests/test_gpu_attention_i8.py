@@ -340,6 +340,13 @@ def test_long_contexts(d):
     run(34, "f16", 4, 1, d, 64, 32, [2500, 600], [40, 3])
 
 
+@pytest.mark.parametrize("heads,kv_heads,d,lens,news", [(16, 2, 64, [6000], [300]), (12, 4, 128, [3000], [400]), (5, 1, 256, [2000, 1990], [100, 90]), (20, 5, 64, [700] * 30, [1] * 30)])
+def test_parts_of_many_rows(heads, kv_heads, d, lens, news):
+    """Keys in parts, whose results are joined for many rows and heads."""
+    run(45, "bf16", heads, kv_heads, d, 64, 64, lens, news, uniform=max(news) == 1)
+    run(46, "f16", heads, kv_heads, d, 64, 32, lens, news, window=900, sinks=2, absent=[(0, 1)], uniform=max(news) == 1)
+
+
 def test_pools_of_more_than_four_gib():
     """Pages beyond 2^32 bytes of the pools."""
     d, page, kv, block = 128, 256, 8, 32
