@@ -347,6 +347,34 @@ def test_parts_of_many_rows(heads, kv_heads, d, lens, news):
     run(46, "f16", heads, kv_heads, d, 64, 32, lens, news, window=900, sinks=2, absent=[(0, 1)], uniform=max(news) == 1)
 
 
+@pytest.mark.parametrize("lens,news,prefix", [([300, 70, 900], [150, 1, 2], 0), ([2500, 1800], [300, 1], 0), ([1900] * 40, [1] * 40, 1024), ([900, 800, 850], [60, 3, 40], 700), ([50, 60], [1, 2], 0)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_behind_the_last_sequence(lens, news, prefix, d):
+    """Rows of no sequence, as a recorded step has them: their results stay as they were."""
+    print(f"case i8 rows behind lens={lens} news={news} prefix={prefix} d={d}", flush=True)
+    p = paged_i8(47, 2, d, 32, 32, lens, news, prefix)
+    heads, rows, more = 8, int(p["batch"]["starts"][-1]), 150
+    q = queries(p, heads)
+    cache, t = device_cache_i8(p)
+    starts = torch.from_numpy(p["batch"]["starts"]).cuda()
+    lens_d, pages = torch.from_numpy(p["batch"]["lens"]).cuda(), torch.from_numpy(p["batch"]["pages"]).cuda()
+    prefix_pages = torch.from_numpy(p["batch"]["prefix_pages"]).cuda()
+    b = dc.KVBatch(len(lens), rows + more, max(news), max(lens), lens_d, pages, pages.shape[1], row_start_dev=starts, prefix_len=prefix,
+                   prefix_pages_dev=prefix_pages if prefix else None)
+    qd = torch.full((rows + more, heads, d), float("nan"), dtype=q.dtype, device="cuda")
+    qd[:rows] = q.cuda()
+    out = torch.full_like(qd, SENTINEL)
+    lse = torch.full((rows + more, heads), SENTINEL, dtype=torch.float32, device="cuda")
+    a = dc.Attention(heads, qd, out, lse, d ** -0.5)
+    n = dc.attention_paged_workspace(cache, b, a)
+    ws = torch.full((n + 16,), 0xFF, dtype=torch.uint8, device="cuda")
+    dc.attention_paged(cache, b, a, ws, n, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert (out[rows:] == SENTINEL).all() and (lse[rows:] == SENTINEL).all()
+    want = oa.attend(*pool_values(p), p["batch"], f64(q), np.float64(np.float32(d ** -0.5)))
+    check_attend_i8("bf16", d, f64(out[:rows]), f64(lse[:rows]), *want, 2.0 ** -4)
+
+
 def test_pools_of_more_than_four_gib():
     """Pages beyond 2^32 bytes of the pools."""
     d, page, kv, block = 128, 256, 8, 32
