@@ -45,6 +45,10 @@ struct AttentionArgs {
     bool whole;        // the prefix is read with the sequences' own pages, not as a part of its own
     Part prefix, own, few;  // few: of sequences with at most least_many rows among others with many
     uint32_t least_many;
+    // The splits of those are theirs alone (0: they are as many as the others'): [sequence][row, few_rows_a_seq of them][head][slot], as above.
+    uint32_t few_rows_a_seq;
+    float *few_partial;
+    f32x2 *few_partial_ml;
     // of a cache of 8 bits: scale of [page][head][token >> block_shift]
     const float *k_scales, *v_scales;
     uint32_t block_shift;
@@ -191,6 +195,7 @@ enum Kind { kFew16 = 0, kFew32 = 1, kTile = 2 };
 struct Plan {
     Kind prefix_kind, own_kind;
     uint32_t tile_rows; // of a workgroup of the kernel for many rows
+    uint64_t few_at;    // where the workspace has what the splits of few rows among many leave
 };
 // Over a cache of 8 bits a workgroup has up to this many rows (of heads of 64 and 256 a half less: a wavefront's part of a tile is no whole load, or registers
 // are for four wavefronts only).

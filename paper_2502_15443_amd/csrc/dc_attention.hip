@@ -784,20 +784,46 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
     }
 }
 
+// Rows of sequence `seq` times the query heads of a key/value head.
+__device__ __forceinline__ uint32_t rows_of(const AttentionArgs &a, uint32_t seq, uint32_t &first)
+{
+    first = a.batch.first_row(seq);
+    const uint32_t end = a.batch.rows_end(seq);
+    return end > first ? min(end - first, a.max_new) * a.group : 0;
+}
+// Which row a workgroup joins, and whether there is one: `i` is the row, or counts off the rows of sequences with few.
+enum Joined { kAllRows, kManyRows, kFewRows };
+template <Joined ROWS> __device__ __forceinline__ bool row_to_join(const AttentionArgs &a, uint32_t i, uint32_t &row)
+{
+    row = i;
+    if (ROWS == kAllRows) return a.batch.sequence_of(row, a.max_new) < a.batch.n_seqs;
+    uint32_t first;
+    if (ROWS == kManyRows) {
+        const uint32_t seq = a.batch.sequence_of(row, a.max_new);
+        return seq < a.batch.n_seqs && rows_of(a, seq, first) > a.least_many;
+    }
+    const uint32_t rows = rows_of(a, i / a.few_rows_a_seq, first), in_seq = i % a.few_rows_a_seq;
+    row = first + in_seq;
+    return rows <= a.least_many && in_seq * a.group < rows;
+}
+
 // Joins the splits of a row and head: each has its sums relative to a maximum of its own.  The weights of the splits first, into the LDS; then
 // 4 D / 1024 of the threads go through every so many splits with several loads under way: 3 us for 32 rows and heads, 5.4 for 64 rows of 32 heads.  (The last
 // split to arrive joining them all instead: every workgroup's device-wide fence empties its L2, one token 106 instead of 12 us.)
 constexpr uint32_t kMostSplits = 128, kMostSlots = 2 * kMostSplits; // of a part, of both parts
-template <typename T, int D> __global__ __launch_bounds__(256) void dc_attention_join_kernel(AttentionArgs a)
+template <typename T, int D, Joined ROWS> __global__ __launch_bounds__(256) void dc_attention_join_kernel(AttentionArgs a)
 {
     constexpr uint32_t kQuads = D / 4, kSets = 256 / kQuads, kAtOnce = 4;
     __shared__ f32x4 lds_sum[kSets][kQuads];
     __shared__ float lds_weight[kMostSlots], lds_top[4], lds_total[4];
-    const uint32_t row = blockIdx.x, head = blockIdx.y, at = threadIdx.x % kQuads, set = threadIdx.x / kQuads;
-    const uint64_t first = ((uint64_t)row * a.n_heads + head) * a.n_slots;
+    const uint32_t head = blockIdx.y, at = threadIdx.x % kQuads, set = threadIdx.x / kQuads, n_slots = ROWS == kFewRows ? a.few.n_splits : a.n_slots;
+    const uint64_t first = ((uint64_t)blockIdx.x * a.n_heads + head) * n_slots;
+    const float *partial = ROWS == kFewRows ? a.few_partial : a.partial;
+    const f32x2 *partial_ml = ROWS == kFewRows ? a.few_partial_ml : a.partial_ml;
     f32x2 ml = {-INFINITY, 0.0f};
-    if (threadIdx.x < a.n_slots) ml = a.partial_ml[first + threadIdx.x];
-    if (a.batch.sequence_of(row, a.max_new) >= a.batch.n_seqs) return;
+    if (threadIdx.x < n_slots) ml = partial_ml[first + threadIdx.x];
+    uint32_t row;
+    if (!row_to_join<ROWS>(a, blockIdx.x, row)) return;
     float top = max_over_16(ml[0]);
 #pragma unroll
     for (int k = 1; k < 16; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
@@ -813,14 +839,14 @@ template <typename T, int D> __global__ __launch_bounds__(256) void dc_attention
     __syncthreads();
     total = (lds_total[0] + lds_total[1]) + (lds_total[2] + lds_total[3]);
     f32x4 sum = {};
-    const float *src = a.partial + first * D + 4 * at;
-    for (uint32_t slot = set; slot < a.n_slots; slot += kSets * kAtOnce) {
+    const float *src = partial + first * D + 4 * at;
+    for (uint32_t slot = set; slot < n_slots; slot += kSets * kAtOnce) {
         f32x4 v[kAtOnce];
         float w[kAtOnce];
 #pragma unroll
         for (uint32_t i = 0; i < kAtOnce; i++) {
             const uint32_t k = slot + i * kSets;
-            w[i] = k < a.n_slots ? lds_weight[k] : -1.0f; // a split that saw nothing has left nothing to add
+            w[i] = k < n_slots ? lds_weight[k] : -1.0f; // a split that saw nothing has left nothing to add
             v[i] = f32x4{};
             if (w[i] >= 0.0f || w[i] != w[i]) v[i] = *reinterpret_cast<const f32x4 *>(src + (uint64_t)k * D);
         }
@@ -873,14 +899,15 @@ template <typename T> void launch_d(const AttentionArgs &a, const Plan &plan, ui
 // 16384 rows and heads of 4 splits 7.8 us, with a workgroup to each 20.2; 4800 of 12 the whole call 27.8 and 30.8; 32 of 8 as long; 2048 of 16 7.1 and 5.3, for
 // with so few each thread's loads count, which are behind one another.
 bool few_splits(const AttentionArgs &a) { return a.n_slots <= 8 || (a.n_slots <= 16 && (uint64_t)a.batch.n_rows * a.n_heads >= 4096); }
-template <typename T, int D> __global__ __launch_bounds__(256) void dc_attention_join_few_kernel(AttentionArgs a)
+template <typename T, int D, Joined ROWS> __global__ __launch_bounds__(256) void dc_attention_join_few_kernel(AttentionArgs a)
 {
     constexpr uint32_t kQuads = D / 4, kAtOnce = 8;
     const uint32_t row = blockIdx.x, head = blockIdx.y * (256 / kQuads) + threadIdx.x / kQuads, at = threadIdx.x % kQuads, lane16 = threadIdx.x & 15u;
     const uint64_t first = ((uint64_t)row * a.n_heads + min(head, a.n_heads - 1)) * a.n_slots;
     f32x2 ml = {-INFINITY, 0.0f};
     if (lane16 < a.n_slots) ml = a.partial_ml[first + lane16];
-    if (a.batch.sequence_of(row, a.max_new) >= a.batch.n_seqs) return;
+    uint32_t same;
+    if (!row_to_join<ROWS>(a, row, same)) return;
     float top = ml[0];
 #pragma unroll
     for (int k = 1; k < 16; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
@@ -905,21 +932,29 @@ template <typename T, int D> __global__ __launch_bounds__(256) void dc_attention
     if (head < a.n_heads) store_whole<T>(a, row, head, 4 * at, sum, top, total);
 }
 
-template <typename T> void launch_join_few(const AttentionArgs &a, uint32_t head_dim, hipStream_t stream)
+template <typename T, Joined ROWS> void launch_join_few(const AttentionArgs &a, uint32_t head_dim, hipStream_t stream)
 {
     const uint32_t heads = 1024 / head_dim;
     const dim3 grid(a.batch.n_rows, (a.n_heads + heads - 1) / heads), threads(256);
-    if (head_dim == 64) hipLaunchKernelGGL((dc_attention_join_few_kernel<T, 64>), grid, threads, 0, stream, a);
-    else if (head_dim == 128) hipLaunchKernelGGL((dc_attention_join_few_kernel<T, 128>), grid, threads, 0, stream, a);
-    else hipLaunchKernelGGL((dc_attention_join_few_kernel<T, 256>), grid, threads, 0, stream, a);
+    if (head_dim == 64) hipLaunchKernelGGL((dc_attention_join_few_kernel<T, 64, ROWS>), grid, threads, 0, stream, a);
+    else if (head_dim == 128) hipLaunchKernelGGL((dc_attention_join_few_kernel<T, 128, ROWS>), grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL((dc_attention_join_few_kernel<T, 256, ROWS>), grid, threads, 0, stream, a);
 }
 
-template <typename T> void launch_join(const AttentionArgs &a, uint32_t head_dim, hipStream_t stream)
+template <typename T, Joined ROWS> void launch_join_one(const AttentionArgs &a, uint32_t head_dim, hipStream_t stream)
 {
-    const dim3 grid(a.batch.n_rows, a.n_heads), threads(256);
-    if (head_dim == 64) hipLaunchKernelGGL((dc_attention_join_kernel<T, 64>), grid, threads, 0, stream, a);
-    else if (head_dim == 128) hipLaunchKernelGGL((dc_attention_join_kernel<T, 128>), grid, threads, 0, stream, a);
-    else hipLaunchKernelGGL((dc_attention_join_kernel<T, 256>), grid, threads, 0, stream, a);
+    const dim3 grid(ROWS == kFewRows ? a.batch.n_seqs * a.few_rows_a_seq : a.batch.n_rows, a.n_heads), threads(256);
+    if (head_dim == 64) hipLaunchKernelGGL((dc_attention_join_kernel<T, 64, ROWS>), grid, threads, 0, stream, a);
+    else if (head_dim == 128) hipLaunchKernelGGL((dc_attention_join_kernel<T, 128, ROWS>), grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL((dc_attention_join_kernel<T, 256, ROWS>), grid, threads, 0, stream, a);
+}
+
+template <typename T> void launch_join(const AttentionArgs &a, bool is_i8, uint32_t head_dim, hipStream_t stream)
+{
+    const bool few = is_i8 && few_splits(a);
+    if (a.n_slots > 1 && a.few_rows_a_seq) few ? launch_join_few<T, kManyRows>(a, head_dim, stream) : launch_join_one<T, kManyRows>(a, head_dim, stream);
+    else if (a.n_slots > 1) few ? launch_join_few<T, kAllRows>(a, head_dim, stream) : launch_join_one<T, kAllRows>(a, head_dim, stream);
+    if (a.few_rows_a_seq && a.few.n_splits > 1) launch_join_one<T, kFewRows>(a, head_dim, stream);
 }
 
 // How a call's keys are cut: fills prefix, own and n_slots, and gives the bytes of workspace.  False for a batch that is too large.
@@ -936,14 +971,14 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     // Keys and values of 8 bits are made wide once for 256 rows instead of 128 where there are as many (a prompt of 4096, 32 heads of 128: 168 and 188 us), and
     // where the kernel for many rows has the launch to itself.
     const uint64_t tile_rows = cache->type == DC_TYPE_I8 && own_kind == kTile && seq_rows > kTileRows ? wide_tile_rows((uint32_t)d) : kTileRows;
-    plan = Plan{prefix_kind, own_kind, (uint32_t)tile_rows};
+    plan = Plan{prefix_kind, own_kind, (uint32_t)tile_rows, 0};
     const uint64_t own_len = batch->max_len > prefix_len ? batch->max_len - prefix_len : 1;
     const uint64_t seq_tiles = (seq_rows + tile_rows - 1) / tile_rows; // workgroups to a sequence's rows
     // upper bound of the workgroups' number, as the kernel counts them off
     const uint64_t row_tiles = !batch->row_start_dev ? batch->n_seqs * seq_tiles : std::min<uint64_t>(all_rows / tile_rows + batch->n_seqs, all_rows);
     const uint64_t tile_many = d == 256 ? 32 : 64;
     const Kind few_kind = prefix_len && prefix_kind != kTile ? prefix_kind : own_kind; // of the kernel for few rows, if one runs
-    const uint64_t tile_few = cache->type == DC_TYPE_I8 ? few_tile(few_kind == kFew16 ? 1 : 2) : 32;
+    const uint64_t tile_few = cache->type == DC_TYPE_I8 ? few_tile(few_kind == kFew32 ? 2 : 1) : 32;
     const double unit_rate = d == 64 ? 1.5 : d == 128 ? 0.87 : 0.55; // steps a us of a full compute unit in the kernel for many rows
 
     // Of the kernel for few rows: items are workgroups uncut.
@@ -1024,13 +1059,16 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     }
     if (own_kind == kTile) {
         if (!a.whole) a.own = many_part(false);
-        // Over a cache of 8 bits sequences of at most 16 rows, which may be among them, are taken as few rows, in as many parts.
+        // Over a cache of 8 bits sequences of at most 16 rows, which may be among them, are taken as few rows, in as many parts as the others; without a prefix in
+        // parts of their own, and joined by a launch of their own, where those would be long, of which one reads 80 tokens a us (us: as many parts, and their own: 2048
+        // new tokens and 4 sequences of one token over 32768 335 and 168, and one over 100000 798 and 172; but 512 and 32 of one over 4096 114 and 131).
         if (cache->type == DC_TYPE_I8 && !a.whole && batch->row_start_dev && batch->n_seqs > 1 && group <= 16) {
-            const uint64_t n_tiles = std::max<uint64_t>(1, (seen(own_len, 16) + few_tile(1) - 1) / few_tile(1)), n = a.own.n_splits;
-            const uint64_t blocks = (uint64_t)cache->n_kv_heads * batch->n_seqs * n;
-            if (a.own.blocks + (uint64_t)a.prefix.blocks + blocks < 1u << 24) {
-                a.few = Part{(uint32_t)blocks, (uint32_t)n, (uint32_t)((n_tiles + n - 1) / n), a.own.first_slot};
-                a.least_many = 16;
+            const uint64_t items = (uint64_t)cache->n_kv_heads * batch->n_seqs, tokens = seen(own_len, 16), n_tiles = std::max<uint64_t>(1, (tokens + tile_few - 1) / tile_few);
+            const bool apart = !prefix_len && tokens / a.own.n_splits >= 8192;
+            const uint64_t n = apart ? cut_few(items, tokens) : a.own.n_splits;
+            if (a.own.blocks + (uint64_t)a.prefix.blocks + items * n < 1u << 24) {
+                a.few = apart ? part(items, tokens, tile_few, n, 0) : Part{(uint32_t)(items * n), (uint32_t)n, (uint32_t)((n_tiles + n - 1) / n), a.own.first_slot};
+                a.least_many = 16, a.few_rows_a_seq = apart ? (uint32_t)(16 / group) : 0;
             }
         }
     } else {
@@ -1040,6 +1078,10 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     if (!a.own.blocks || (uint64_t)a.own.blocks + a.prefix.blocks >= 1u << 24) return false;
     a.n_slots = a.prefix.n_splits + a.own.n_splits;
     if (a.n_slots > 1) *workspace_bytes = (uint64_t)batch->n_rows * t->n_heads * a.n_slots * (d + 2) * sizeof(float);
+    if (a.few_rows_a_seq && a.few.n_splits > 1) {
+        plan.few_at = (*workspace_bytes + 15) / 16 * 16;
+        *workspace_bytes = plan.few_at + (uint64_t)batch->n_seqs * a.few_rows_a_seq * t->n_heads * a.few.n_splits * (d + 2) * sizeof(float);
+    }
     return true;
 }
 
@@ -1074,6 +1116,10 @@ extern "C" int dc_attention_paged(const dc_kv_cache *cache, const dc_kv_batch *b
     if (workspace_bytes < needed) return DC_E_CAP;
     a.partial = static_cast<float *>(workspace_dev);
     a.partial_ml = reinterpret_cast<f32x2 *>(a.partial + (uint64_t)batch->n_rows * a.n_heads * a.n_slots * cache->head_dim);
+    if (a.few_rows_a_seq && a.few.n_splits > 1) {
+        a.few_partial = reinterpret_cast<float *>(static_cast<char *>(workspace_dev) + plan.few_at);
+        a.few_partial_ml = reinterpret_cast<f32x2 *>(a.few_partial + (uint64_t)batch->n_seqs * a.few_rows_a_seq * a.n_heads * a.few.n_splits * cache->head_dim);
+    }
     const uint32_t d = cache->head_dim, rows_type = rows_type_of(cache);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (cache->type == DC_TYPE_I8) {
@@ -1084,12 +1130,7 @@ extern "C" int dc_attention_paged(const dc_kv_cache *cache, const dc_kv_batch *b
     } else {
         launch_d<_Float16>(a, plan, d, stream);
     }
-    if (a.n_slots > 1 && cache->type == DC_TYPE_I8 && few_splits(a)) {
-        if (rows_type == DC_TYPE_BF16) launch_join_few<__bf16>(a, d, stream);
-        else launch_join_few<_Float16>(a, d, stream);
-    } else if (a.n_slots > 1) {
-        if (rows_type == DC_TYPE_BF16) launch_join<__bf16>(a, d, stream);
-        else launch_join<_Float16>(a, d, stream);
-    }
+    if (rows_type == DC_TYPE_BF16) launch_join<__bf16>(a, cache->type == DC_TYPE_I8, d, stream);
+    else launch_join<_Float16>(a, cache->type == DC_TYPE_I8, d, stream);
     return dc_launch_status();
 }

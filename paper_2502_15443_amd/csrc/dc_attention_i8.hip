@@ -121,7 +121,8 @@ template <int D, int RT> struct FewLds {
     int32_t p[16 * RT];
 };
 
-template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(const AttentionArgs &a, const Part &part, FewLds<D, RT> &lds, bool common, uint32_t item)
+// APART: the parts of these rows are theirs alone.
+template <typename T, int D, int RT, bool APART = false> __device__ __forceinline__ void few_rows(const AttentionArgs &a, const Part &part, FewLds<D, RT> &lds, bool common, uint32_t item)
 {
     constexpr int kTile = few_tile(RT), kQuarters = kTile / 16, KS = D / 32, DT = D / 16;
     constexpr int kChunks = D / 16, kTokensALoad = 64 / kChunks, kLoads = kTile / kTokensALoad; // chunks: of 16 bytes
@@ -403,7 +404,16 @@ template <typename T, int D, int RT> __device__ __forceinline__ void few_rows(co
                 sum += *reinterpret_cast<const f32x4 *>(&lds.sums[w4][col][at]);
                 if (lds.m[w4][rr] != -INFINITY) total += lds.l[w4][rr] * exp2_of(lds.m[w4][rr] - big);
             }
-            store_result<T, D>(a, row_first + rr / a.group, kv * a.group + rr % a.group, part.first_slot + split, at, sum, big, total);
+            const uint32_t in_seq = rr / a.group, head = kv * a.group + rr % a.group;
+            if (!APART) {
+                store_result<T, D>(a, row_first + in_seq, head, part.first_slot + split, at, sum, big, total);
+            } else if (part.n_splits == 1) {
+                store_whole<T>(a, row_first + in_seq, head, at, sum, big, total);
+            } else {
+                const uint64_t to = (((uint64_t)seq * a.few_rows_a_seq + in_seq) * a.n_heads + head) * part.n_splits + split;
+                *reinterpret_cast<f32x4 *>(a.few_partial + to * D + at) = sum;
+                if (at == 0) a.few_partial_ml[to] = f32x2{big, total};
+            }
         }
     }
 }
@@ -845,7 +855,7 @@ template <typename T, int D, int RT> __global__ __launch_bounds__(256, D == 256 
 // taken as few rows, behind the others; two to a workgroup of 512 threads.  8 heads of 128 for 32 (us; all as many rows, and so): 2048 tokens and 63 sequences of one
 // token over 4096 264 and 153 (the parts alone 74 and 85), 512 behind 1536 and 32 of them 175 and 114; where all have many rows, 852 workgroups of heads of
 // 64, 67.8 and 68.9.
-template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, workgroups_a_unit<D>()) void dc_attention_i8_mixed_kernel(AttentionArgs a)
+template <typename T, int D, int WAVES, bool APART> __global__ __launch_bounds__(64 * WAVES, workgroups_a_unit<D>()) void dc_attention_i8_mixed_kernel(AttentionArgs a)
 {
     __shared__ __align__(16) union {
         FewLds<D, 1> few[WAVES / 4];
@@ -857,8 +867,15 @@ template <typename T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES,
         many_rows<T, D, WAVES>(a, lds.many, common, common ? blockIdx.x : blockIdx.x - a.prefix.blocks);
     } else {
         const uint32_t team = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), item = (blockIdx.x - many) * (WAVES / 4) + team;
-        if (item < a.few.blocks) few_rows<T, D, 1>(a, a.few, lds.few[team], false, item);
+        if (item < a.few.blocks) few_rows<T, D, 1, APART>(a, a.few, lds.few[team], false, item);
     }
+}
+template <typename T, int D, int WAVES> void launch_mixed(const AttentionArgs &a, hipStream_t stream)
+{
+    constexpr uint32_t kTeams = WAVES / 4;
+    const dim3 grid(a.prefix.blocks + a.own.blocks + (a.few.blocks + kTeams - 1) / kTeams), threads(64 * WAVES);
+    if (a.few_rows_a_seq) hipLaunchKernelGGL((dc_attention_i8_mixed_kernel<T, D, WAVES, true>), grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL((dc_attention_i8_mixed_kernel<T, D, WAVES, false>), grid, threads, 0, stream, a);
 }
 
 template <typename T, int D> void launch(const AttentionArgs &a, const Plan &plan, hipStream_t stream)
@@ -875,12 +892,12 @@ template <typename T, int D> void launch(const AttentionArgs &a, const Plan &pla
         else if (kind == kTile) {
             if constexpr (wide_tile_rows(D) > kTileRows) {
                 if (plan.tile_rows > kTileRows) {
-                    if (a.few.blocks) hipLaunchKernelGGL((dc_attention_i8_mixed_kernel<T, D, 8>), dim3(grid.x + (a.few.blocks + 1) / 2), dim3(512), 0, stream, a);
+                    if (a.few.blocks) launch_mixed<T, D, 8>(a, stream);
                     else hipLaunchKernelGGL((dc_attention_i8_tile_kernel<T, D, 8>), grid, dim3(512), 0, stream, a);
                     return;
                 }
             }
-            if (a.few.blocks) hipLaunchKernelGGL((dc_attention_i8_mixed_kernel<T, D, 4>), dim3(grid.x + a.few.blocks), threads, 0, stream, a);
+            if (a.few.blocks) launch_mixed<T, D, 4>(a, stream);
             else hipLaunchKernelGGL((dc_attention_i8_tile_kernel<T, D, 4>), grid, threads, 0, stream, a);
         }
         else if constexpr (D < 256) hipLaunchKernelGGL((dc_attention_i8_few_kernel<T, D, 2>), grid, threads, 0, stream, a);

@@ -104,10 +104,14 @@ def test_prompts_among_single_tokens(heads, kv_heads, d, news, lens):
 
 @pytest.mark.parametrize("news,lens,kw", [([300, 1, 3], [3000, 5000, 2000], {}), ([300, 1, 3], [3000, 5000, 2000], dict(window=1000, sinks=70)),
                                           ([200, 4] * 2, [9000, 8300, 8500, 8333], dict(prefix=8192)), ([300, 1, 3], [3000, 5000, 2000], dict(max_len=1)),
-                                          ([300, 1, 3], [30, 1, 2000], {}), ([600, 16, 1], [700, 5000, 3000], dict(absent=[(1, 3), (2, 0), (2, 40)]))])
+                                          ([300, 1, 3], [30, 1, 2000], {}), ([40, 2, 0, 1], [50, 30000, 0, 17000], {}), ([600, 16, 1], [700, 5000, 3000], dict(absent=[(1, 3), (2, 0), (2, 40)]))])
 def test_prompts_among_single_tokens_of_long_contexts(news, lens, kw):
     """Few sequences, whose keys are cut into parts for both kinds of rows; hints that are too small; sequences shorter than their rows; pages that are not there."""
     run(43, "bf16", 4, 2, 128, 32, 32, lens, news, **kw)
+    # (a hint by which the few rows' keys are cut into parts of their own)
+    if "prefix" not in kw:
+        run(43, "bf16", 4, 2, 128, 32, 32, lens, news, **{**kw, "max_len": 2 ** 20})
+        run(44, "f16", 5, 1, 256, 32, 32, lens, news, **{**kw, "max_len": 2 ** 20, "window": 0})
     run(44, "f16", 8, 1, 64, 64, 16, lens, news, **kw)
 
 
