@@ -615,7 +615,8 @@ typedef struct {
  *   workspace_dev   at least dc_attention_paged_workspace() bytes, 16-byte aligned (NULL if that is 0); its contents before the
  *                   call do not matter, and it may be reused once the call's work on the stream is done
  * Errors: DC_E_ARG (also where n_rows * n_heads reaches 2^31, or n_kv_heads times the sequences, or times the runs of 128 rows that share
- * a key/value head, 2^24), DC_E_CAP (workspace too small), DC_E_HIP.
+ * a key/value head, 2^24; with a common prefix that is read once, those runs of all rows together and of the sequences count together), DC_E_CAP
+ * (workspace too small), DC_E_HIP.
  */
 int dc_attention_paged_workspace(const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_attention *attention,
                                  uint64_t *workspace_bytes);

@@ -957,8 +957,9 @@ template <typename T> void launch_join(const AttentionArgs &a, bool is_i8, uint3
     if (a.few_rows_a_seq && a.few.n_splits > 1) launch_join_one<T, kFewRows>(a, head_dim, stream);
 }
 
-// How a call's keys are cut: fills prefix, own and n_slots, and gives the bytes of workspace.  False for a batch that is too large.
-bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_attention *t, uint64_t *workspace_bytes)
+// How a call's keys are cut, with at most `most_rows` rows to a workgroup: fills prefix, own and n_slots, and gives the bytes of workspace.  False for a
+// batch that is too large.
+bool make_plan_by(uint32_t most_rows, AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_attention *t, uint64_t *workspace_bytes)
 {
     *workspace_bytes = 0;
     const uint64_t group = t->n_heads / cache->n_kv_heads, d = cache->head_dim, prefix_len = batch->prefix_len;
@@ -970,7 +971,7 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
     const Kind prefix_kind = kind_of(all_rows), own_kind = kind_of(seq_rows);
     // Keys and values of 8 bits are made wide once for 256 rows instead of 128 where there are as many (a prompt of 4096, 32 heads of 128: 168 and 188 us), and
     // where the kernel for many rows has the launch to itself.
-    const uint64_t tile_rows = cache->type == DC_TYPE_I8 && own_kind == kTile && seq_rows > kTileRows ? wide_tile_rows((uint32_t)d) : kTileRows;
+    const uint64_t tile_rows = cache->type == DC_TYPE_I8 && own_kind == kTile && seq_rows > kTileRows ? std::min(wide_tile_rows((uint32_t)d), most_rows) : kTileRows;
     plan = Plan{prefix_kind, own_kind, (uint32_t)tile_rows, 0};
     const uint64_t own_len = batch->max_len > prefix_len ? batch->max_len - prefix_len : 1;
     const uint64_t seq_tiles = (seq_rows + tile_rows - 1) / tile_rows; // workgroups to a sequence's rows
@@ -1077,6 +1078,8 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
         a.own = part(items, tokens, tile_few, cut_few(items, tokens), a.prefix.n_splits);
     }
     if (!a.own.blocks || (uint64_t)a.own.blocks + a.prefix.blocks >= 1u << 24) return false;
+    // a launch has fewer than 2^32 threads: 512 of them to a workgroup of 256 rows, or to two of few rows beside those
+    if (tile_rows > kTileRows && ((uint64_t)a.own.blocks + a.prefix.blocks + (a.few.blocks + 1ull) / 2) * 512 >= 1ull << 32) return false;
     a.n_slots = a.prefix.n_splits + a.own.n_splits;
     if (a.n_slots > 1) *workspace_bytes = (uint64_t)batch->n_rows * t->n_heads * a.n_slots * (d + 2) * sizeof(float);
     if (a.few_rows_a_seq && a.few.n_splits > 1) {
@@ -1084,6 +1087,16 @@ bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_
         *workspace_bytes = plan.few_at + (uint64_t)batch->n_seqs * a.few_rows_a_seq * t->n_heads * a.few.n_splits * (d + 2) * sizeof(float);
     }
     return true;
+}
+
+// Where workgroups of 256 rows would be too many threads, those of 128 may not be: they have half as many each, and where sequences have fewer rows than that
+// there are as many of them.
+bool make_plan(AttentionArgs &a, Plan &plan, const dc_kv_cache *cache, const dc_kv_batch *batch, const dc_attention *t, uint64_t *workspace_bytes)
+{
+    const AttentionArgs given = a;
+    if (make_plan_by(2 * kTileRows, a, plan, cache, batch, t, workspace_bytes)) return true;
+    a = given;
+    return make_plan_by(kTileRows, a, plan, cache, batch, t, workspace_bytes);
 }
 
 } // namespace
