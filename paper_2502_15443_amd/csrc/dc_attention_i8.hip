@@ -142,7 +142,7 @@ template <typename T, int D, int RT, bool APART = false> __device__ __forceinlin
     // Without a window it is known at once where a wavefront's first tile is: its pages are asked for together with the sequence's length.
     int32_t first_entry = -1;
     const uint64_t first_tile = (uint64_t)split * part.chunk + wave;
-    if (!a.window && first_tile < 1u << 25) first_entry = entry_at((uint32_t)first_tile * kTile);
+    if (!a.window && first_tile < 0x80000000u / kTile) first_entry = entry_at((uint32_t)first_tile * kTile);
 
     // rows of this workgroup: row_first + i / group of head kv * group + i % group for i < n
     uint32_t row_first = 0, n;
