@@ -608,8 +608,8 @@ typedef struct {
  * Scores, sums and results are held in fp32; exp(s_j - reference) is rounded to the cache's type for the product with the values (f16: to at least
  * 2^-32 of the row's largest, so that many small ones are not lost beside a large one).  Over a cache of DC_TYPE_I8 queries and keys enter their product
  * as they are (bf16 queries below 2^-29 of their row's largest value are rounded to 2^-40 of it), and exp(s_j - reference) times the value's scale is
- * rounded to f16, to at least 2^-32 of the largest weight at the largest scale.  The sum of exp(s_j - max s) |v_j| has to stay below 2^120
- * (bf16 values near the type's largest).
+ * rounded to f16, to at least 2^-32 of the largest weight at the largest scale of values (rounded up to a power of two) in a block that the row sees a
+ * token of.  The sum of exp(s_j - max s) |v_j| has to stay below 2^120 (bf16 values near the type's largest).
  * A common prefix (prefix_len > 0) is read once for all sequences' rows together, or where that takes longer by each sequence's rows
  * along with its own pages.
  *   workspace_dev   at least dc_attention_paged_workspace() bytes, 16-byte aligned (NULL if that is 0); its contents before the

@@ -80,24 +80,36 @@ __device__ __forceinline__ uint32_t largest_over_16(uint32_t v)
     return largest_over_32(max(r[0], r[1]));
 }
 
-// Weights go into the product with the values as f16, times the value's scale over the largest scale so far (as a power of two, at least 2^-100) and
-// times 2^kLift: f16 loses bits below 2^-14 and everything below 2^-25, and its largest value is 2^16.  In the kernel for few rows a weight is at most
-// 1, in the one for many 2^8.
+// Weights go into the product with the values as f16, times the value's scale over the largest scale of a block that the row has seen a token of, rounded up to a
+// power of two.  f16 loses bits below 2^-14 and everything below 2^-25, and its largest value is 2^16: the exponentials' reference lies kLift below the largest
+// score, so that the largest weight is 2^15 in the kernel for few rows and 2^7 to 2^15 in the one for many.
 constexpr int kLiftFew = 15, kLiftMany = 7;
 struct ValueScale {
-    uint32_t ref; // bits of the largest scale so far, rounded up to a power of two
-    __device__ __forceinline__ ValueScale() : ref(27u << 23) {}
+    uint32_t ref = 0, least = 0; // of the lane's row: bits of that scale; the smallest of the wavefront's rows
+    float by = 0.0f;             // 1 / ref
+    // (one of a row that is not there never has to grow)
+    __device__ __forceinline__ void begin(bool there) { set(there ? 1u << 23 : 254u << 23); }
     __device__ __forceinline__ float value() const { return __uint_as_float(ref); }
-    // by what weights are multiplied
-    template <int LIFT> __device__ __forceinline__ float by() const { return __uint_as_float(((254u + LIFT) << 23) - ref); }
-    // takes another scale in; true if the reference has grown, and by what sums are multiplied then
-    __device__ __forceinline__ bool grows(uint32_t scale_bits, float &fade)
+    // A scale over it: 1 at most, and for a scale of tokens that the row does not see, whose weights are 0, anything up to 1.
+    __device__ __forceinline__ float share(float scale) const { return __builtin_amdgcn_fmed3f(scale * by, 0.0f, 1.0f); }
+    __device__ __forceinline__ static uint32_t power_above(uint32_t scale_bits) { return (scale_bits + 0x7FFFFFu) & 0x7F800000u; }
+    // Whether the row's has to grow if it sees a scale; whether that of any row would have to, by a scalar comparison (in the kernel for few rows 64 sequences of up to 8192
+    // tokens 120.9 us, by the lanes' 122.4; in the one for many, where some row mostly sees none of the tokens yet, pieces behind a window 70.1 and 69.0).
+    __device__ __forceinline__ bool below(uint32_t scale_bits) const { return power_above(scale_bits) > ref; }
+    __device__ __forceinline__ bool may_grow(uint32_t most_bits) const { return power_above(most_bits) > least; }
+    // Takes in the largest scale that the row sees; by what its sums are multiplied then.
+    __device__ __forceinline__ float take_in(uint32_t scale_bits)
     {
-        const uint32_t up = (scale_bits + 0x7FFFFFu) & 0x7F800000u;
-        if (up <= ref) return false;
-        fade = __uint_as_float((uint32_t)max((int32_t)((127u << 23) + ref - up), 0));
-        ref = up;
-        return true;
+        const uint32_t before = ref;
+        set(max(power_above(scale_bits), ref));
+        return __uint_as_float((uint32_t)max((int32_t)((127u << 23) + before - ref), 0));
+    }
+
+private:
+    __device__ __forceinline__ void set(uint32_t bits)
+    {
+        ref = bits, by = __uint_as_float(max((254u << 23) - bits, 0x400000u)); // (1 / 2^127 is below the normal range)
+        least = ~largest_of_lanes(~bits);
     }
 };
 
@@ -179,6 +191,7 @@ template <typename T, int D, int RT, bool APART = false> __device__ __forceinlin
 
     // queries, and what the lane's rows see
     f16x8 q[RT][KS];
+    ValueScale value_scale[RT];
     float row_scale[RT]; // with a key's scale it makes powers of two of the scores as they come out of the products
     Seen seen[RT];
 #pragma unroll
@@ -198,6 +211,7 @@ template <typename T, int D, int RT, bool APART = false> __device__ __forceinlin
             if (a.negate) x[s] ^= 0x80008000u;
             most = largest(most, x[s]);
         }
+        value_scale[rt].begin(is);
         const Queries<T> as_f16(largest_over_16(most));
         row_scale[rt] = fminf(fmaxf(a.scale * as_f16.back, 0x1p-149f), 0x1p127f);
 #pragma unroll
@@ -205,7 +219,7 @@ template <typename T, int D, int RT, bool APART = false> __device__ __forceinlin
     }
 
     f32x4 o[RT][DT];
-    float m[RT], l[RT];
+    float m[RT], l[RT]; // what a row's weights are relative to, kLiftFew below its largest score; their sum
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) {
         m[rt] = -INFINITY, l[rt] = 0.0f;
@@ -258,7 +272,6 @@ template <typename T, int D, int RT, bool APART = false> __device__ __forceinlin
     // of this tile and the next one: pages of the quarters, scales; of the one behind it the table's entries
     int32_t page = -1, next_page = -1, entry = -1;
     float scale = 0.0f, next_scale = 0.0f;
-    ValueScale value_scale;
     int32_t t = t_begin + (int32_t)wave;
     auto token_of = [&](int32_t t) { return tiles.first_token(min(t, t_end - 1)); };
     if (t < t_end) {
@@ -308,20 +321,18 @@ template <typename T, int D, int RT, bool APART = false> __device__ __forceinlin
         // tokens that not all rows see
         const bool edge = __any(page < 0) || j + kTile > p_min + 1 || j + kTile > tiles.high || (j < tiles.low && j + kTile > tiles.sinks) ||
                           (a.window && j + kTile > tiles.sinks && (int64_t)j <= (int64_t)p_max - a.window);
+        float vs[kQuarters];
         uint32_t most_vs = 0;
 #pragma unroll
-        for (int h = 0; h < kQuarters; h++) most_vs = max(most_vs, __float_as_uint(scale_in(kQuarters + h)));
-        float less;
-        if (value_scale.grows(most_vs, less)) {
-#pragma unroll
-            for (int rt = 0; rt < RT; rt++)
-#pragma unroll
-                for (int dt = 0; dt < DT; dt++) o[rt][dt] *= less;
-        }
+        for (int h = 0; h < kQuarters; h++) vs[h] = scale_in(kQuarters + h), most_vs = max(most_vs, __float_as_uint(vs[h]));
         f16x8 w[RT][kQuarters / 2];
 #pragma unroll
         for (int rt = 0; rt < RT; rt++) {
+            uint32_t row_vs = most_vs; // of what the row sees
             if (edge) {
+                row_vs = 0;
+#pragma unroll
+                for (int h = 0; h < kQuarters; h++) row_vs = max(row_vs, seen[rt].some_of16(j + 16 * h) ? __float_as_uint(vs[h]) : 0u);
 #pragma unroll
                 for (int h = 0; h < kQuarters; h++) {
                     const bool is_there = page_of(page, h) >= 0;
@@ -335,7 +346,12 @@ template <typename T, int D, int RT, bool APART = false> __device__ __forceinlin
             float top = -INFINITY;
 #pragma unroll
             for (int h = 0; h < kQuarters; h++) top = fmaxf(top, fmaxf(fmaxf(s[rt][h][0], s[rt][h][1]), fmaxf(s[rt][h][2], s[rt][h][3])));
-            top = fmaxf(m[rt], max_over_16(top));
+            if (value_scale[rt].may_grow(most_vs)) {
+                const float less = value_scale[rt].take_in(row_vs);
+#pragma unroll
+                for (int dt = 0; dt < DT; dt++) o[rt][dt] *= less;
+            }
+            top = fmaxf(m[rt], max_over_16(top) - kLiftFew);
             const float ref = top == -INFINITY ? 0.0f : top;
             const float fade = exp2_of(m[rt] - ref);
             m[rt] = top;
@@ -346,9 +362,9 @@ template <typename T, int D, int RT, bool APART = false> __device__ __forceinlin
 #pragma unroll
                 for (int i = 0; i < 8; i++) e[i] = exp2_of(s[rt][2 * u + i / 4][i % 4] - ref);
                 sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-                const float vs[2] = {scale_in(kQuarters + 2 * u) * value_scale.by<kLiftFew>(), scale_in(kQuarters + 2 * u + 1) * value_scale.by<kLiftFew>()};
+                const float share[2] = {value_scale[rt].share(vs[2 * u]), value_scale[rt].share(vs[2 * u + 1])};
 #pragma unroll
-                for (int i = 0; i < 8; i++) e[i] *= vs[i / 4];
+                for (int i = 0; i < 8; i++) e[i] *= share[i / 4];
                 w[rt][u] = __builtin_convertvector(e, f16x8);
             }
             l[rt] = l[rt] * fade + sum;
@@ -376,7 +392,7 @@ template <typename T, int D, int RT, bool APART = false> __device__ __forceinlin
     // the wavefronts' sums, brought to one maximum and added up in their order
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) {
-        l[rt] = sum_over_16(l[rt]);
+        l[rt] = sum_over_16(l[rt]) * __uint_as_float((127u - kLiftFew) << 23), m[rt] += kLiftFew;
         if (l[rt] != l[rt] && m[rt] == -INFINITY) m[rt] = 0.0f; // saw scores, none of them a number
         if (g == 0) lds.m[wave][rt * 16 + c] = m[rt], lds.l[wave][rt * 16 + c] = l[rt];
     }
@@ -386,7 +402,7 @@ template <typename T, int D, int RT, bool APART = false> __device__ __forceinlin
         const uint32_t r = rt * 16 + c;
         const float top = fmaxf(fmaxf(lds.m[0][r], lds.m[1][r]), fmaxf(lds.m[2][r], lds.m[3][r]));
         // (the largest scale, and what the weights were lifted by, in two steps: neither product leaves the range)
-        const float f = m[rt] == -INFINITY ? 0.0f : exp2_of(m[rt] - top - kLiftFew) * value_scale.value();
+        const float f = m[rt] == -INFINITY ? 0.0f : exp2_of(m[rt] - top - kLiftFew) * value_scale[rt].value();
         if (rt) __syncthreads();
 #pragma unroll
         for (int dt = 0; dt < DT; dt++)
@@ -546,7 +562,7 @@ template <typename T, int D, int WAVES> __device__ __forceinline__ void many_row
     const Seen seen(my_p, there, a.window, a.sinks);
     f16x8 q[KS];
     f32x16 o[DT];
-    float ref = 0.0f; // what the weights are relative to, in powers of two
+    float ref = 0.0f; // what the weights are relative to, in powers of two: kLiftMany or more below the largest score
     bool any = false; // a score has been seen
     float l = 0.0f;
     const T *q_src = static_cast<const T *>(a.q) + my_packed * a.q_row + my_head * a.q_head + 8 * half;
@@ -564,6 +580,7 @@ template <typename T, int D, int WAVES> __device__ __forceinline__ void many_row
 #pragma unroll
     for (int i = 0; i < KS; i++) q[i] = as_f16(raw[i]);
     ValueScale value_scale;
+    value_scale.begin(my_row < n);
 #pragma unroll
     for (int dt = 0; dt < DT; dt++) o[dt] = f32x16{};
 
@@ -715,10 +732,17 @@ template <typename T, int D, int WAVES> __device__ __forceinline__ void many_row
                 __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
             __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+            uint32_t most_vs = 0;
+#pragma unroll
+            for (int u = 0; u < 2 * HT; u++) most_vs = max(most_vs, vs[u]);
+            uint32_t row_vs = most_vs; // of what the row sees
             if (flags & kEdge) {
                 const int32_t j = first_token(t);
                 Seen here = seen;
                 here.high = min(here.high, end_of(flags));
+                row_vs = 0;
+#pragma unroll
+                for (int u = 0; u < 2 * HT; u++) row_vs = max(row_vs, here.some_of16(j + 16 * u) ? vs[u] : 0u);
 #pragma unroll
                 for (int h = 0; h < HT; h++)
 #pragma unroll
@@ -737,10 +761,10 @@ template <typename T, int D, int WAVES> __device__ __forceinline__ void many_row
                 top = fmaxf(top, fmaxf(most, s[u / 2][8 * (u % 2) + 7]) * scale[u]);
             }
             top = max_over_32(top);
-            // The reference moves, to the largest score so far, only when one is so far above it that its weight would exceed 2^8: what has been
-            // added up is scaled now and then, not for every tile.
-            if (__any(top - ref > 8.0f || (!any && top != -INFINITY))) {
-                const float next = any ? fmaxf(ref, top) : top == -INFINITY ? 0.0f : top;
+            // The reference moves, to kLiftMany below the largest score so far, only when one is so far above it that its weight would exceed
+            // 2^(kLiftMany + 8): what has been added up is scaled now and then, not for every tile.
+            if (__any(top - ref > kLiftMany + 8.0f || (!any && top != -INFINITY))) {
+                const float next = any ? fmaxf(ref, top - kLiftMany) : top == -INFINITY ? 0.0f : top - kLiftMany;
                 const float fade = any ? exp2_of(ref - next) : 0.0f;
                 any = any || top != -INFINITY;
                 l *= fade;
@@ -748,15 +772,11 @@ template <typename T, int D, int WAVES> __device__ __forceinline__ void many_row
                 for (int dt = 0; dt < DT; dt++) o[dt] *= fade;
                 ref = next;
             }
-            uint32_t most_vs = 0;
-#pragma unroll
-            for (int u = 0; u < 2 * HT; u++) most_vs = max(most_vs, vs[u]);
-            float less;
-            if (value_scale.grows(most_vs, less)) {
+            if (__any(value_scale.below(most_vs))) {
+                const float less = value_scale.take_in(row_vs);
 #pragma unroll
                 for (int dt = 0; dt < DT; dt++) o[dt] *= less;
             }
-            const float vs_by = value_scale.by<kLiftMany>();
             f16x8 w[kGroups], y[kAhead];
 #pragma unroll
             for (int i = 0; i < kAhead; i++) y[i] = v_operand(i, buffer);
@@ -766,7 +786,7 @@ template <typename T, int D, int WAVES> __device__ __forceinline__ void many_row
 #pragma unroll
                 for (int i = 0; i < 8; i++) e[i] = exp2_of(__builtin_fmaf(s[u / 2][8 * (u % 2) + i], scale[u], -ref));
                 l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-                w[u] = __builtin_convertvector(e * (__uint_as_float(vs[u]) * vs_by), f16x8);
+                w[u] = __builtin_convertvector(e * value_scale.share(__uint_as_float(vs[u])), f16x8);
             }
 #pragma unroll
             for (int i = 0; i < kGroups * DT; i++) {
@@ -792,9 +812,9 @@ template <typename T, int D, int WAVES> __device__ __forceinline__ void many_row
     }
 
     const f32x2 both = swapped32(l);
-    const float total = both[0] + both[1];
+    const float total = (both[0] + both[1]) * __uint_as_float((127u - kLiftMany) << 23);
     // what the weights are relative to (also if the row saw scores and none was a number)
-    const float top = any || total != total ? ref : -INFINITY;
+    const float top = any || total != total ? ref + kLiftMany : -INFINITY;
     if (my_row >= n) return;
     uint32_t row = my_row; // where the results go is worked out here, not kept in registers from the beginning
     dcdev::anew(row);
