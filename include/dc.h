@@ -505,7 +505,7 @@ int dc_gemv_i8(const int8_t *q_dev, const float *row_scale_dev, uint32_t rows, u
  * element [page][head][token][i], i < head_dim, type bf16 or f16.  16-byte aligned; offsets are 64-bit.
  * A cache of DC_TYPE_I8 holds whole numbers of 8 bits: the value that element [page][head][token][i] stands for is that number times
  * scale [page][head][token / scale_tokens], of keys in k_scale_dev, of values in v_scale_dev.  Half the room and half the reading of 16 bits.
- * Scales are numbers above 0 (one that is not, or is NaN, counts as 2^-126).  What calls write as "type of the cache" is rows_type then.
+ * Scales are numbers from 2^-126 to 2^127 (one below, or NaN, counts as 2^-126, one above as 2^127).  What calls write as "type of the cache" is rows_type then.
  *
  * Batch.  Sequence b has len_dev[b] tokens, the new ones included; its new tokens are its last ones and their rows
  * (queries, keys, values, results) stand one after the other: rows row_start_dev[b] .. row_start_dev[b+1]-1.

@@ -37,8 +37,10 @@ def rotate32(x: np.ndarray, cos: np.ndarray, sin: np.ndarray, neighbours: bool) 
 
 
 def whole(x: np.ndarray, scale) -> np.ndarray:
+    """The whole numbers nearest to x / scale.  A quotient of two fp32 numbers below 128 that is not the middle between two whole numbers is at least 2^-27 away from it,
+    and its rounding in fp64 is off by 2^-47 at most."""
     with np.errstate(invalid="ignore", over="ignore"):
-        n = np.clip(np.rint(np.asarray(x, np.float32) * (np.float32(1) / np.float32(scale))), -127, 127)
+        n = np.clip(np.rint(np.asarray(x, np.float32).astype(np.float64) / np.float64(np.float32(scale))), -127, 127)
     return np.where(np.isnan(n), 0, n).astype(np.int8)
 
 
@@ -81,8 +83,8 @@ def append(k_pages, v_pages, k_scales, v_scales, batch, block: int, k, v, cos, s
                         old = sound(scales[which][page, h, n])
                         s = max(s, old)
                         if s != old:  # the tokens before the sequence's first new one
-                            numbers = pools[which][page, h, n * block:start[1]].astype(np.float32)
-                            pools[which][page, h, n * block:start[1]] = np.rint(numbers * (old * (np.float32(1) / s))).astype(np.int8)
+                            numbers = pools[which][page, h, n * block:start[1]].astype(np.float64)  # s is a power of two: exact
+                            pools[which][page, h, n * block:start[1]] = np.rint(numbers * np.float64(old) / np.float64(s)).astype(np.int8)
                     for place, kr, vr in new:
                         pools[which][page, h, place] = whole((kr, vr)[which][h], s)
                     scales[which][page, h, n] = s

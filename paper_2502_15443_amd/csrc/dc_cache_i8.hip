@@ -2,7 +2,7 @@
 // with a scale for each block of tokens of a head.
 //
 // A block's scale is the smallest power of two s >= 2^-126 with |x| <= 127 s for its values; a value is held as the whole number nearest to
-// x / s, which for a power of two is x times its reciprocal, exactly.  A block that the call's rows do not reach back to the beginning of has
+// x / s, which for a power of two is x times its reciprocal, exactly (for a scale that somebody else wrote and that is none, see nearest).  A block that the call's rows do not reach back to the beginning of has
 // earlier tokens: its scale only grows, and then their numbers are rounded to the larger steps.  So the call must see all of a block's new rows
 // together: the row that is the first of its block in this call takes care of the block (its leader).
 #include "dc_cache.h"
@@ -157,39 +157,77 @@ struct Most {
     }
 };
 
-// The whole numbers nearest to 8 values times `by`, as bytes: added to 1.5 2^23, a number of up to 127 is rounded to the nearest whole one, ties to even,
-// and its low byte is what is wanted.  Infinities are 127 with their sign, NaN is 0.
-__device__ __forceinline__ u32x2 whole_numbers(const f32x8 &x, float by, bool numbers)
+__device__ __forceinline__ bool power_of_two(float s) { return (__float_as_uint(s) & 0x7FFFFFu) == 0; }
+// The whole number nearest to x / s, ties to even: rint(x / s) with a quotient that may be off in its last bits, or one of that number's neighbours.  Which side of
+// the middle between two x lies on comes out of one rounding, which leaves the sign and zero as they are: what small scales take below the normal range is
+// lifted by 2^64 before.
+__device__ __forceinline__ int32_t nearest(float x, float s, float quotient)
+{
+    const float lift = s < 1.0f ? 0x1p64f : 1.0f, n = rintf(quotient);
+    x *= lift, s *= lift;
+    const float above = __builtin_fmaf(-(n + 0.5f), s, x), below = __builtin_fmaf(-(n - 0.5f), s, x);
+    const int32_t i = (int32_t)n;
+    return i + (above > 0.0f || (above == 0.0f && (i & 1))) - (below < 0.0f || (below == 0.0f && (i & 1)));
+}
+
+// The whole numbers nearest to 8 values / scale, as bytes, of which `by` is the reciprocal.  A power of two's is exact; added to 1.5 2^23, a number of up to 127 is
+// rounded to the nearest whole one, ties to even, and its low byte is what is wanted.  Infinities are 127 with their sign, NaN is 0.
+// plain: the values are numbers, and the scale a power of two.
+__device__ __forceinline__ u32x2 whole_numbers(const f32x8 &x, float scale, float by, bool plain)
 {
 #pragma clang fp contract(off)
-    uint32_t n[8];
-#pragma unroll
-    for (int i = 0; i < 8; i++) n[i] = __float_as_uint(x[i] * by + 12582912.0f);
-    if (!numbers) {
-        dcdev::keep_order();
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const uint32_t u = __float_as_uint(x[i]);
-            if ((u & 0x7FFFFFFFu) >= 0x7F800000u) n[i] = u & 0x7FFFFFu ? 0u : (u >> 31 ? (uint32_t)-127 : 127u);
-        }
-    }
     u32x2 w;
+    if (plain) {
+        uint32_t n[8];
 #pragma unroll
-    for (int h = 0; h < 2; h++) {
-        const uint32_t low = __builtin_amdgcn_perm(n[4 * h + 1], n[4 * h], 0x0C0C0400u), high = __builtin_amdgcn_perm(n[4 * h + 3], n[4 * h + 2], 0x0C0C0400u);
-        w[h] = __builtin_amdgcn_perm(high, low, 0x05040100u);
+        for (int i = 0; i < 8; i++) n[i] = __float_as_uint(x[i] * by + 12582912.0f);
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const uint32_t low = __builtin_amdgcn_perm(n[4 * h + 1], n[4 * h], 0x0C0C0400u), high = __builtin_amdgcn_perm(n[4 * h + 3], n[4 * h + 2], 0x0C0C0400u);
+            w[h] = __builtin_amdgcn_perm(high, low, 0x05040100u);
+        }
+    } else { // hardly ever: short rather than fast
+        f32x8 left = x;
+        uint64_t bytes = 0;
+#pragma unroll 1
+        for (int i = 0; i < 8; i++) {
+            const uint32_t u = __float_as_uint(left[0]), most = u >> 31 ? (uint32_t)-127 : 127u;
+            const uint32_t n = (u & 0x7FFFFFFFu) < 0x7F800000u ? (uint32_t)nearest(left[0], scale, left[0] * by) : u & 0x7FFFFFu ? 0u : most;
+            bytes = bytes >> 8 | (uint64_t)n << 56;
+            left = __builtin_shufflevector(left, left, 1, 2, 3, 4, 5, 6, 7, 0);
+        }
+        w = u32x2{(uint32_t)bytes, (uint32_t)(bytes >> 32)};
     }
     return w;
 }
-// 16 bytes' whole numbers times `by`, rounded.
-__device__ __forceinline__ dcdev::u32x4 in_larger_steps(const dcdev::u32x4 &from, float by)
+// 16 bytes' whole numbers of a scale `before`, of a larger one that is a power of two and has the reciprocal `by`.
+__device__ __forceinline__ dcdev::u32x4 in_larger_steps(const dcdev::u32x4 &from, float before, float by)
 {
     dcdev::u32x4 to;
+    const float less = before * by;
+    if (power_of_two(before)) {
 #pragma unroll
-    for (int k = 0; k < 4; k++) {
-        to[k] = 0;
+        for (int k = 0; k < 4; k++) {
+            to[k] = 0;
 #pragma unroll
-        for (int i = 0; i < 4; i++) to[k] |= ((uint32_t)(int32_t)rintf((float)(int8_t)(from[k] >> (8 * i)) * by) & 255u) << (8 * i);
+            for (int i = 0; i < 4; i++) to[k] |= ((uint32_t)(int32_t)rintf((float)(int8_t)(from[k] >> (8 * i)) * less) & 255u) << (8 * i);
+        }
+    } else { // (the product of a number and such a scale can be rounded to the middle between two)
+        dcdev::u32x4 left = from;
+        to = dcdev::u32x4{};
+#pragma unroll 1
+        for (int k = 0; k < 16; k++) {
+            const float q = (float)(int8_t)left[0], n = rintf(q * less);
+            const float above = __builtin_fmaf(q, less, -(n + 0.5f)), below = __builtin_fmaf(q, less, -(n - 0.5f));
+            const int32_t whole = (int32_t)n, i = whole + (above > 0.0f || (above == 0.0f && (whole & 1))) - (below < 0.0f || (below == 0.0f && (whole & 1)));
+            // all 16 bytes by one: out at the low end, in at the high end
+            const dcdev::u32x4 next_left = {left[1], left[2], left[3], 0u}, next_to = {to[1], to[2], to[3], (uint32_t)i};
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                left[j] = (uint32_t)(((uint64_t)next_left[j] << 32 | left[j]) >> 8);
+                to[j] = (uint32_t)(((uint64_t)next_to[j] << 32 | to[j]) >> 8);
+            }
+        }
     }
     return to;
 }
@@ -255,20 +293,20 @@ template <typename X, int D, bool NEIGHBOURS, bool QUERIES, bool KEYS> __device_
         if (!any || p.entry < 0) continue;
         uint8_t *dst = static_cast<uint8_t *>(is_k ? a.k_pages : a.v_pages) + ((head_at << a.batch.page_shift) + p.in_page) * D;
         const float scale = fmaxf(scale_for(most), before), by = reciprocal(scale);
+        const bool plain = numbers & power_of_two(scale);
 #pragma unroll 1
         for (uint32_t i = 0; i < p.count; i++) {
             if (i) v = values(i, given);
             if (!given) continue;
-            *reinterpret_cast<u32x2 *>(dst + i * D + u.first) = whole_numbers(v.x, by, numbers);
-            *reinterpret_cast<u32x2 *>(dst + i * D + u.second) = whole_numbers(v.y, by, numbers);
+            *reinterpret_cast<u32x2 *>(dst + i * D + u.first) = whole_numbers(v.x, scale, by, plain);
+            *reinterpret_cast<u32x2 *>(dst + i * D + u.second) = whole_numbers(v.y, scale, by, plain);
         }
         if (in_block && scale != before) {
-            const float less = before * by;
             uint8_t *at = dst - in_block * D + 16 * unit;
 #pragma unroll 2
             for (uint32_t i = 0; i < in_block; i++) {
                 dcdev::u32x4 *e = reinterpret_cast<dcdev::u32x4 *>(at + i * D);
-                *e = in_larger_steps(*e, less);
+                *e = in_larger_steps(*e, before, by);
             }
         }
         if (unit == 0) *scale_at = scale;
@@ -391,21 +429,21 @@ template <typename X, int D, bool NEIGHBOURS, int ROWS, bool BIG> __device__ __f
                 }
                 if (!most) continue;
                 const float scale = fmaxf(scale_for(__uint_as_float(most - 1u)), before), by = reciprocal(scale);
+                const bool plain = numbers & power_of_two(scale);
                 uint8_t *dst = pages + (((page * a.n_kv_heads + head) << a.batch.page_shift) + in_page) * D;
                 auto store = [&](uint32_t n, const Values &x) {
-                    *reinterpret_cast<u32x2 *>(dst + n * D + u.first) = whole_numbers(x.x, by, numbers);
-                    *reinterpret_cast<u32x2 *>(dst + n * D + u.second) = whole_numbers(x.y, by, numbers);
+                    *reinterpret_cast<u32x2 *>(dst + n * D + u.first) = whole_numbers(x.x, scale, by, plain);
+                    *reinterpret_cast<u32x2 *>(dst + n * D + u.second) = whole_numbers(x.y, scale, by, plain);
                 };
 #pragma unroll
                 for (int i = 0; i < kRows; i++)
                     if (given[i]) store(token + i * tokens, v[i]);
                 further(src, store);
                 if (in_block && scale != before) {
-                    const float less = before * by;
 #pragma unroll 1
                     for (uint32_t i = token; i < in_block; i += tokens) {
                         dcdev::u32x4 *e = reinterpret_cast<dcdev::u32x4 *>(dst - (in_block - i) * D + 16 * unit);
-                        *e = in_larger_steps(*e, less);
+                        *e = in_larger_steps(*e, before, by);
                     }
                 }
                 if (t == 0) *scale_at(head) = scale;
