@@ -640,6 +640,9 @@ int dc_attention_paged(const dc_kv_cache *cache, const dc_kv_batch *batch, const
  * the order of sequences and entries, and go back to its end in that order; what goes back in a call is not taken in it.  Where none is left entries stay
  * -1, and queue_dev[2] counts them: the program gives such a sequence's tokens again once there are pages, or ends a sequence.
  * A program begins with every page in the ring and every entry -1, and holds no page twice; a common prefix's pages are in neither.
+ * A sequence that begins behind a common prefix holds its tokens already: held_dev[b] is prefix_len.  (With fewer its first new tokens would be the prefix's, and
+ * dc_kv_append would write them into the pages that all sequences share.)  Steps in place leave 0 in len_dev[b] of a sequence that is over: where another one
+ * takes its place, the program makes that prefix_len before, on the stream or in the recorded step (the larger of held_dev[b] and prefix_len will do).
  *
  * Results: len_dev[b] = h + n (which has to stay below 2^31) and row_start_dev as in dc_kv_batch, rows one after the other.  If the rows are more than n_rows, those
  * beyond are cut: row starts are at most n_rows, and len_dev[b] counts the rows that there are.  For each row slot_dev (place in the
