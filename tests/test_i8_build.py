@@ -49,3 +49,22 @@ def test_no_access_takes_more_than_16_bytes_for_granted(source):
     accesses = re.findall(r"^.*(?:\bload |\bstore ).*\balign (\d+)", ir, re.M)
     assert len(accesses) > 100
     assert max(int(a) for a in accesses) == 16
+
+
+def test_registers_of_the_kernels_for_mixed_batches_and_of_the_append(assembly):
+    """No vector register goes to memory, but for one of heads of 64, of which three workgroups share a compute unit; scalar ones that do not fit are lanes of at most two."""
+    most = {64: 168, 128: 256, 256: 512}
+    seen = {"mixed": 0, "rows": 0, "blocks": 0, "both": 0}
+    for source in SOURCES[:2]:
+        for kernel in assembly[source].split("amdhsa.kernels:")[1].split("\n  - ."):
+            value = dict(re.findall(r"^\s*\.(\w+): +(\S+)$", kernel, re.M))
+            m = re.search(r"dc_(attention|kv_append)_i8_(mixed|rows|blocks|both)_kernelI\w+?Li(\d+)(?:ELb[01]ELi(\d))?", value.get("name", ""))
+            if not m or (m.group(1) == "attention") != (m.group(2) == "mixed"):
+                continue
+            seen[m.group(2)] += 1
+            # the append's blocks that are a workgroup's (rows to a thread: 0) have up to 1024 threads
+            limit = most[int(m.group(3))] if m.group(2) == "mixed" else 128 if m.group(4) == "0" else 256
+            assert int(value["vgpr_count"]) <= limit, value["name"]
+            assert int(value["vgpr_spill_count"]) <= (1 if m.group(2) == "mixed" and m.group(3) == "64" else 0), value["name"]
+            assert int(value["sgpr_spill_count"]) <= 128, value["name"]
+    assert seen == {"mixed": 16, "rows": 54, "blocks": 54, "both": 36}
