@@ -100,17 +100,6 @@ __device__ __forceinline__ float sum_over_16(float v)
     return r[0] + r[1];
 }
 
-// Largest of the lanes' values.
-__device__ __forceinline__ uint32_t largest_of_lanes(uint32_t v)
-{
-    v = max(v, dcdev::dpp_or_zero<0x111, 0xF>(v));
-    v = max(v, dcdev::dpp_or_zero<0x112, 0xF>(v));
-    v = max(v, dcdev::dpp_or_zero<0x114, 0xF>(v));
-    v = max(v, dcdev::dpp_or_zero<0x118, 0xF>(v));
-    v = max(v, dcdev::dpp_or_zero<0x142, 0xA>(v));
-    v = max(v, dcdev::dpp_or_zero<0x143, 0xC>(v));
-    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
-}
 // Smallest and largest of the lanes' positions but kNoPosition; both are that if there is none.
 __device__ __forceinline__ void range_of_positions(int32_t p_low, int32_t p_high, int32_t &low, int32_t &high)
 {

@@ -35,9 +35,6 @@ __device__ __forceinline__ u32x2 lds_column8(uint32_t addr)
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2 *)(uintptr_t)addr));
 }
 
-// A scale that is read: a number above 0.
-__device__ __forceinline__ float sound_scale(float s) { return fminf(fmaxf(s, 0x1p-126f), 0x1p127f); }
-
 // Queries as f16.  Those of bf16 are brought to a largest one of 2^14 to 2^15 by a power of two, of which the score gets the reciprocal: the 8 bits of
 // all that are above 2^-29 times the largest stay as they are, and those below are off by 2^-40 of it at most, far less than the sum's own roundings.
 // `most`: largest of the row's values, as bits without sign.

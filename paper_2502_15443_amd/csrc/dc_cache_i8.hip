@@ -51,19 +51,6 @@ __device__ __forceinline__ float reciprocal(float s)
     const uint32_t u = __float_as_uint(s);
     return u & 0x7FFFFFu || u > 253u << 23 ? 1.0f / s : __uint_as_float((254u << 23) - u);
 }
-// Largest of the lanes' numbers, which are at least 0; the same in all lanes.
-__device__ __forceinline__ uint32_t largest_of_lanes(uint32_t v)
-{
-    v = max(v, dcdev::dpp_or_zero<0x111, 0xF>(v));
-    v = max(v, dcdev::dpp_or_zero<0x112, 0xF>(v));
-    v = max(v, dcdev::dpp_or_zero<0x114, 0xF>(v));
-    v = max(v, dcdev::dpp_or_zero<0x118, 0xF>(v));
-    v = max(v, dcdev::dpp_or_zero<0x142, 0xA>(v));
-    v = max(v, dcdev::dpp_or_zero<0x143, 0xC>(v));
-    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
-}
-// A scale that is read: a number above 0.
-__device__ __forceinline__ float sound_scale(float s) { return fminf(fmaxf(s, 0x1p-126f), 0x1p127f); }
 
 // A thread's 16 values of a head, in two groups of 8 that hold whole pairs.
 struct Values {

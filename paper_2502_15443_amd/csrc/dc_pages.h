@@ -1,5 +1,5 @@
-// What the kernels over a paged cache of keys and values share: the batch as they see it, where a row and a token are, and the
-// host's checks of both descriptions.
+// What the kernels over a paged cache of keys and values share: the batch as they see it, where a row and a token are, how scales are read, and
+// the host's checks of both descriptions.
 #ifndef DC_PAGES_H
 #define DC_PAGES_H
 
@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "dc.h"
+#include "dc_device.h"
 
 namespace dcpages {
 
@@ -59,6 +60,21 @@ struct Batch {
         return n_seqs;
     }
 };
+
+// Largest of the lanes' values; the same in all lanes.
+__device__ __forceinline__ uint32_t largest_of_lanes(uint32_t v)
+{
+    v = max(v, dcdev::dpp_or_zero<0x111, 0xF>(v));
+    v = max(v, dcdev::dpp_or_zero<0x112, 0xF>(v));
+    v = max(v, dcdev::dpp_or_zero<0x114, 0xF>(v));
+    v = max(v, dcdev::dpp_or_zero<0x118, 0xF>(v));
+    v = max(v, dcdev::dpp_or_zero<0x142, 0xA>(v));
+    v = max(v, dcdev::dpp_or_zero<0x143, 0xC>(v));
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
+// A scale of a cache of 8 bits as it is read: a number above 0.
+__device__ __forceinline__ float sound_scale(float s) { return fminf(fmaxf(s, 0x1p-126f), 0x1p127f); }
 
 inline bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 
