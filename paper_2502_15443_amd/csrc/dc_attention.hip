@@ -1062,7 +1062,7 @@ bool make_plan_by(uint32_t most_rows, AttentionArgs &a, Plan &plan, const dc_kv_
         if (!a.whole) a.own = many_part(false);
         if (!a.own.blocks) return false;
         // Over a cache of 8 bits sequences of at most 16 rows, which may be among them, are taken as few rows, in as many parts as the others; without a prefix in
-        // parts of their own, and joined by a launch of their own, where those would be long, of which one reads 80 tokens a us (us: as many parts, and their own: 2048
+        // parts of their own, and joined by a launch of their own, where those would be long, of which one reads 80 tokens a us (heads of 128; us: as many parts, and their own: 2048
         // new tokens and 4 sequences of one token over 32768 335 and 168, and one over 100000 798 and 172; but 512 and 32 of one over 4096 114 and 131).
         if (cache->type == DC_TYPE_I8 && !a.whole && batch->row_start_dev && batch->n_seqs > 1 && group <= 16) {
             const uint64_t items = (uint64_t)cache->n_kv_heads * batch->n_seqs, tokens = seen(own_len, 16), n_tiles = std::max<uint64_t>(1, (tokens + tile_few - 1) / tile_few);

@@ -117,9 +117,9 @@ private:
 // the tile; two quarters are the second operand of [head_dim][row] = V^T P^T if the product's 32 tokens are numbered that way.  K and then V go through
 // registers into the wavefront's own part of the LDS, as bytes, and become f16 on their way to the products: of K a lane reads 16 neighbouring values of a
 // token, for two products; of V the transposing read gives it 8 tokens of one value.  No barrier in the loop; the next tile's loads are under way during the
-// rest of the tile's work.  64 sequences of 4096 tokens, 32 heads on 8 of 128: 87 us, 6.2 TB/s; where lengths differ by up to 16, 122 us, 4.9 TB/s, for
-// sequences end at unlike times (shares of equal length, cut on the device: 118 to 126, the alike ones 93 to 103); one of 131071 tokens 51 us.  A tile of 64
-// tokens takes 590 vector operations and 211 registers, for two workgroups a compute unit (three, of 168, spill: 84 us).
+// rest of the tile's work.  64 sequences of 4096 tokens, 32 heads on 8 of 128: 88 us, 6.1 TB/s; where lengths differ by up to 16, 121 us, 4.9 TB/s, for
+// sequences end at unlike times (shares of equal length, cut on the device: 118 to 126, the alike ones 93 to 103); one of 131071 tokens 52 us.  A tile of 64
+// tokens takes 590 vector operations and 210 registers, for two workgroups a compute unit (three, of 168, spill: 84 us).
 template <int D, int RT> struct FewLds {
     static constexpr int kPadded = D + 4; // floats of a row's sums
     union {
@@ -438,8 +438,8 @@ template <typename T, int D, int RT, bool APART = false> __device__ __forceinlin
 // wavefronts share, made 16 bits wide on their way, double buffered with one barrier a tile; a wavefront owns 32 rows.  Scores as [token][row] = K Q^T, results as [head_dim][row] = V^T P^T in the 32x32x16 shape; maxima and
 // sums stay in a lane but for one exchange between the halves.
 //
-// 32 heads of 128, 8 of keys and values, 2048 tokens behind 6144: 272 us, 885 TFLOP/s, the matrix units busy 35 % and the vector units 47 % of the cycles; a
-// prompt of 4096 with 32 heads of each 168 us, 820 TFLOP/s (by 128 rows 188: a tile is made wide for half the rows); heads of 64 109 us, 630 TFLOP/s.  With the
+// 32 heads of 128, 8 of keys and values, 2048 tokens behind 6144: 275 us, 875 TFLOP/s, the matrix units busy 37 % and the vector units 52 % of the cycles; a
+// prompt of 4096 with 32 heads of each 168 us, 820 TFLOP/s (by 128 rows 188: a tile is made wide for half the rows); heads of 64 110 us, 625 TFLOP/s.  With the
 // value scale in the exponent, a multiplication less, registers spill for heads of 64 (215 us), and heads of 128 gain nothing.  Little work costs latency: a
 // workgroup's first tile begins 4.5 us after the launch, and its results take 2 us.
 template <int D, int WAVES> struct TileLds {

@@ -303,8 +303,8 @@ template <typename X, int D, bool NEIGHBOURS, bool QUERIES, bool KEYS> __device_
 // The blocks led by a row among `block` neighbouring ones that have more than `few` new rows, of some heads of the keys or of the values, one after the
 // other.  A team of threads has a head's block, each of them 16 values of ROWS rows, whose cosines and sines it keeps for all heads.
 // Small blocks (up to 2048 values) are a wavefront's: no barrier; else the team is the workgroup, of 256 to 1024 threads, and the next head's values
-// are on their way while this head's maximum is found.  8192 rows of 40 heads of 128 in blocks of 64: 58 us for 252 MB, 4.3 TB/s, the vector units busy 44 % (14
-// operations a value); what is under way at once bounds it, and neither two heads ahead (no change) nor two blocks a team (212 registers, 167 us) gives more.
+// are on their way while this head's maximum is found.  8192 rows of 40 heads of 128 in blocks of 64: 59 us for 252 MB, 4.3 TB/s, the vector units busy 46 % (14
+// operations a value); 1280 workgroups of 512 threads meet 512 places, which hold what is under way at once, and neither two heads ahead (no change) nor two blocks a team (212 registers, 167 us) gives more.
 // BIG: a block has more than 16 values for each of 1024 threads; those of its further rows are read twice.
 template <typename X, int D, bool NEIGHBOURS, int ROWS, bool BIG> __device__ __forceinline__ void append_blocks(const AppendArgs &a, uint32_t few, uint32_t group, bool is_k, uint32_t head_first,
                                                                                                                 uint32_t heads, uint32_t (&lds_most)[2][kMostThreads / 64])
@@ -518,8 +518,8 @@ template <typename X, int D, bool NEIGHBOURS, int ROWS, bool BIG> void launch_n(
     }
     const uint32_t row_threads = rows >= 512 && slots * (D / 16) <= 128 ? 64 : kThreads;
     // A sequence has at most two blocks with few rows, its first and its last one: beside many blocks they are the same kernel's (8192 rows of 40/40 heads of
-    // 128 94 us, with a launch for them 101; 2048 rows of 32/8 14.2 and 16.4).  Queries have a launch of their own, 36 us for 168 MB of 40 heads; mixed with the
-    // blocks' in one, 2048 rows take 13.3 us, but 8192 104.
+    // 128 94 us, with a launch for them 101; 2048 rows of 32/8 14.2 and 16.4).  Queries have a launch of their own, 36 us for 168 MB of 40 heads (256 threads
+    // have 32 heads at a time: of the second time three quarters are idle); mixed with the blocks' in one, 2048 rows take 13.3 us, but 8192 104.
     BlockWork all = b;
     if ((uint64_t)a.batch.n_seqs * 16 <= rows >> a.block_shift) all.few = 0;
     hipLaunchKernelGGL((dc_kv_append_i8_blocks_kernel<X, D, NEIGHBOURS, ROWS, BIG>), dim3((uint32_t)std::min(b.items, kMostItems)), dim3(threads), 0, stream, a, all);
