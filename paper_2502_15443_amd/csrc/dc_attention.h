@@ -133,8 +133,8 @@ struct Seen {
         sinks = (int32_t)min((int64_t)high, max(sinks_left, (int64_t)0));
     }
     __device__ __forceinline__ bool token(int32_t j) const { return (j < high) & ((j >= low) | (j < sinks)); }
-    // one of 16 tokens from j on
-    __device__ __forceinline__ bool some_of16(int32_t j) const { return (j < high) & ((j + 16 > low) | (j < sinks)); }
+    // one of 16 tokens from j on (there may be none between low and high)
+    __device__ __forceinline__ bool some_of16(int32_t j) const { return (max(low, j) < min(high, j + 16)) | (j < min(sinks, high)); }
 };
 
 // The keys of one part that the rows of a workgroup see, as tiles of TILE tokens: the tiles with sinks, then those from the window's

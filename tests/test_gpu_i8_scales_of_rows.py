@@ -88,6 +88,19 @@ def test_one_block_far_above_the_others(heads, kv_heads, news, d):
 
 
 @pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("heads,kv_heads,news", ROWS + [(8, 2, [1] * 40)])
+@pytest.mark.parametrize("prefix", [97, 101, 111])
+def test_the_end_of_the_prefix(heads, kv_heads, news, prefix, d):
+    """The prefix ends inside its last block, whose scale is 2^100; rows' windows begin before, in and behind that block, and where its 16 tokens would end."""
+    def change(p):
+        p["vs"][p["batch"]["prefix_pages"][-1], :, 0] = 2.0 ** 100
+
+    lens = [prefix + n + i % 40 for i, n in enumerate(news)]
+    for window, sinks in ((5, 0), (20, 0), (33, 97), (33, 98)):
+        run("bf16", heads, kv_heads, d, 16, 16, lens, news, (-6, -4), window, sinks, prefix=prefix, uniform=len(news) == 40, change=change)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("news", [[1], [9], [150]])
 def test_the_smallest_scales(news, d):
     """All of a sequence's values at the smallest scale there is."""
